@@ -25,7 +25,7 @@
  *   - Random numbers: Philox4x32-10, key = seed, counter = (row, feature / 4, epoch * 256 + stream),
  *     output word feature % 4, the top 24 bits as a uniform in [0,1).  Streams 1, 2 are the two
  *     sample quantisations (row = sample index), 3 and 4 the model and gradient quantisations
- *     (row = step index within the epoch).  epoch must be < 2^24.
+ *     (row = step index within the epoch), 16 and up the stored activations.  epoch must be < 2^24.
  */
 #ifndef ZIPML_H
 #define ZIPML_H
@@ -273,6 +273,32 @@ int zipml_loss(void *stream, const float *A_dev, int64_t lda, const void *packed
                const float *levels_dev, int bits, const float *b_dev, const float *x_dev,
                int64_t n, int64_t d, double *loss_host, void *workspace_dev,
                size_t workspace_bytes);
+
+/* ---- layers whose activations are stored in 8 bits ------------------------------------------ */
+
+#define ZIPML_F32  0             /* element types of activations and gradients                     */
+#define ZIPML_BF16 1
+
+/* Bytes of a rows x cols tensor stored in 8 bits (33/32 of a byte a value, cols rounded up to a
+ * multiple of 32); 0 if the arguments are invalid.  Layout (public): codes, int8 [rows][padded], then one
+ * byte for each 32 columns of a row, [rows][padded / 32], the exponent e of the group's step 2^e plus 127.
+ * value = code * 2^e, which bf16 and fp32 hold exactly. */
+size_t zipml_act_bytes(int64_t rows, int64_t cols);
+
+/* Stores rows x cols values in 8 bits by stochastic rounding (Sec. 2.1's quantiser on evenly spaced
+ * levels, per 32 columns of a row): e is the least integer >= -126 with max |v| <= 127 * 2^e, code =
+ * floor(v * 2^-e + (k + 1/2) / 2^16), evaluated in fp32, k a 16-bit draw, so a decoded value is v in
+ * expectation (to 2^-17 of a step).  A group that holds an infinity or a NaN decodes to NaN throughout.
+ * x_dev: dtype ZIPML_F32 or ZIPML_BF16, row-major, ldx >= cols elements between rows (rows that are
+ * 16-byte aligned are read faster).  Draws: Philox as above with counter (row, col / 8, epoch * 256 + 16 +
+ * tag), output word (col % 8) / 2, its low half for even columns, its high half for odd ones; tag in 0..239
+ * tells the tensors of one step apart.  Asynchronous. */
+int zipml_act_encode(void *stream, const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t ldx,
+                     uint64_t seed, uint32_t epoch, int tag, void *act_dev);
+
+/* The values that act_dev stands for, in out_dev[rows][ldo], ldo >= cols.  Asynchronous. */
+int zipml_act_decode(void *stream, const void *act_dev, int64_t rows, int64_t cols, void *out_dev, int dtype,
+                     int64_t ldo);
 
 /* ---- parity / debug exports (not on the timed path) --------------------------------------- */
 

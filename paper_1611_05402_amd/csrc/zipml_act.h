@@ -1,0 +1,151 @@
+// Activations stored in 8 bits: the layout and the device code that writes and reads it.
+//
+// 32 columns of a row share a step 2^e, e the least integer >= -126 with max |v| <= 127 * 2^e; a value is kept as
+// floor(v * 2^-e + u), u uniform on the odd multiples of 2^-17 in (0, 1).  With a power of two as the step a
+// code times its step has at most 7 significant bits, so it is a bf16 (and fp32) number exactly: what reads the
+// codes may feed the bf16 matrix cores without rounding again.  Against a step of max / 127 this costs a step
+// up to twice as large, 1.5 bits of 255 levels at worst and about half a bit on average.
+#pragma once
+#include "zipml_device.h"
+#include "zipml_host.h"
+
+namespace zipml {
+
+constexpr int kActGroup = 32;    // columns that share a step
+constexpr int kActStream = 16;   // Philox stream of tag 0 (1 .. 4 are those of the quantisers)
+constexpr int kActMaxTag = 239;  // streams have 8 bits
+
+// Codes, int8 [rows][pitch], then the steps' biased exponents, uint8 [rows][pitch / 32]; pitch = cols rounded up to
+// 32.  The codes of the columns beyond cols are zeros.
+struct ActLayout {
+    int64_t rows, cols, pitch, groups;
+    int64_t steps;   // where the exponents start
+    size_t bytes() const { return (size_t)(steps + rows * groups); }
+};
+inline ActLayout act_layout(int64_t rows, int64_t cols)
+{
+    const int64_t pitch = round_up(cols, kActGroup);
+    return ActLayout{rows, cols, pitch, pitch / kActGroup, rows * pitch};
+}
+// Sizes whose byte offsets stay far below 2^63 (fp32 rows with any admissible stride).
+inline bool act_sizes_ok(int64_t rows, int64_t cols)
+{
+    return rows > 0 && cols > 0 && rows <= (1ll << 40) && cols <= (1ll << 31) - 64 && rows <= (1ll << 56) / cols;
+}
+inline bool valid_dtype(int dtype) { return dtype == ZIPML_F32 || dtype == ZIPML_BF16; }
+inline size_t dtype_bytes(int dtype) { return dtype == ZIPML_F32 ? 4 : 2; }
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float as_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ uint32_t as_u32(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+// ---- eight neighbouring values of a row, as fp32 ----------------------------------------------
+// `left` values of the eight exist, the others read as zero.  VEC: the rows are 16-byte aligned.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T *p, int64_t left, float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[2 * k] = as_f32(w[k] << 16);
+                v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
+            }
+        } else {
+            const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < left ? (float)p[k] : 0.0f;
+    }
+}
+// (rounded to T once, to the nearest)
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 o;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = (__bf16)v[k];
+            *reinterpret_cast<bf16x8 *>(p) = o;
+        } else {
+            reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < left) p[k] = (T)v[k];
+    }
+}
+
+// ---- storing ----------------------------------------------------------------------------------
+struct ActCodes8 {
+    u32x2 codes;
+    uint32_t byte;   // of the whole group
+};
+
+// Four neighbouring lanes, the first a multiple of four, hold the 32 values of a group, eight each (zeros beyond the
+// row's end).  All four have to be active.  One Philox block gives the eight draws, 16 bits each: the chance of the
+// upper neighbour is right to 2^-17 of a step, and half the multiplies of 24-bit draws are saved (the generator
+// is more than half of the kernel's instructions).
+__device__ __forceinline__ ActCodes8 act_encode8(const float (&v)[8], uint64_t seed, uint32_t epoch, int64_t row,
+                                                 uint32_t col8, uint32_t stream)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t m = as_u32(v[k]) & 0x7FFFFFFFu;      // as integers: finite < infinity < NaN
+        top = top > m ? top : m;
+    }
+    uint32_t o = dpp_move<0xB1>(top);
+    top = top > o ? top : o;
+    o = dpp_move<0x4E>(top);
+    top = top > o ? top : o;
+
+    // exponent of max minus 6, one more where its mantissa is above 127 / 64
+    int byte = (int)((top + 0x1FFFFu) >> 23) - 6;
+    byte = byte < 1 ? 1 : byte;
+    const bool finite = top < 0x7F800000u;
+    const float inverse = as_f32((uint32_t)(254 - byte) << 23);
+
+    const Philox4 r = philox_block(seed, epoch, (uint64_t)row, col8, stream);
+    uint32_t c[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t half = k & 1 ? r.w[k >> 1] >> 16 : r.w[k >> 1] & 0xFFFFu;
+        const float u = __builtin_fmaf((float)half, 1.0f / 65536.0f, 1.0f / 131072.0f);   // exact
+        // the product is exact, so the fused form rounds the sum as two operations would
+        const float t = __builtin_floorf(__builtin_fmaf(v[k], inverse, u));
+        c[k] = (uint32_t)(int)t;
+    }
+    ActCodes8 out;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const uint32_t lo = __builtin_amdgcn_perm(c[4 * q + 1], c[4 * q], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(c[4 * q + 3], c[4 * q + 2], 0x04000C0Cu);
+        out.codes[q] = finite ? lo | hi : 0u;
+    }
+    out.byte = finite ? (uint32_t)byte : 255u;
+    return out;
+}
+
+// ---- reading ----------------------------------------------------------------------------------
+// Step of a group.  Byte 255 gives infinity, and a code of 0 times it NaN.
+__device__ __forceinline__ float act_step(uint32_t byte) { return as_f32(byte << 23); }
+
+__device__ __forceinline__ void act_decode8(u32x2 codes, float step, float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (float)(int8_t)(codes[k >> 2] >> (8 * (k & 3))) * step;
+}
+
+}  // namespace zipml

@@ -19,6 +19,8 @@ SGD_STEPWISE, SGD_AVERAGED, SGD_PRODUCTION = 1, 2, 4
 STATIC_WORKSPACE_BYTES = 8 << 20
 PROX_NONE, PROX_L1, PROX_L2SQ, PROX_BOX = 0, 1, 2, 3
 
+F32, BF16 = 0, 1
+
 OK, EINVAL, EALIGN, ERANGE, EWORKSPACE, ELAUNCH, EUNSUPPORTED, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
 
 EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zipml_levels",
@@ -26,7 +28,8 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_compact_decode", "zipml_sgd_epoch", "zipml_sgd_epoch_l2",
            "zipml_sgd_epoch_prox", "zipml_sgd_epoch_avg", "zipml_sgd_epoch_static", "zipml_sgd_status",
            "zipml_loss", "zipml_debug_stream", "zipml_debug_set", "zipml_sgd_epoch_compact",
-           "zipml_unpack_codes", "zipml_debug_step"]
+           "zipml_unpack_codes", "zipml_debug_step", "zipml_act_bytes", "zipml_act_encode",
+           "zipml_act_decode"]
 
 
 class ZipmlError(RuntimeError):
@@ -100,6 +103,12 @@ def lib() -> C.CDLL:
         L.zipml_debug_set.argtypes = [i32, i64]
         L.zipml_unpack_codes.restype = i32
         L.zipml_unpack_codes.argtypes = [vp, vp, i32, i64, i64, i32, vp]
+        L.zipml_act_bytes.restype = sz
+        L.zipml_act_bytes.argtypes = [i64, i64]
+        L.zipml_act_encode.restype = i32
+        L.zipml_act_encode.argtypes = [vp, vp, i32, i64, i64, i64, u64, u32, i32, vp]
+        L.zipml_act_decode.restype = i32
+        L.zipml_act_decode.argtypes = [vp, vp, i64, i64, vp, i32, i64]
         _lib = L
     return _lib
 
@@ -276,3 +285,24 @@ def loss(b, x, n, d, workspace, *, A=None, lda=0, packed=None, copy=2, levels_t=
 def unpack_codes(packed, copy, n, d, bits, codes_out, stream=None):
     _check(lib().zipml_unpack_codes(_stream(stream), _ptr(packed), copy, n, d, bits,
                                     _ptr(codes_out)), "zipml_unpack_codes")
+
+
+def _dtype(t) -> int:
+    """ZIPML_F32 or ZIPML_BF16 for a tensor (or a torch dtype); the library refuses -1."""
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16}.get(t if isinstance(t, torch.dtype) else t.dtype, -1)
+
+
+def act_bytes(rows: int, cols: int) -> int:
+    return int(lib().zipml_act_bytes(rows, cols))
+
+
+def act_encode(x, rows, cols, ldx, seed, epoch, tag, act, stream=None):
+    """Stores x (fp32 or bf16) in 8 bits; `act`: act_bytes(rows, cols) bytes."""
+    _check(lib().zipml_act_encode(_stream(stream), _ptr(x), _dtype(x), rows, cols, ldx, seed, epoch, tag,
+                                  _ptr(act)), "zipml_act_encode")
+
+
+def act_decode(act, rows, cols, out, ldo, stream=None):
+    _check(lib().zipml_act_decode(_stream(stream), _ptr(act), rows, cols, _ptr(out), _dtype(out), ldo),
+           "zipml_act_decode")
