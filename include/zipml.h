@@ -300,6 +300,19 @@ int zipml_act_encode(void *stream, const void *x_dev, int dtype, int64_t rows, i
 int zipml_act_decode(void *stream, const void *act_dev, int64_t rows, int64_t cols, void *out_dev, int dtype,
                      int64_t ldo);
 
+/* Weight gradient of a linear layer Y = X W^T from its stored input:
+ *   dW[o][i] = sum_t dY[t][o] Q(X)[t][i],   or dW += that with ZIPML_WGRAD_ADD,
+ * the estimator of eq. (5) for a layer: unbiased, as Q's draws are independent of dY given X.  dY_dev: rows x d_out,
+ * lddy >= d_out; act_dev: rows x d_in as zipml_act_encode wrote it; dw_dev: fp32, d_out rows of d_in values, lddw >=
+ * d_in apart.  Products are exact (fp32 dY is taken as three bf16 terms), sums are in fp32, in an order that depends on
+ * the sizes alone: the same call gives the same bits.  A NaN group of X makes its columns of dW NaN.  d_out and d_in
+ * up to 2^24.  Asynchronous. */
+#define ZIPML_WGRAD_ADD 1
+size_t zipml_act_wgrad_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in, int dtype);
+int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int64_t lddy, const void *act_dev, int64_t rows,
+                    int64_t d_out, int64_t d_in, int flags, float *dw_dev, int64_t lddw, void *workspace_dev,
+                    size_t workspace_bytes);
+
 /* ---- parity / debug exports (not on the timed path) --------------------------------------- */
 
 /* Canonical codes of one packed copy (`copy` = 1 or 2): codes_dev[n][d], row-major uint8. */

@@ -20,6 +20,7 @@ STATIC_WORKSPACE_BYTES = 8 << 20
 PROX_NONE, PROX_L1, PROX_L2SQ, PROX_BOX = 0, 1, 2, 3
 
 F32, BF16 = 0, 1
+WGRAD_ADD = 1
 
 OK, EINVAL, EALIGN, ERANGE, EWORKSPACE, ELAUNCH, EUNSUPPORTED, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
 
@@ -29,7 +30,7 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_sgd_epoch_prox", "zipml_sgd_epoch_avg", "zipml_sgd_epoch_static", "zipml_sgd_status",
            "zipml_loss", "zipml_debug_stream", "zipml_debug_set", "zipml_sgd_epoch_compact",
            "zipml_unpack_codes", "zipml_debug_step", "zipml_act_bytes", "zipml_act_encode",
-           "zipml_act_decode"]
+           "zipml_act_decode", "zipml_act_wgrad_workspace_bytes", "zipml_act_wgrad"]
 
 
 class ZipmlError(RuntimeError):
@@ -109,6 +110,10 @@ def lib() -> C.CDLL:
         L.zipml_act_encode.argtypes = [vp, vp, i32, i64, i64, i64, u64, u32, i32, vp]
         L.zipml_act_decode.restype = i32
         L.zipml_act_decode.argtypes = [vp, vp, i64, i64, vp, i32, i64]
+        L.zipml_act_wgrad_workspace_bytes.restype = sz
+        L.zipml_act_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.zipml_act_wgrad.restype = i32
+        L.zipml_act_wgrad.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, i32, vp, i64, vp, sz]
         _lib = L
     return _lib
 
@@ -306,3 +311,15 @@ def act_encode(x, rows, cols, ldx, seed, epoch, tag, act, stream=None):
 def act_decode(act, rows, cols, out, ldo, stream=None):
     _check(lib().zipml_act_decode(_stream(stream), _ptr(act), rows, cols, _ptr(out), _dtype(out), ldo),
            "zipml_act_decode")
+
+
+def act_wgrad_workspace_bytes(rows: int, d_out: int, d_in: int, dtype) -> int:
+    """dtype: the torch type of dY."""
+    return int(lib().zipml_act_wgrad_workspace_bytes(rows, d_out, d_in, _dtype(dtype)))
+
+
+def act_wgrad(dy, lddy, act, rows, d_out, d_in, dw, lddw, workspace, *, flags=0, stream=None):
+    """dw = dy^T Q(X) (fp32) from the stored X; flags: WGRAD_ADD adds to dw."""
+    _check(lib().zipml_act_wgrad(_stream(stream), _ptr(dy), _dtype(dy), lddy, _ptr(act), rows, d_out, d_in, flags,
+                                 _ptr(dw), lddw, _ptr(workspace), workspace.numel() * workspace.element_size()),
+           "zipml_act_wgrad")
