@@ -313,6 +313,47 @@ int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int64_t lddy, c
                     int64_t d_out, int64_t d_in, int flags, float *dw_dev, int64_t lddw, void *workspace_dev,
                     size_t workspace_bytes);
 
+/* Gated linear recurrence over packed sequences:
+ *   f_t = sigmoid(z_t),  h_t = f_t h_{t-1} + (1 - f_t) x_t,  y_t = h_t,  channel by channel, states in fp32.
+ * x_dev, z_dev, y_dev: tokens x channels, dtype ZIPML_F32 or ZIPML_BF16, rows ld* >= channels apart (so x and z may be
+ * two halves of one projection).  seq_start_dev: n_seq + 1 ascending offsets; sequence s holds the tokens from
+ * seq_start[s] up to seq_start[s + 1], none if they are equal; NULL with n_seq = 1: all tokens are one sequence.
+ * Tokens in no sequence (before the first offset, from the last one on) give y = 0.  Offsets that do not ascend or lie
+ * outside the tokens give undefined results, but nothing outside the arrays is touched.
+ * h0_dev [n_seq][channels]: the states before the sequences, NULL for zeros.  h_last_dev [n_seq][channels], optional:
+ * the states after them (an empty sequence hands its h0 on).  A NaN or an infinity stays within its sequence and channel.
+ * For training, act_x_dev, act_z_dev (zipml_act_bytes(tokens, channels) bytes each) and states_dev
+ * ([ceil(tokens / ZIPML_SCAN_BLOCK)][channels], the state before each block of so many tokens) are written for
+ * zipml_scan_backward: x as zipml_act_encode stores it with `tag`, z clamped to [-16, 16] and stored with tag + 1
+ * (tag in 0..238).  For serving all three are NULL.  Asynchronous. */
+#define ZIPML_SCAN_BLOCK 256
+size_t zipml_scan_workspace_bytes(int64_t tokens, int64_t channels);
+int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,
+                       int64_t tokens, int64_t channels, const int64_t *seq_start_dev, int64_t n_seq,
+                       const float *h0_dev, void *y_dev, int64_t ldy, float *h_last_dev, void *act_x_dev,
+                       void *act_z_dev, float *states_dev, uint64_t seed, uint32_t epoch, int tag,
+                       void *workspace_dev, size_t workspace_bytes);
+
+/* Backward pass of zipml_scan_forward from its stored inputs Q(x), Q(z):
+ *   d_t = dy_t + f_{t+1} d_{t+1}  (a sequence's last token: dy_t + dh_last),
+ *   dx_t = (1 - f_t) d_t,  dz_t = d_t (h_{t-1} - Q(x_t)) f_t (1 - f_t),  dh0 = f d of its first token,
+ * with f = sigmoid(Q(z)) and the states formed again from Q(x), Q(z): from h0 at a sequence's start and from states_dev
+ * at the start of each block of ZIPML_SCAN_BLOCK tokens.  dy, dx, dz: dtype, any rows apart; dh_last_dev (NULL for zeros)
+ * and dh0_dev (optional): [n_seq][channels].  Tokens in no sequence give dx = dz = 0; an empty sequence's dh0 is its
+ * dh_last.  seq_start_dev, n_seq, h0_dev and the sizes as in the forward pass.  Asynchronous. */
+int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
+                        const void *dy_dev, int64_t lddy, int dtype, int64_t tokens, int64_t channels,
+                        const int64_t *seq_start_dev, int64_t n_seq, const float *h0_dev,
+                        const float *dh_last_dev, void *dx_dev, int64_t lddx, void *dz_dev, int64_t lddz,
+                        float *dh0_dev, void *workspace_dev, size_t workspace_bytes);
+
+/* One token of each of `rows` requests (serving): row r takes the state in row slots[r] of h_dev [n_slots][channels]
+ * (row r without slots_dev) one step on, in place, and y gets it.  A row whose slot is outside 0..n_slots - 1 belongs to no
+ * request: y = 0, no state is touched.  No two rows may name the same slot.  Asynchronous. */
+int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,
+                    int64_t rows, int64_t channels, float *h_dev, int64_t n_slots, const int32_t *slots_dev,
+                    void *y_dev, int64_t ldy);
+
 /* ---- parity / debug exports (not on the timed path) --------------------------------------- */
 
 /* Canonical codes of one packed copy (`copy` = 1 or 2): codes_dev[n][d], row-major uint8. */

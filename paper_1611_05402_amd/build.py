@@ -13,7 +13,7 @@ OUT = os.path.join(HERE, "libzipml.so")
 UNITS = [("zipml_sgd.hip", [f"-DZIPML_SGD_BITS={b}"], f"zipml_sgd_{b}.o") for b in (8, 4, 2, 7, 6, 5, 3, 1)]
 UNITS += [("zipml_sgd_solo.hip", [f"-DZIPML_SGD_BITS={b}"], f"zipml_sgd_solo_{b}.o") for b in range(1, 9)]
 UNITS += [(s, [], s.replace(".hip", ".o")) for s in ("zipml_sgd.hip", "zipml_quantize.hip", "zipml_loss.hip", "zipml_levels.hip",
-                                                         "zipml_act.hip", "zipml_wgrad.hip")]
+                                                         "zipml_act.hip", "zipml_wgrad.hip", "zipml_scan.hip")]
 
 # -ffp-contract=off: fp32/fp64 decision sequences must stay single IEEE operations (fused
 #   multiply-adds are written explicitly where they are wanted).

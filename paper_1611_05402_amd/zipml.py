@@ -21,6 +21,7 @@ PROX_NONE, PROX_L1, PROX_L2SQ, PROX_BOX = 0, 1, 2, 3
 
 F32, BF16 = 0, 1
 WGRAD_ADD = 1
+SCAN_BLOCK = 256
 
 OK, EINVAL, EALIGN, ERANGE, EWORKSPACE, ELAUNCH, EUNSUPPORTED, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
 
@@ -30,7 +31,8 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_sgd_epoch_prox", "zipml_sgd_epoch_avg", "zipml_sgd_epoch_static", "zipml_sgd_status",
            "zipml_loss", "zipml_debug_stream", "zipml_debug_set", "zipml_sgd_epoch_compact",
            "zipml_unpack_codes", "zipml_debug_step", "zipml_act_bytes", "zipml_act_encode",
-           "zipml_act_decode", "zipml_act_wgrad_workspace_bytes", "zipml_act_wgrad"]
+           "zipml_act_decode", "zipml_act_wgrad_workspace_bytes", "zipml_act_wgrad",
+           "zipml_scan_workspace_bytes", "zipml_scan_forward", "zipml_scan_backward", "zipml_scan_step"]
 
 
 class ZipmlError(RuntimeError):
@@ -114,6 +116,16 @@ def lib() -> C.CDLL:
         L.zipml_act_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.zipml_act_wgrad.restype = i32
         L.zipml_act_wgrad.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, i32, vp, i64, vp, sz]
+        L.zipml_scan_workspace_bytes.restype = sz
+        L.zipml_scan_workspace_bytes.argtypes = [i64, i64]
+        L.zipml_scan_forward.restype = i32
+        L.zipml_scan_forward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, i64, vp, vp, vp, vp, u64,
+                                         u32, i32, vp, sz]
+        L.zipml_scan_backward.restype = i32
+        L.zipml_scan_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp,
+                                          vp, sz]
+        L.zipml_scan_step.restype = i32
+        L.zipml_scan_step.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, i64]
         _lib = L
     return _lib
 
@@ -323,3 +335,35 @@ def act_wgrad(dy, lddy, act, rows, d_out, d_in, dw, lddw, workspace, *, flags=0,
     _check(lib().zipml_act_wgrad(_stream(stream), _ptr(dy), _dtype(dy), lddy, _ptr(act), rows, d_out, d_in, flags,
                                  _ptr(dw), lddw, _ptr(workspace), workspace.numel() * workspace.element_size()),
            "zipml_act_wgrad")
+
+
+def scan_workspace_bytes(tokens: int, channels: int) -> int:
+    return int(lib().zipml_scan_workspace_bytes(tokens, channels))
+
+
+def _same_dtype(*tensors) -> int:
+    """The common type of x, z and y (or of the gradients); -1, which the library refuses, if they differ."""
+    return _dtype(tensors[0]) if all(t.dtype == tensors[0].dtype for t in tensors) else -1
+
+
+def scan_forward(x, ldx, z, ldz, tokens, channels, y, ldy, workspace, *, seq_start=None, n_seq=1, h0=None, h_last=None,
+                 act_x=None, act_z=None, states=None, seed=0, epoch=0, tag=0, stream=None):
+    """The recurrence over packed sequences; with act_x, act_z and states, its inputs are stored for scan_backward."""
+    _check(lib().zipml_scan_forward(_stream(stream), _ptr(x), ldx, _ptr(z), ldz, _same_dtype(x, z, y), tokens, channels,
+                                    _ptr(seq_start), n_seq, _ptr(h0), _ptr(y), ldy, _ptr(h_last), _ptr(act_x),
+                                    _ptr(act_z), _ptr(states), seed, epoch, tag, _ptr(workspace),
+                                    workspace.numel() * workspace.element_size()), "zipml_scan_forward")
+
+
+def scan_backward(act_x, act_z, states, dy, lddy, tokens, channels, dx, lddx, dz, lddz, workspace, *, seq_start=None,
+                  n_seq=1, h0=None, dh_last=None, dh0=None, stream=None):
+    _check(lib().zipml_scan_backward(_stream(stream), _ptr(act_x), _ptr(act_z), _ptr(states), _ptr(dy), lddy,
+                                     _same_dtype(dy, dx, dz), tokens, channels, _ptr(seq_start), n_seq, _ptr(h0),
+                                     _ptr(dh_last), _ptr(dx), lddx, _ptr(dz), lddz, _ptr(dh0), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size()), "zipml_scan_backward")
+
+
+def scan_step(x, ldx, z, ldz, rows, channels, h, n_slots, y, ldy, *, slots=None, stream=None):
+    """One token of each request; `slots`: int32 rows of the states h [n_slots][channels], which are updated."""
+    _check(lib().zipml_scan_step(_stream(stream), _ptr(x), ldx, _ptr(z), ldz, _same_dtype(x, z, y), rows, channels,
+                                 _ptr(h), n_slots, _ptr(slots), _ptr(y), ldy), "zipml_scan_step")
