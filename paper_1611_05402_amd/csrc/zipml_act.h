@@ -44,20 +44,25 @@ __device__ __forceinline__ float as_f32(uint32_t u) { return __builtin_bit_cast(
 __device__ __forceinline__ uint32_t as_u32(float f) { return __builtin_bit_cast(uint32_t, f); }
 
 // ---- eight neighbouring values of a row, as fp32 ----------------------------------------------
-// `left` values of the eight exist, the others read as zero.  VEC: the rows are 16-byte aligned.
-template <typename T, bool VEC>
+// `left` values of the eight exist, the others read as zero.  Rows may start at any element: global memory is read 16
+// bytes at a time at any alignment (rows aligned to 16 bytes take fewer cycles, no other code).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+template <typename T>
 __device__ __forceinline__ void load8(const T *p, int64_t left, float (&v)[8])
 {
-    if (VEC && left >= 8) {
+    if (left >= 8) {
         if constexpr (sizeof(T) == 2) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+            const u32x4 w = *reinterpret_cast<const u32x4_any *>(p);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 v[2 * k] = as_f32(w[k] << 16);
                 v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
             }
         } else {
-            const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+            const f32x4 a = reinterpret_cast<const f32x4_any *>(p)[0], b = reinterpret_cast<const f32x4_any *>(p)[1];
 #pragma unroll
             for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
         }
@@ -67,18 +72,18 @@ __device__ __forceinline__ void load8(const T *p, int64_t left, float (&v)[8])
     }
 }
 // (rounded to T once, to the nearest)
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8])
 {
-    if (VEC && left >= 8) {
+    if (left >= 8) {
         if constexpr (sizeof(T) == 2) {
             bf16x8 o;
 #pragma unroll
             for (int k = 0; k < 8; ++k) o[k] = (__bf16)v[k];
-            *reinterpret_cast<bf16x8 *>(p) = o;
+            *reinterpret_cast<bf16x8_any *>(p) = o;
         } else {
-            reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-            reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+            reinterpret_cast<f32x4_any *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<f32x4_any *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
         }
     } else {
 #pragma unroll

@@ -13,7 +13,7 @@ struct ActGrid {
     int64_t col_blocks, row_blocks;
 };
 
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, ActLayout lay, int64_t ldx, ActGrid g,
                                                     uint64_t seed, uint32_t epoch, uint32_t stream,
                                                     uint8_t *__restrict__ act)
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, Act
 #pragma unroll
         for (int q = 0; q < kRows; ++q) {
             const int64_t row = row0 + q * ny;
-            load8<T, VEC>(x + row * ldx + unit * 8, row < lay.rows ? lay.cols - unit * 8 : 0, v[q]);
+            load8(x + row * ldx + unit * 8, row < lay.rows ? lay.cols - unit * 8 : 0, v[q]);
         }
 #pragma unroll
         for (int q = 0; q < kRows; ++q) {
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, Act
     }
 }
 
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_act_decode(const uint8_t *__restrict__ act, ActLayout lay, ActGrid g,
                                                     T *__restrict__ out, int64_t ldo)
 {
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_act_decode(const uint8_t *__restrict__ 
             if (row >= lay.rows) break;
             float v[8];
             act_decode8(c[q], act_step(byte[q]), v);
-            store8<T, VEC>(out + row * ldo + unit * 8, lay.cols - unit * 8, v);
+            store8(out + row * ldo + unit * 8, lay.cols - unit * 8, v);
         }
     }
 }
@@ -91,12 +91,7 @@ static int launch_encode(hipStream_t s, const T *x, const ActLayout &lay, int64_
                          uint32_t stream, uint8_t *act)
 {
     const ActGrid g = act_grid(lay.rows, lay.pitch / 8);
-    if (ldx * (int64_t)sizeof(T) % 16 == 0)
-        hipLaunchKernelGGL((k_act_encode<T, true>), dim3(act_blocks(g)), dim3(256), 0, s, x, lay, ldx, g, seed, epoch,
-                           stream, act);
-    else
-        hipLaunchKernelGGL((k_act_encode<T, false>), dim3(act_blocks(g)), dim3(256), 0, s, x, lay, ldx, g, seed, epoch,
-                           stream, act);
+    hipLaunchKernelGGL(k_act_encode<T>, dim3(act_blocks(g)), dim3(256), 0, s, x, lay, ldx, g, seed, epoch, stream, act);
     return hip_check(hipGetLastError());
 }
 
@@ -104,10 +99,7 @@ template <typename T>
 static int launch_decode(hipStream_t s, const uint8_t *act, const ActLayout &lay, T *out, int64_t ldo)
 {
     const ActGrid g = act_grid(lay.rows, lay.pitch / 8);
-    if (ldo * (int64_t)sizeof(T) % 16 == 0)
-        hipLaunchKernelGGL((k_act_decode<T, true>), dim3(act_blocks(g)), dim3(256), 0, s, act, lay, g, out, ldo);
-    else
-        hipLaunchKernelGGL((k_act_decode<T, false>), dim3(act_blocks(g)), dim3(256), 0, s, act, lay, g, out, ldo);
+    hipLaunchKernelGGL(k_act_decode<T>, dim3(act_blocks(g)), dim3(256), 0, s, act, lay, g, out, ldo);
     return hip_check(hipGetLastError());
 }
 

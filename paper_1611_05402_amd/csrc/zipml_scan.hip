@@ -152,7 +152,6 @@ __device__ __forceinline__ void block_scan(float (&A)[8], float (&B)[8], float2 
 }
 
 // What both passes of the forward direction need: the pair (a, b) of each of the thread's tokens.
-template <typename T, bool VEC>
 __device__ __forceinline__ void forward_tokens(const ScanArgs &p, const BlockMap &m, Range r, int64_t t0, int sub, int64_t c,
                                                const float (&x)[kRun][8], float (&a)[kRun][8], float (&b)[kRun][8])
 {
@@ -187,7 +186,7 @@ __device__ __forceinline__ void forward_tokens(const ScanArgs &p, const BlockMap
 }
 
 // APPLY = false: the pair of each block.  APPLY = true: states, from what enters the block.
-template <typename T, bool VEC, bool APPLY>
+template <typename T, bool APPLY>
 __global__ __launch_bounds__(kThreads, 2) void k_scan_forward(ScanArgs p)
 {
     __shared__ BlockMap map;
@@ -202,8 +201,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_forward(ScanArgs p)
     for (int j = 0; j < kRun; ++j) {
         const int64_t t = t0 + sub * kRun + j;
         const int64_t n = t < p.tokens ? left : 0;
-        load8<T, VEC>((const T *)p.x + t * p.ldx + c, n, x[j]);
-        load8<T, VEC>((const T *)p.z + t * p.ldz + c, n, a[j]);
+        load8((const T *)p.x + t * p.ldx + c, n, x[j]);
+        load8((const T *)p.z + t * p.ldz + c, n, a[j]);
     }
     if (APPLY && p.wx) {
 #pragma unroll
@@ -224,7 +223,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_forward(ScanArgs p)
             }
         }
     }
-    forward_tokens<T, VEC>(p, map, r, t0, sub, c, x, a, b);
+    forward_tokens(p, map, r, t0, sub, c, x, a, b);
 
     float A[8], B[8], tA[8], tB[8];
 #pragma unroll
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_forward(ScanArgs p)
             const int64_t t = t0 + sub * kRun + j;
 #pragma unroll
             for (int k = 0; k < 8; ++k) h[k] = join(a[j][k], h[k], b[j][k]);
-            if (t < p.tokens) store8<T, VEC>((T *)p.y + t * p.ldy + c, left, h);
+            if (t < p.tokens) store8((T *)p.y + t * p.ldy + c, left, h);
             if (p.h_last && map.some && map.last[sub * kRun + j] >= 0)
                 store_row(p.h_last + (int64_t)map.last[sub * kRun + j] * p.channels + c, left, h);
         }
@@ -283,7 +282,7 @@ __global__ __launch_bounds__(64) void k_scan_blocks(float2 *pairs, int64_t block
     }
 }
 
-template <typename T, bool VEC, bool APPLY>
+template <typename T, bool APPLY>
 __global__ __launch_bounds__(kThreads, 2) void k_scan_backward(ScanArgs p)
 {
     __shared__ BlockMap map;
@@ -307,7 +306,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_backward(ScanArgs p)
             qx[j] = there ? *reinterpret_cast<const u32x2 *>(p.rx + at) : u32x2{0, 0};
             ex[j] = there ? p.rx[step] : 0u;
         }
-        load8<T, VEC>((const T *)p.dy + t * p.lddy + c, t < p.tokens ? left : 0, d[j]);
+        load8((const T *)p.dy + t * p.lddy + c, t < p.tokens ? left : 0, d[j]);
     }
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
@@ -417,8 +416,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_backward(ScanArgs p)
                 h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[j][k] * x[k]);
             }
             if (t < p.tokens) {
-                store8<T, VEC>((T *)p.dx + t * p.lddx + c, left, dx);
-                store8<T, VEC>((T *)p.dz + t * p.lddz + c, left, dz);
+                store8((T *)p.dx + t * p.lddx + c, left, dx);
+                store8((T *)p.dz + t * p.lddz + c, left, dz);
             }
         }
         // empty sequences hand their gradients on
@@ -430,7 +429,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_scan_backward(ScanArgs p)
 }
 
 // One token of each of `rows` requests: the state in slot slots[row] (or row) of the pool is taken one step on.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int64_t ldx, const T *__restrict__ z, int64_t ldz,
                                                    int64_t rows, int64_t channels, float *h, int64_t n_slots,
                                                    const int32_t *__restrict__ slots, T *__restrict__ y, int64_t ldy)
@@ -442,8 +441,8 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
     float v[8] = {};
     if (slot >= 0 && slot < n_slots) {
         float xv[8], zv[8];
-        load8<T, VEC>(x + row * ldx + c, left, xv);
-        load8<T, VEC>(z + row * ldz + c, left, zv);
+        load8(x + row * ldx + c, left, xv);
+        load8(z + row * ldz + c, left, zv);
         float *s = h + slot * channels + c;
         load_row(s, left, v);
 #pragma unroll
@@ -454,7 +453,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
         }
         store_row(s, left, v);
     }
-    store8<T, VEC>(y + row * ldy + c, left, v);
+    store8(y + row * ldy + c, left, v);
 }
 
 static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
@@ -464,28 +463,28 @@ static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
-template <typename T, bool VEC>
+template <typename T>
 static int launch_forward(hipStream_t s, const ScanArgs &p)
 {
     const dim3 grid((uint32_t)(p.blocks * p.groups));
     if (p.blocks > 1) {
-        hipLaunchKernelGGL((k_scan_forward<T, VEC, false>), grid, dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((k_scan_forward<T, false>), grid, dim3(kThreads), 0, s, p);
         hipLaunchKernelGGL(k_scan_blocks<false>, dim3((uint32_t)((p.channels + 63) / 64)), dim3(64), 0, s, p.pairs, p.blocks,
                            p.channels);
     }
-    hipLaunchKernelGGL((k_scan_forward<T, VEC, true>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((k_scan_forward<T, true>), grid, dim3(kThreads), 0, s, p);
     return hip_check(hipGetLastError());
 }
-template <typename T, bool VEC>
+template <typename T>
 static int launch_backward(hipStream_t s, const ScanArgs &p)
 {
     const dim3 grid((uint32_t)(p.blocks * p.groups));
     if (p.blocks > 1) {
-        hipLaunchKernelGGL((k_scan_backward<T, VEC, false>), grid, dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((k_scan_backward<T, false>), grid, dim3(kThreads), 0, s, p);
         hipLaunchKernelGGL(k_scan_blocks<true>, dim3((uint32_t)((p.channels + 63) / 64)), dim3(64), 0, s, p.pairs, p.blocks,
                            p.channels);
     }
-    hipLaunchKernelGGL((k_scan_backward<T, VEC, true>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((k_scan_backward<T, true>), grid, dim3(kThreads), 0, s, p);
     return hip_check(hipGetLastError());
 }
 
@@ -529,10 +528,7 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    const int64_t es = (int64_t)dtype_bytes(dtype);
-    const bool vec = ldx * es % 16 == 0 && ldz * es % 16 == 0 && ldy * es % 16 == 0;
-    if (dtype == ZIPML_F32) return vec ? launch_forward<float, true>(s, p) : launch_forward<float, false>(s, p);
-    return vec ? launch_forward<__bf16, true>(s, p) : launch_forward<__bf16, false>(s, p);
+    return dtype == ZIPML_F32 ? launch_forward<float>(s, p) : launch_forward<__bf16>(s, p);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -563,19 +559,15 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    const int64_t es = (int64_t)dtype_bytes(dtype);
-    const bool vec = lddy * es % 16 == 0 && lddx * es % 16 == 0 && lddz * es % 16 == 0;
-    if (dtype == ZIPML_F32) return vec ? launch_backward<float, true>(s, p) : launch_backward<float, false>(s, p);
-    return vec ? launch_backward<__bf16, true>(s, p) : launch_backward<__bf16, false>(s, p);
+    return dtype == ZIPML_F32 ? launch_backward<float>(s, p) : launch_backward<__bf16>(s, p);
 }
 
 template <typename T>
 static int launch_step(hipStream_t s, const void *x, int64_t ldx, const void *z, int64_t ldz, int64_t rows, int64_t channels,
                        float *h, int64_t n_slots, const int32_t *slots, void *y, int64_t ldy)
 {
-    const int64_t es = sizeof(T), blocks = (rows * ((channels + 7) / 8) + 255) / 256;
-    auto k = ldx * es % 16 == 0 && ldz * es % 16 == 0 && ldy * es % 16 == 0 ? k_scan_step<T, true> : k_scan_step<T, false>;
-    hipLaunchKernelGGL(k, dim3((uint32_t)blocks), dim3(256), 0, s, (const T *)x, ldx, (const T *)z, ldz, rows, channels, h,
+    const int64_t blocks = (rows * ((channels + 7) / 8) + 255) / 256;
+    hipLaunchKernelGGL(k_scan_step<T>, dim3((uint32_t)blocks), dim3(256), 0, s, (const T *)x, ldx, (const T *)z, ldz, rows, channels, h,
                        n_slots, slots, (T *)y, ldy);
     return hip_check(hipGetLastError());
 }

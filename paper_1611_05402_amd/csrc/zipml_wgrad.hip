@@ -25,23 +25,25 @@ struct WgradArgs {
     int d_out, d_in, tiles_o, tiles_i, add;
 };
 
-// MT x NT is the tile of dW, BK the tokens of one step; WM x WN waves share the tile.
+// MT x NT is the tile of dW, BK the tokens of one round; WM x WN waves share the tile.
 template <typename T, int MT_, int NT_, int BK_, int WM_, int WN_>
 struct WgradShape {
     static constexpr int MT = MT_, NT = NT_, BK = BK_, WM = WM_, WN = WN_;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;        // bf16 terms of a dY value
-    // LDS rows of 64 bytes more than a multiple of 256: the four rows that 16 lanes of a transposing read touch, and
+    // LDS rows of 64 or 192 bytes more than a multiple of 256: the four rows that 16 lanes of a transposing read touch, and
     // the 64 bytes that the neighbouring 16 lanes add to each, then fall on all banks once.
     static constexpr int kRowA = MT * 2 + 64, kRowB = NT * 2 + 64;
     static constexpr int kBytesA = BK * kRowA, kBytesB = BK * kRowB;
     static constexpr int kStage = kPlanes * kBytesA + kBytesB;
     static constexpr int kLoadsA = BK * MT / 8 / kThreads;        // eight dY values each
-    static constexpr int kLoadsB = BK * NT / 16 / kThreads;       // sixteen codes each
+    static constexpr int kLoadsB = BK * NT / 8 / kThreads;        // eight codes each
+    static constexpr int kSteps = BK / 16 * kPlanes;              // steps of a product: sixteen tokens, one term
     static constexpr int TM = MT / WM / 32, TN = NT / WN / 32;    // 32 x 32 tiles of a wave
-    static_assert(kLoadsA * 8 * kThreads == BK * MT && kLoadsB * 16 * kThreads == BK * NT, "whole loads");
-    static_assert(MT % 128 == 0 && NT % 128 == 0, "LDS rows");
+    static_assert(kLoadsA * 8 * kThreads == BK * MT && kLoadsB * 8 * kThreads == BK * NT, "whole loads");
+    static_assert(MT % 64 == 0 && NT % 64 == 0, "LDS rows");
     static_assert(2 * kStage <= 160 * 1024, "LDS");
+    static_assert(kSteps % 2 == 0 && BK / 16 % 2 == 0, "operands of the steps by turns");
 };
 
 // Four tokens of one column of an LDS tile, transposed (see the file's head).
@@ -57,92 +59,142 @@ __device__ __forceinline__ bf16x8 fragment(const char *tile, int row_bytes)
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Eight dY values as bf16 terms; the first takes the upper 8 bits of the mantissa by truncation, so that it never
-// overflows, the second those of the rest, the third what is left (an infinity or a NaN has only the first).
-template <typename T>
-__device__ __forceinline__ void split8(const float (&v)[8], u32x4 (&plane)[sizeof(T) == 4 ? 3 : 1])
+// Rows of a tile as a buffer: what lies behind its last value reads as zeros, so that neither the last tokens of a range
+// nor tiles beyond the layer's edge need a branch.  (A column beyond the edge reads the next row's values where there
+// is one: they reach only sums that are not kept.)
+struct Rows {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Rows(const void *base, int64_t bytes)
+    {
+        const int n = bytes < 0 ? 0 : bytes > 0x7FFFFFFF ? 0x7FFFFFFF : (int)bytes;
+        r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, n, 0x00020000);
+    }
+    __device__ __forceinline__ u32x4 load16(int at) const { return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0); }
+    __device__ __forceinline__ u32x2 load8(int at) const { return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0); }
+    __device__ __forceinline__ uint32_t load1(int at) const { return __builtin_amdgcn_raw_buffer_load_b8(r, at, 0, 0); }
+};
+
+// Eight dY values as they lie in memory.
+template <typename T> struct Raw8;
+template <> struct Raw8<__bf16> { u32x4 w; };
+template <> struct Raw8<float> { u32x4 w, w2; };
+
+// Four fp32 values as three bf16 terms each; the first takes the upper 8 bits of the mantissa by truncation, so that it
+// never overflows, the second those of the rest, the third what is left (an infinity or a NaN has only the first).
+__device__ __forceinline__ void split4(u32x4 v, uint32_t (&plane)[3][2])
 {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
         uint32_t hi[2], mid[2], lo[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float x = v[2 * k + h];
-            const uint32_t bits = as_u32(x);
-            if constexpr (sizeof(T) == 2) {
-                hi[h] = bits;
-            } else {
-                const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
-                hi[h] = x != x ? 0x7FC00000u : bits & 0xFFFF0000u;
-                const float r = finite ? x - as_f32(hi[h]) : 0.0f;
-                mid[h] = as_u32(r) & 0xFFFF0000u;
-                lo[h] = as_u32(r - as_f32(mid[h]));
-            }
+            const float x = as_f32(v[2 * k + h]);
+            const uint32_t bits = v[2 * k + h];
+            const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+            hi[h] = x != x ? 0x7FC00000u : bits & 0xFFFF0000u;
+            const float r = finite ? x - as_f32(hi[h]) : 0.0f;
+            mid[h] = as_u32(r) & 0xFFFF0000u;
+            lo[h] = as_u32(r - as_f32(mid[h]));
         }
         plane[0][k] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);
-        if constexpr (sizeof(T) == 4) {
-            plane[1][k] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
-            plane[2][k] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
-        }
+        plane[1][k] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
+        plane[2][k] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
     }
 }
 
-template <typename T, typename S, bool VEC>
+// Workgroups go to the eight XCDs in turn; each XCD gets a run of neighbouring ones: all tiles of a range of tokens
+// before those of the next, tiles in bands four deep, so that its L2 serves rows of dY and codes to several of them.
+__device__ __forceinline__ void place_of(const WgradArgs &a, int &split, int &o, int &i)
+{
+    const uint32_t n = gridDim.x, xcd = blockIdx.x & 7, per = n >> 3, more = n & 7;
+    const uint32_t id = xcd * per + (xcd < more ? xcd : more) + (blockIdx.x >> 3), tiles = a.tiles_o * a.tiles_i;
+    split = id / tiles;
+    const uint32_t tile = id - split * tiles, band = tile / (4 * a.tiles_i), in = tile - band * 4 * a.tiles_i;
+    const uint32_t deep = a.tiles_o - band * 4 < 4 ? a.tiles_o - band * 4 : 4;
+    o = band * 4 + in % deep;
+    i = in / deep;
+}
+
+// WIDE: rows of dY are read 16 bytes at a time; otherwise value by value.
+template <typename T, typename S, bool WIDE>
 __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int tiles = a.tiles_o * a.tiles_i;
-    const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
-    const int o0 = tile / a.tiles_i * S::MT, i0 = tile % a.tiles_i * S::NT;
+    int split, o0, i0;
+    place_of(a, split, o0, i0);
+    o0 *= S::MT;
+    i0 *= S::NT;
     const int64_t t_begin = split * a.rows_split;
     const int64_t t_end = t_begin + a.rows_split < a.rows ? t_begin + a.rows_split : a.rows;
     const T *dy = (const T *)a.dy;
 
-    float va[S::kLoadsA][8];
-    u32x4 vb[S::kLoadsB];
+    Raw8<T> va[S::kLoadsA];
+    u32x2 vb[S::kLoadsB];
     uint32_t step[S::kLoadsB];
 
-    auto load = [&](int64_t t0) {
+    // The loads and the stores of a tile are dealt over the steps of a round but the last.
+    constexpr int kDeals = S::kSteps - 1;
+    auto load = [&](int64_t t0, int k) {
+        const int64_t left = t_end - t0;
+        const Rows ra(dy + t0 * a.lddy + o0, WIDE ? ((left - 1) * a.lddy + a.d_out - o0) * (int64_t)sizeof(T) : 0);
+        const Rows rb(a.act + t0 * a.pitch + i0, left * a.pitch - i0);
+        const Rows rs(a.act + a.steps + t0 * a.groups + (i0 >> 5), left * a.groups - (i0 >> 5));
 #pragma unroll
         for (int q = 0; q < S::kLoadsA; ++q) {
-            const int c = tid + q * S::kThreads, r = c / (S::MT / 8), col = o0 + c % (S::MT / 8) * 8;
-            const int64_t t = t0 + r;
-            load8<T, VEC>(dy + t * a.lddy + col, t < t_end ? a.d_out - col : 0, va[q]);
+            if (q * kDeals / S::kLoadsA != k) continue;
+            const int c = tid + q * S::kThreads, r = c / (S::MT / 8), col = c % (S::MT / 8) * 8;
+            if constexpr (WIDE) {
+                const int at = (r * (int)a.lddy + col) * (int)sizeof(T);
+                va[q].w = ra.load16(at);
+                if constexpr (sizeof(T) == 4) va[q].w2 = ra.load16(at + 16);
+            } else {
+                const T *p = dy + (t0 + r) * a.lddy + o0 + col;
+                const int n = r < left ? a.d_out - o0 - col : 0;
+                T v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (T)0.0f;
+                va[q] = __builtin_bit_cast(Raw8<T>, v);
+            }
         }
 #pragma unroll
         for (int q = 0; q < S::kLoadsB; ++q) {
-            const int c = tid + q * S::kThreads, r = c / (S::NT / 16), col = i0 + c % (S::NT / 16) * 16;
-            const int64_t t = t0 + r;
-            const bool there = t < t_end && col < a.pitch;      // the pitch is a multiple of 32
-            vb[q] = there ? *reinterpret_cast<const u32x4 *>(a.act + t * a.pitch + col) : u32x4{0, 0, 0, 0};
-            step[q] = there ? a.act[a.steps + t * a.groups + (col >> 5)] : 0u;
+            if (q * kDeals / S::kLoadsB != k) continue;
+            const int c = tid + q * S::kThreads, r = c / (S::NT / 8), col = c % (S::NT / 8) * 8;
+            vb[q] = rb.load8(r * (int)a.pitch + col);
+            step[q] = rs.load1(r * (int)a.groups + (col >> 5));
         }
     };
-    auto store = [&](char *stage) {
+    auto store = [&](char *stage, int k) {
 #pragma unroll
         for (int q = 0; q < S::kLoadsA; ++q) {
+            if (q * kDeals / S::kLoadsA != k) continue;
             const int c = tid + q * S::kThreads, r = c / (S::MT / 8), col = c % (S::MT / 8) * 8;
-            u32x4 plane[S::kPlanes];
-            split8<T>(va[q], plane);
+            char *p = stage + r * S::kRowA + col * 2;
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<u32x4 *>(p) = va[q].w;
+            } else {
+                uint32_t x[3][2], y[3][2];
+                split4(va[q].w, x);
+                split4(va[q].w2, y);
 #pragma unroll
-            for (int p = 0; p < S::kPlanes; ++p)
-                *reinterpret_cast<u32x4 *>(stage + p * S::kBytesA + r * S::kRowA + col * 2) = plane[p];
+                for (int t = 0; t < 3; ++t)
+                    *reinterpret_cast<u32x4 *>(p + t * S::kBytesA) = u32x4{x[t][0], x[t][1], y[t][0], y[t][1]};
+            }
         }
 #pragma unroll
         for (int q = 0; q < S::kLoadsB; ++q) {
-            const int c = tid + q * S::kThreads, r = c / (S::NT / 16), col = c % (S::NT / 16) * 16;
+            if (q * kDeals / S::kLoadsB != k) continue;
+            const int c = tid + q * S::kThreads, r = c / (S::NT / 8), col = c % (S::NT / 8) * 8;
             const float s = act_step(step[q]);
-            u32x4 o[2];
+            u32x4 o;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t w = vb[q][k >> 1];
-                const float x = (float)(int8_t)(w >> (16 * (k & 1))) * s, y = (float)(int8_t)(w >> (16 * (k & 1) + 8)) * s;
-                o[k >> 2][k & 3] = __builtin_amdgcn_perm(as_u32(y), as_u32(x), 0x07060302u);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = vb[q][j >> 1];
+                const float x = (float)(int8_t)(w >> (16 * (j & 1))) * s, y = (float)(int8_t)(w >> (16 * (j & 1) + 8)) * s;
+                o[j] = __builtin_amdgcn_perm(as_u32(y), as_u32(x), 0x07060302u);
             }
-            u32x4 *p = reinterpret_cast<u32x4 *>(stage + S::kPlanes * S::kBytesA + r * S::kRowB + col * 2);
-            p[0] = o[0];
-            p[1] = o[1];
+            *reinterpret_cast<u32x4 *>(stage + S::kPlanes * S::kBytesA + r * S::kRowB + col * 2) = o;
         }
     };
 
@@ -153,34 +205,53 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
     const int off_b = tr_row * S::kRowB + (wn * S::TN * 32 + tr_col) * 2 + S::kPlanes * S::kBytesA;
     f32x16 acc[S::TM][S::TN] = {};
 
-    if (t_begin < t_end) {
-        load(t_begin);
-        store(lds);
-        __syncthreads();
-        int cur = 0;
-        for (int64_t t0 = t_begin; t0 < t_end; t0 += S::BK) {
-            const bool more = t0 + S::BK < t_end;
-            if (more) load(t0 + S::BK);
-            const char *stage = lds + cur * S::kStage;
+    bf16x8 fa[2][S::TM], fb[2][S::TN];
+    auto read = [&](const char *stage, int s) {
+        const int k = s / S::kPlanes, p = s % S::kPlanes;
 #pragma unroll
-            for (int k = 0; k < S::BK / 16; ++k) {
-                bf16x8 fb[S::TN];
+        for (int m = 0; m < S::TM; ++m)
+            fa[s & 1][m] = fragment(stage + off_a + p * S::kBytesA + k * 16 * S::kRowA + m * 64, S::kRowA);
+        if (p == 0)
 #pragma unroll
-                for (int n = 0; n < S::TN; ++n) fb[n] = fragment(stage + off_b + k * 16 * S::kRowB + n * 64, S::kRowB);
+            for (int n = 0; n < S::TN; ++n) fb[k & 1][n] = fragment(stage + off_b + k * 16 * S::kRowB + n * 64, S::kRowB);
+    };
+
+    // While the tile of these tokens is multiplied, the next one goes from registers to LDS, and each register is loaded
+    // anew for the one after it as soon as it is free.  The operands of a step are read during the step before; the
+    // barrier stands before a round's last step, whose own are in registers by then.  The steps are kept apart, since the
+    // compiler otherwise moves all loads to a round's end, where their latency shows (555 us in place of 460 for 16,384
+    // tokens, 4,096 x 4,096, in the same arrangement).
+    char *here = lds, *next = lds + S::kStage;
 #pragma unroll
-                for (int p = 0; p < S::kPlanes; ++p)
+    for (int k = 0; k < kDeals; ++k) load(t_begin, k);
 #pragma unroll
-                    for (int m = 0; m < S::TM; ++m) {
-                        const bf16x8 fa = fragment(stage + off_a + p * S::kBytesA + k * 16 * S::kRowA + m * 64, S::kRowA);
+    for (int k = 0; k < kDeals; ++k) {
+        store(here, k);
+        load(t_begin + S::BK, k);
+    }
+    lds_barrier();
+    read(here, 0);
+    for (int64_t t0 = t_begin; t0 < t_end; t0 += S::BK) {
 #pragma unroll
-                        for (int n = 0; n < S::TN; ++n)
-                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[n], acc[m][n], 0, 0, 0);
-                    }
+        for (int s = 0; s < S::kSteps; ++s) {
+            if (s < kDeals) {
+                read(here, s + 1);
+                store(next, s);
+                load(t0 + 2 * S::BK, s);
+            } else {
+                lds_barrier();
+                read(next, 0);
             }
-            cur ^= 1;
-            if (more) store(lds + cur * S::kStage);
-            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < S::TM; ++m)
+#pragma unroll
+                for (int n = 0; n < S::TN; ++n)
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][m], fb[s / S::kPlanes & 1][n], acc[m][n], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        char *const t = here;
+        here = next;
+        next = t;
     }
 
     float *out = a.out + split * a.out_split;
@@ -200,49 +271,87 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         }
 }
 
-// Sum of the ranges' partial sums, in their order.
+// Sum of the ranges' partial sums, in their order; a thread takes four neighbouring elements, the partial sums' rows being
+// multiples of 64.
 __global__ __launch_bounds__(256) void k_wgrad_sum(const float *__restrict__ part, int splits, int64_t out_split, int d_out,
                                                    int d_in, int64_t ld_part, float *__restrict__ dw, int64_t lddw, int add)
 {
-    const int i = (blockIdx.x % ((d_in + 255) / 256)) * 256 + threadIdx.x, o = blockIdx.x / ((d_in + 255) / 256);
-    if (i >= d_in || o >= d_out) return;
+    const uint32_t units = (d_in + 3) / 4, u = blockIdx.x * 256u + threadIdx.x, o = u / units, i = (u - o * units) * 4;
+    if (o >= (uint32_t)d_out) return;
     const float *p = part + o * ld_part + i;
-    float sum = 0.0f;
-    for (int s = 0; s < splits; ++s) sum += p[s * out_split];
+    f32x4 sum = {};
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * out_split);
     float *w = dw + o * lddw + i;
-    *w = add ? *w + sum : sum;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if ((int)i + k < d_in) w[k] = add ? w[k] + sum[k] : sum[k];
 }
 
+// The shapes.  256 x 256: per value of an operand the most products, one workgroup a compute unit; the smaller ones fill
+// the machine where dW is small, two or more workgroups to a compute unit.
+template <typename T> struct Shapes {
+    static constexpr int BK = sizeof(T) == 4 ? 32 : 64;
+    typedef WgradShape<T, 256, 256, BK, 2, 4> Large;
+    typedef WgradShape<T, 128, 128, BK, 2, 4> Middle;
+    typedef WgradShape<T, 64, 64, BK, 2, 2> Small;
+};
+
+// Which shape, and in how many ranges the tokens are taken (whose partial sums a second launch joins): the least of
+//   start + rounds of a range * (one workgroup on a compute unit: lone, k of them: k * shared)
+//         + (ranges > 1: a launch, partial sums written and read),
+// with the times of a round measured on either side of each choice (us; 64 tokens of bf16 or 32 of fp32 dY):
+//   256: 1.4 to 1.8, fp32 2.6;  128: 0.68 to 0.85 alone, 0.65 each of two, fp32 1.0;  64: 0.5 alone, 0.37 each, fp32 0.65.
+// 4,096 tokens, 2,048 x 2,048, launches alone: 256 in 4 ranges 43 us + 67 MB of partial sums, 128 in one 53; 4,096 tokens,
+// 1,024 x 1,024: 256 in 16 ranges 23, 128 in 4 22, 64 in one 36; 256 tokens, 256 x 256: 128 in one 12, 64 in one 8.
 struct WgradPlan {
     int tile, splits, tiles_o, tiles_i;
     int64_t rows_split;
     size_t workspace() const { return splits > 1 ? (size_t)splits * tiles_o * tiles_i * tile * tile * 4 : 0; }
 };
-static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in)
+static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype)
 {
-    WgradPlan p;
-    auto tiles = [&](int t) { return ((d_out + t - 1) / t) * ((d_in + t - 1) / t); };
-    p.tile = tiles(256) >= 128 ? 256 : 128;
-    p.tiles_o = (int)((d_out + p.tile - 1) / p.tile);
-    p.tiles_i = (int)((d_in + p.tile - 1) / p.tile);
-    const int64_t n = tiles(p.tile);
-    int64_t s = p.tile == 256 ? 1 : 256 / n;
-    const int64_t most = (rows + 127) / 128;
-    s = s < 1 ? 1 : s > most ? most : s;
-    p.rows_split = round_up((rows + s - 1) / s, 64);
-    p.splits = (int)((rows + p.rows_split - 1) / p.rows_split);
-    return p;
+    struct { int tile; double lone, shared; } const shapes[2][3] = {{{256, 1.6, 1.6}, {128, 0.8, 0.65}, {64, 0.5, 0.37}},
+                                                                    {{256, 2.6, 2.6}, {128, 1.0, 0.95}, {64, 0.65, 0.55}}};
+    const int64_t round = dtype == ZIPML_F32 ? 32 : 64;
+    WgradPlan best{};
+    double least = 0;
+    for (const auto &c : shapes[dtype == ZIPML_F32]) {
+        const int64_t to = (d_out + c.tile - 1) / c.tile, ti = (d_in + c.tile - 1) / c.tile;
+        for (int64_t s = 1; s <= 256 && (s == 1 || (s - 1) * 128 < rows); s *= 2) {
+            const int64_t rows_split = round_up((rows + s - 1) / s, 64), splits = (rows + rows_split - 1) / rows_split;
+            const double k = (double)((to * ti * splits + 255) / 256), rounds = (double)((rows_split + round - 1) / round);
+            const double us = 5.0 + rounds * (k > 1 ? k * c.shared : c.lone) +
+                              (splits > 1 ? 4.0 + (double)splits * to * ti * c.tile * c.tile * 8.0 / 4.5e6 : 0.0);
+            if (best.tile == 0 || us < least) {
+                least = us;
+                best = WgradPlan{c.tile, (int)splits, (int)to, (int)ti, rows_split};
+            }
+        }
+    }
+    return best;
 }
 
 template <typename T, typename S>
 static int launch_wgrad(hipStream_t s, const WgradArgs &a, int splits)
 {
-    const bool vec = a.lddy * (int64_t)sizeof(T) % 16 == 0;
-    auto k = vec ? k_act_wgrad<T, S, true> : k_act_wgrad<T, S, false>;
+    // 16 bytes at a time where rows start and end on whole dwords (a buffer's end is exact to a dword) and the offsets of a
+    // round fit 31 bits
+    const int64_t es = sizeof(T);
+    const bool wide = a.lddy * es % 4 == 0 && a.d_out * es % 4 == 0 && a.lddy * es < (1 << 24);
+    auto k = wide ? k_act_wgrad<T, S, true> : k_act_wgrad<T, S, false>;
     if (HIP_FAILED(hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * S::kStage)))
         return ZIPML_ELAUNCH;
     hipLaunchKernelGGL(k, dim3(a.tiles_o * a.tiles_i * splits), dim3(S::kThreads), 2 * S::kStage, s, a);
     return hip_check(hipGetLastError());
+}
+
+template <typename T>
+static int launch_tile(hipStream_t s, const WgradArgs &a, const WgradPlan &p)
+{
+    if (p.tile == 256) return launch_wgrad<T, typename Shapes<T>::Large>(s, a, p.splits);
+    if (p.tile == 128) return launch_wgrad<T, typename Shapes<T>::Middle>(s, a, p.splits);
+    return launch_wgrad<T, typename Shapes<T>::Small>(s, a, p.splits);
 }
 
 }  // namespace zipml
@@ -252,13 +361,13 @@ using namespace zipml;
 static bool wgrad_sizes_ok(int64_t rows, int64_t d_out, int64_t d_in)
 {
     return act_sizes_ok(rows, d_in) && d_out > 0 && d_out <= (1 << 24) && d_in <= (1 << 24) &&
-           ((d_out + 127) / 128) * ((d_in + 127) / 128) <= (1ll << 30);
+           ((d_out + 63) / 64) * ((d_in + 63) / 64) <= (1ll << 30);
 }
 
 extern "C" size_t zipml_act_wgrad_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in, int dtype)
 {
     if (!wgrad_sizes_ok(rows, d_out, d_in) || !valid_dtype(dtype)) return 0;
-    const size_t b = wgrad_plan(rows, d_out, d_in).workspace();
+    const size_t b = wgrad_plan(rows, d_out, d_in, dtype).workspace();
     return b < 256 ? 256 : b;
 }
 
@@ -273,7 +382,7 @@ extern "C" int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int6
         return ZIPML_EWORKSPACE;
     if (!aligned16(dy_dev) || !aligned16(act_dev) || !aligned16(dw_dev) || !aligned16(workspace_dev)) return ZIPML_EALIGN;
     const ActLayout lay = act_layout(rows, d_in);
-    const WgradPlan p = wgrad_plan(rows, d_out, d_in);
+    const WgradPlan p = wgrad_plan(rows, d_out, d_in, dtype);
     hipStream_t s = entry_stream(stream);
     const int add = flags & ZIPML_WGRAD_ADD ? 1 : 0;
     WgradArgs a{dy_dev, (const uint8_t *)act_dev, dw_dev, lddy, rows, lay.pitch, lay.groups, lay.steps, lddw, 0,
@@ -284,15 +393,9 @@ extern "C" int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int6
         a.out_split = a.ldo * p.tiles_o * p.tile;
         a.add = 0;
     }
-    int rc;
-    if (dtype == ZIPML_BF16)
-        rc = p.tile == 256 ? launch_wgrad<__bf16, WgradShape<__bf16, 256, 256, 64, 2, 2>>(s, a, p.splits)
-                           : launch_wgrad<__bf16, WgradShape<__bf16, 128, 128, 64, 2, 2>>(s, a, p.splits);
-    else
-        rc = p.tile == 256 ? launch_wgrad<float, WgradShape<float, 256, 256, 32, 2, 2>>(s, a, p.splits)
-                           : launch_wgrad<float, WgradShape<float, 128, 128, 32, 2, 2>>(s, a, p.splits);
+    const int rc = dtype == ZIPML_F32 ? launch_tile<float>(s, a, p) : launch_tile<__bf16>(s, a, p);
     if (rc || p.splits == 1) return rc;
-    const int64_t blocks = (d_in + 255) / 256 * d_out;
+    const int64_t blocks = ((d_in + 3) / 4 * d_out + 255) / 256;
     hipLaunchKernelGGL(k_wgrad_sum, dim3((uint32_t)blocks), dim3(256), 0, s, a.out, p.splits, a.out_split, (int)d_out,
                        (int)d_in, a.ldo, dw_dev, lddw, add);
     return hip_check(hipGetLastError());
