@@ -93,6 +93,32 @@ __device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8])
 }
 
 // ---- storing ----------------------------------------------------------------------------------
+struct ActStep {
+    uint32_t byte;     // biased exponent of the step, 255 for a group that is not finite
+    float inverse;     // 1 / step
+    bool finite;
+};
+// From the largest magnitude of a group, as the bits of an fp32 number (as integers: finite < infinity < NaN): the exponent of
+// max minus 6, one more where its mantissa is above 127 / 64.
+__device__ __forceinline__ ActStep act_step_of(uint32_t top)
+{
+    int byte = (int)((top + 0x1FFFFu) >> 23) - 6;
+    byte = byte < 1 ? 1 : byte;
+    const bool finite = top < 0x7F800000u;
+    return ActStep{finite ? (uint32_t)byte : 255u, as_f32((uint32_t)(254 - byte) << 23), finite};
+}
+// The code of a value from its 16-bit draw, in the low byte.  (k + 1/2) / 2^16 is exact, and so is the product, so that the
+// fused form rounds the sum as two operations would.
+__device__ __forceinline__ uint32_t act_code(float v, float inverse, uint32_t draw)
+{
+    const float u = __builtin_fmaf((float)draw, 1.0f / 65536.0f, 1.0f / 131072.0f);
+    return (uint32_t)(int)__builtin_floorf(__builtin_fmaf(v, inverse, u));
+}
+__device__ __forceinline__ uint32_t act_pack4(const uint32_t (&c)[4])
+{
+    return __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000C0Cu);
+}
+
 struct ActCodes8 {
     u32x2 codes;
     uint32_t byte;   // of the whole group
@@ -100,46 +126,34 @@ struct ActCodes8 {
 
 // Four neighbouring lanes, the first a multiple of four, hold the 32 values of a group, eight each (zeros beyond the
 // row's end).  All four have to be active.  One Philox block gives the eight draws, 16 bits each: the chance of the
-// upper neighbour is right to 2^-17 of a step, and half the multiplies of 24-bit draws are saved (the generator
-// is more than half of the kernel's instructions).
+// upper neighbour is right to 2^-17 of a step, and half the multiplies of 24-bit draws are saved.
 __device__ __forceinline__ ActCodes8 act_encode8(const float (&v)[8], uint64_t seed, uint32_t epoch, int64_t row,
                                                  uint32_t col8, uint32_t stream)
 {
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint32_t m = as_u32(v[k]) & 0x7FFFFFFFu;      // as integers: finite < infinity < NaN
+        const uint32_t m = as_u32(v[k]) & 0x7FFFFFFFu;
         top = top > m ? top : m;
     }
     uint32_t o = dpp_move<0xB1>(top);
     top = top > o ? top : o;
     o = dpp_move<0x4E>(top);
     top = top > o ? top : o;
-
-    // exponent of max minus 6, one more where its mantissa is above 127 / 64
-    int byte = (int)((top + 0x1FFFFu) >> 23) - 6;
-    byte = byte < 1 ? 1 : byte;
-    const bool finite = top < 0x7F800000u;
-    const float inverse = as_f32((uint32_t)(254 - byte) << 23);
-
+    const ActStep s = act_step_of(top);
     const Philox4 r = philox_block(seed, epoch, (uint64_t)row, col8, stream);
-    uint32_t c[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t half = k & 1 ? r.w[k >> 1] >> 16 : r.w[k >> 1] & 0xFFFFu;
-        const float u = __builtin_fmaf((float)half, 1.0f / 65536.0f, 1.0f / 131072.0f);   // exact
-        // the product is exact, so the fused form rounds the sum as two operations would
-        const float t = __builtin_floorf(__builtin_fmaf(v[k], inverse, u));
-        c[k] = (uint32_t)(int)t;
-    }
     ActCodes8 out;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const uint32_t lo = __builtin_amdgcn_perm(c[4 * q + 1], c[4 * q], 0x0C0C0400u);
-        const uint32_t hi = __builtin_amdgcn_perm(c[4 * q + 3], c[4 * q + 2], 0x04000C0Cu);
-        out.codes[q] = finite ? lo | hi : 0u;
+        uint32_t c[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = r.w[2 * q + (k >> 1)];
+            c[k] = act_code(v[4 * q + k], s.inverse, k & 1 ? w >> 16 : w & 0xFFFFu);
+        }
+        out.codes[q] = s.finite ? act_pack4(c) : 0u;
     }
-    out.byte = finite ? (uint32_t)byte : 255u;
+    out.byte = s.byte;
     return out;
 }
 

@@ -1,13 +1,22 @@
 // Gated linear recurrence  h_t = f_t h_{t-1} + (1 - f_t) x_t,  f = sigmoid(z): packed sequences, forward and backward.
 //
 // Both directions are scans of pairs: a run of tokens takes a state h to A h + B, and two runs one after the other
-// to (A2 A1) h + (A2 B1 + B2).  A workgroup owns 64 channels and kBlock tokens: eight lanes side by side take eight
-// channels each (128 bytes of a bf16 row), 32 such rows of lanes take eight tokens each, which a thread walks through in
-// registers.  The rows of lanes are joined by shuffles and LDS, the blocks by the pairs in global memory.
+// to (A2 A1) h + (A2 B1 + B2).  A workgroup owns 64 channels and a block of 256 tokens: sixteen lanes side by side take four
+// channels each (128 bytes of a bf16 row), 32 such rows of lanes eight tokens each, which a thread walks through in
+// registers.  Everything is read and written once: the rows of lanes are joined by shuffles and LDS, the blocks by a chain in
+// global memory while their tokens stay in registers.
+//
+// The chain.  A block publishes its pair, takes the pairs of the blocks before it up to the last multiple of kSuper and the
+// state there, which the block before that multiple has published, and so has the state that enters it.  What is
+// joined in which order depends on the block's number alone, so the results do not depend on timing.  A word is a pair of
+// floats stored and polled as 64 bits, all ones before it is there (A is never a NaN).  Blocks are handed out by a
+// counter for each 64 channels, in the chain's order: a block waits only for blocks that were handed out before it, to
+// workgroups that run, and those wait for nothing that is behind them, so every wait ends.
 //
 // A = 0 marks a run that contains the start of a sequence (or lies outside all): what is before it does not matter, and
-// is not multiplied, so that a NaN or an infinity of one sequence never reaches the next.  Every other A is kept at
-// 2^-126 or more, so that within a sequence they do pass on; what that adds to a state is below 2^-126 of it.
+// is not multiplied, so that a NaN or an infinity of one sequence never reaches the next.  Every other A that leaves a
+// thread's block is kept at 2^-126 or more, so that within a sequence they do pass on; what that adds to a state is below
+// 2^-126 of it.
 #include "zipml_act.h"
 
 namespace zipml {
@@ -15,11 +24,15 @@ namespace zipml {
 constexpr int kBlock = ZIPML_SCAN_BLOCK;   // tokens of a workgroup
 constexpr int kCh = 64;                    // channels of a workgroup
 constexpr int kRun = 8;                    // tokens of a thread
-constexpr int kSubs = kBlock / kRun;       // rows of lanes
-constexpr int kThreads = kSubs * kCh / 8;
+constexpr int kOwn = 4;                    // channels of a thread
+constexpr int kLanes = kCh / kOwn;         // lanes side by side
+constexpr int kThreads = kBlock / kRun * kLanes;
 constexpr int kWaves = kThreads / kWave;
+constexpr int kRows = kWave / kLanes;      // runs of a wave
+constexpr int kSuper = 32;                 // blocks between two published states
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1
+static_assert(kSuper % kWaves == 0, "the waves share the pairs of kSuper blocks");
 
 struct ScanArgs {
     const void *x, *z;                     // forward
@@ -35,7 +48,9 @@ struct ScanArgs {
     const int64_t *seq_start;              // n_seq + 1 offsets, or NULL: one sequence
     const float *h0, *dh_last;
     float *h_last, *dh0;
-    float2 *pairs;                         // [blocks][channels]: of each block, then the states that enter it
+    uint64_t *pairs;                       // [blocks][channels], then
+    uint64_t *supers;                      // [blocks / kSuper][channels], then
+    uint32_t *counters;                    // [groups]
     uint64_t seed;
     uint32_t epoch, stream;
     int64_t tokens, channels, n_seq, blocks, groups;
@@ -50,13 +65,67 @@ __device__ __forceinline__ void gates(float z, float &f, float &g)
     g = z >= 0.0f ? eq : q;
 }
 
-__device__ __forceinline__ float join(float a, float prev, float b) { return a == 0.0f ? b : __builtin_fmaf(a, prev, b); }
-__device__ __forceinline__ float times(float a, float b) { return a == 0.0f || b == 0.0f ? 0.0f : __builtin_fmaxf(a * b, kTiny); }
+// Joins of runs.  SOME = false: no sequence starts or ends within, plain arithmetic.
+template <bool SOME>
+__device__ __forceinline__ float join(float a, float prev, float b)
+{
+    return SOME && a == 0.0f ? b : __builtin_fmaf(a, prev, b);
+}
+template <bool SOME>
+__device__ __forceinline__ float times(float a, float b)
+{
+    return !SOME ? a * b : a == 0.0f || b == 0.0f ? 0.0f : __builtin_fmaxf(a * b, kTiny);
+}
 
-// Which of the block's tokens are a sequence's first and last.
+// ---- four neighbouring values of a row, as fp32 -----------------------------------------------
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+template <typename T>
+__device__ __forceinline__ void load4(const T *p, int64_t left, float (&v)[kOwn])
+{
+    if (left >= kOwn) {
+        if constexpr (sizeof(T) == 2) {
+            const u32x2 w = *reinterpret_cast<const u32x2_any *>(p);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v[2 * k] = as_f32(w[k] << 16);
+                v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
+            }
+        } else {
+            const f32x4 w = *reinterpret_cast<const f32x4_any *>(p);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = w[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) v[k] = k < left ? (float)p[k] : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn])
+{
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+    if (left >= kOwn) {
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<bf16x4_any *>(p) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        else
+            *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+            if (k < left) p[k] = (T)v[k];
+    }
+}
+// Row s of an [n_seq][channels] array that may be missing (zeros then).
+__device__ __forceinline__ void load_state(const float *a, int64_t s, int64_t channels, int64_t c, float (&v)[kOwn])
+{
+    load4<float>(a + s * channels + c, a ? channels - c : 0, v);
+}
+
+// ---- sequences ---------------------------------------------------------------------------------
 struct BlockMap {
-    int first[kBlock], last[kBlock];       // the sequence, or -1
-    int some;                              // any token is either, or outside
+    int first[kBlock], last[kBlock];       // the sequence of which a token is the first or last, or -1
+    int some;                              // some token is either, or outside
 };
 struct Range { int64_t begin, end; };      // tokens inside sequences
 
@@ -87,345 +156,449 @@ __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t blk, Block
     return r;
 }
 
-// Eight floats of a row of `channels`, zeros beyond it or without the row.
-__device__ __forceinline__ void load_row(const float *row, int64_t left, float (&v)[8])
+// Empty sequences hand on what they are given.
+__device__ __forceinline__ void pass_on(const ScanArgs &p, int64_t blk, int64_t c0, const float *from, float *to)
 {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = row && k < left ? row[k] : 0.0f;
-}
-__device__ __forceinline__ void store_row(float *row, int64_t left, const float (&v)[8])
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (k < left) row[k] = v[k];
+    if (!to || !p.seq_start) return;
+    const int64_t c = c0 + (threadIdx.x & 63);
+    for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
+        if (p.seq_start[s] >= p.seq_start[s + 1] && c < p.channels)
+            to[s * p.channels + c] = from ? from[s * p.channels + c] : 0.0f;
 }
 
-// Pair of all runs before this thread's in its block (REVERSE: behind it), from each thread's own pair; total: of
-// the whole block.
-template <bool REVERSE>
-__device__ __forceinline__ void block_scan(float (&A)[8], float (&B)[8], float2 (&lds)[kWaves][kCh], float (&tA)[8],
-                                           float (&tB)[8])
+// ---- joining runs ------------------------------------------------------------------------------
+struct ScanShared {
+    BlockMap map;
+    float2 waves[kWaves][kCh];             // pairs of the waves, later of the blocks before
+    float2 total[kCh];
+    float carry[kCh];
+    uint32_t ticket;
+};
+
+// A, B: in, the pair of each thread's run; out, that of all runs before it in the block (REVERSE: behind it).  sh.total gets
+// the whole block's.
+template <bool REVERSE, bool SOME>
+__device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], ScanShared &sh)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cl = lane & 7;
-    const int pos = REVERSE ? 7 - (lane >> 3) : lane >> 3;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cl = lane & (kLanes - 1);
+    const int pos = REVERSE ? kRows - 1 - lane / kLanes : lane / kLanes;
+    auto before = [&](float v, int s) { return __shfl(v, (REVERSE ? lane + kLanes * s : lane - kLanes * s) & 63, 64); };
 #pragma unroll
-    for (int s = 1; s < 8; s <<= 1) {
+    for (int s = 1; s < kRows; s <<= 1)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int from = REVERSE ? lane + 8 * s : lane - 8 * s;
-            const float pa = __shfl(A[k], from & 63, 64), pb = __shfl(B[k], from & 63, 64);
-            if (pos >= s) {
-                B[k] = join(A[k], pb, B[k]);
-                A[k] = times(A[k], pa);
-            }
+        for (int k = 0; k < kOwn; ++k) {
+            const float pa = before(A[k], s), pb = before(B[k], s);
+            B[k] = pos >= s ? join<SOME>(A[k], pb, B[k]) : B[k];
+            A[k] = pos >= s ? times<SOME>(A[k], pa) : A[k];
         }
-    }
-    __syncthreads();                       // (whatever was read from lds before)
-    if (pos == 7)
+    __syncthreads();                       // (whatever was read from sh before)
+    if (pos == kRows - 1)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) lds[wave][cl * 8 + k] = float2{A[k], B[k]};
+        for (int k = 0; k < kOwn; ++k) sh.waves[wave][cl * kOwn + k] = float2{A[k], B[k]};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {          // of the runs before this one
-        const int from = (REVERSE ? lane + 8 : lane - 8) & 63;
-        const float pa = __shfl(A[k], from, 64), pb = __shfl(B[k], from, 64);
+    for (int k = 0; k < kOwn; ++k) {       // of the runs before this one
+        const float pa = before(A[k], 1), pb = before(B[k], 1);
         A[k] = pos == 0 ? 1.0f : pa;
         B[k] = pos == 0 ? 0.0f : pb;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kOwn; ++k) {
         float wa = 1.0f, wb = 0.0f;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
             const int w = REVERSE ? kWaves - 1 - i : i;
-            const float2 p = lds[w][cl * 8 + k];
+            const float2 p = sh.waves[w][cl * kOwn + k];
             if (w == wave) {               // (uniform over a wave)
-                B[k] = join(A[k], wb, B[k]);
-                A[k] = times(A[k], wa);
+                B[k] = join<SOME>(A[k], wb, B[k]);
+                A[k] = times<SOME>(A[k], wa);
             }
-            wb = join(p.x, wb, p.y);
-            wa = times(p.x, wa);
+            wb = join<SOME>(p.x, wb, p.y);
+            wa = times<SOME>(p.x, wa);
         }
-        tA[k] = wa;
-        tB[k] = wb;
+        if (threadIdx.x < kLanes) sh.total[cl * kOwn + k] = float2{SOME ? wa : __builtin_fmaxf(wa, kTiny), wb};
     }
 }
 
-// What both passes of the forward direction need: the pair (a, b) of each of the thread's tokens.
-__device__ __forceinline__ void forward_tokens(const ScanArgs &p, const BlockMap &m, Range r, int64_t t0, int sub, int64_t c,
-                                               const float (&x)[kRun][8], float (&a)[kRun][8], float (&b)[kRun][8])
+constexpr uint64_t kAbsent = ~0ull;
+__device__ __forceinline__ uint64_t word(float a, float b) { return (uint64_t)as_u32(a) << 32 | as_u32(b); }
+// The word once it is there.  (The limit is never reached; a NaN would tell.)
+__device__ __forceinline__ float2 await(const uint64_t *p)
 {
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            float f, g;
-            gates(a[j][k], f, g);
-            a[j][k] = f;
-            b[j][k] = g * x[j][k];
-        }
+    uint64_t w = load_dev(p);
+    for (int n = 0; w == kAbsent && n < (1 << 22); ++n) {
+        __builtin_amdgcn_s_sleep(1);
+        w = load_dev(p);
     }
-    if (!m.some) return;
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + sub * kRun + j;
-        const int s = m.first[sub * kRun + j];
-        if (t < r.begin || t >= r.end) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) a[j][k] = b[j][k] = 0.0f;
-        } else if (s >= 0) {
-            float h[8];
-            load_row(p.h0 ? p.h0 + s * p.channels + c : nullptr, p.channels - c, h);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                b[j][k] = p.h0 ? __builtin_fmaf(a[j][k], h[k], b[j][k]) : b[j][k];
-                a[j][k] = 0.0f;
-            }
-        }
-    }
+    if (w == kAbsent) return float2{0.0f, __builtin_nanf("")};
+    return float2{as_f32((uint32_t)(w >> 32)), as_f32((uint32_t)w)};
 }
 
-// APPLY = false: the pair of each block.  APPLY = true: states, from what enters the block.
-template <typename T, bool APPLY>
-__global__ __launch_bounds__(kThreads, 2) void k_scan_forward(ScanArgs p)
+// The state that enters block `k` of the chain (k counts in the direction of the scan; at(k) is the block), in sh.carry, from
+// sh.total; the block's own pair, and the state behind it where one is due, are published.
+template <bool REVERSE>
+__device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared &sh)
 {
-    __shared__ BlockMap map;
-    __shared__ float2 lds[kWaves][kCh];
-    const int64_t blk = blockIdx.x / p.groups, c0 = (blockIdx.x - blk * p.groups) * kCh;
-    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 3;
-    const int64_t c = c0 + (lane & 7) * 8, left = p.channels - c, t0 = blk * kBlock;
-    const Range r = block_map(p, blk, map);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = c0 + lane;
+    const bool live = c < p.channels;
+    __syncthreads();                       // sh.total is there, sh.waves free
+    auto at = [&](int64_t i) { return (REVERSE ? p.blocks - 1 - i : i) * p.channels + c; };
+    const float2 own = sh.total[lane];
+    if (wave == 0 && live && p.blocks > 1) store_dev(p.pairs + at(k), word(own.x, own.y));
 
-    float x[kRun][8], a[kRun][8], b[kRun][8];
+    // the pairs from the last multiple of kSuper on, a few of them to each wave
+    const int64_t base = k - k % kSuper;
+    float a = 1.0f, b = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kSuper / kWaves; ++i) {
+        const int64_t j = base + wave * (kSuper / kWaves) + i;
+        if (j >= k || !live) break;
+        const float2 w = await(p.pairs + at(j));
+        b = join<true>(w.x, b, w.y);
+        a = times<true>(w.x, a);
+    }
+    sh.waves[wave][lane] = float2{a, b};
+    __syncthreads();
+    if (wave == 0) {
+        float h = base > 0 && live ? await(p.supers + (base / kSuper - 1) * p.channels + c).y : 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) h = join<true>(sh.waves[w][lane].x, h, sh.waves[w][lane].y);
+        sh.carry[lane] = h;
+        if (live && k % kSuper == kSuper - 1)
+            store_dev(p.supers + k / kSuper * p.channels + c, word(0.0f, join<true>(own.x, h, own.y)));
+    }
+    __syncthreads();
+}
+
+// Which channels and which block a workgroup takes.  Workgroups go to the eight XCDs in turn; where there are enough channels,
+// two neighbouring groups of 64 stay on one XCD, since each writes half of a cache line of codes.
+struct Place { int64_t k, c0; };
+__device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
+{
+    const uint32_t n = (uint32_t)p.groups, b = blockIdx.x;
+    uint32_t g = b % n;
+    if (n % 16 == 0) g = (g & ~15u) | (g & 7) << 1 | (g >> 3 & 1);
+    if (p.blocks == 1) return Place{0, g * (int64_t)kCh};
+    if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return Place{sh.ticket, g * (int64_t)kCh};
+}
+
+// The words and counters of a chain before it starts.
+__global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, uint32_t *counters, int64_t groups)
+{
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += step) words[i] = kAbsent;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups; i += step) counters[i] = 0;
+}
+
+// ---- storing and reading the inputs ---------------------------------------------------------------
+// Two tokens (rows row, row + 1) of four columns; eight lanes hold a group's 32 columns.  A Philox block serves eight columns:
+// the two lanes that share them make that of one token each and exchange halves.
+__device__ __forceinline__ void encode_two(const float (&v)[2][kOwn], uint64_t seed, uint32_t epoch, int64_t row, uint32_t col8,
+                                           uint32_t stream, uint32_t (&codes)[2], uint32_t (&byte)[2])
+{
+    const bool odd = threadIdx.x & 1;
+    const Philox4 r = philox_block(seed, epoch, (uint64_t)(row + (odd ? 1 : 0)), col8, stream);
+    const uint32_t x0 = dpp_move<0xB1>(odd ? r.w[0] : r.w[2]), x1 = dpp_move<0xB1>(odd ? r.w[1] : r.w[3]);
+    const uint32_t w[2][2] = {{odd ? x0 : r.w[0], odd ? x1 : r.w[1]}, {odd ? r.w[2] : x0, odd ? r.w[3] : x1}};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const uint32_t m = as_u32(v[t][k]) & 0x7FFFFFFFu;
+            top = top > m ? top : m;
+        }
+        uint32_t o = dpp_move<0xB1>(top);
+        top = top > o ? top : o;
+        o = dpp_move<0x4E>(top);
+        top = top > o ? top : o;
+        o = dpp_move<0x141>(top);
+        top = top > o ? top : o;
+        const ActStep s = act_step_of(top);
+        uint32_t c[kOwn];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) c[k] = act_code(v[t][k], s.inverse, k & 1 ? w[t][k >> 1] >> 16 : w[t][k >> 1] & 0xFFFFu);
+        codes[t] = s.finite ? act_pack4(c) : 0u;
+        byte[t] = s.byte;
+    }
+}
+__device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[kOwn])
+{
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) v[k] = (float)(int8_t)(codes >> (8 * k)) * step;
+}
+
+// ---- forward -----------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
+{
+    __shared__ ScanShared sh;
+    const Place at = take(p, sh);
+    const int64_t blk = at.k, t0 = blk * kBlock;
+    const int run = threadIdx.x / kLanes * kRun;                    // the first token of the thread's run, in the block
+    const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
+
+    float a[kRun][kOwn], b[kRun][kOwn];                             // z and x, later f and (1 - f) x
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + sub * kRun + j;
-        const int64_t n = t < p.tokens ? left : 0;
-        load8((const T *)p.x + t * p.ldx + c, n, x[j]);
-        load8((const T *)p.z + t * p.ldz + c, n, a[j]);
+        const int64_t t = t0 + run + j, n = t < p.tokens ? left : 0;
+        load4<T>((const T *)p.x + t * p.ldx + c, n, b[j]);
+        load4<T>((const T *)p.z + t * p.ldz + c, n, a[j]);
     }
-    if (APPLY && p.wx) {
+    const Range r = block_map(p, blk, sh.map);
+
+    if (p.wx) {
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + sub * kRun + j;
-            float zc[8];
+        for (int j = 0; j < kRun; j += 2) {
+            float v[2][kOwn], z[2][kOwn];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) zc[k] = a[j][k] > kZMax ? kZMax : a[j][k] < -kZMax ? -kZMax : a[j][k];
-            const ActCodes8 cx = act_encode8(x[j], p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream);
-            const ActCodes8 cz = act_encode8(zc, p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream + 1);
-            if (t < p.tokens && c < p.lay.pitch) {
-                *reinterpret_cast<u32x2 *>(p.wx + t * p.lay.pitch + c) = cx.codes;
-                *reinterpret_cast<u32x2 *>(p.wz + t * p.lay.pitch + c) = cz.codes;
-                if ((lane & 3) == 0) {
-                    p.wx[p.lay.steps + t * p.lay.groups + (c >> 5)] = (uint8_t)cx.byte;
-                    p.wz[p.lay.steps + t * p.lay.groups + (c >> 5)] = (uint8_t)cz.byte;
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < kOwn; ++k) {
+                    const float q = a[j + i][k];
+                    v[i][k] = b[j + i][k];
+                    z[i][k] = q > kZMax ? kZMax : q < -kZMax ? -kZMax : q;
                 }
-            }
+            const int64_t t = t0 + run + j;
+            uint32_t cx[2], cz[2], ex[2], ez[2];
+            encode_two(v, p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream, cx, ex);
+            encode_two(z, p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream + 1, cz, ez);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (t + i < p.tokens && c < p.lay.pitch) {
+                    const int64_t o = (t + i) * p.lay.pitch + c;
+                    *reinterpret_cast<uint32_t *>(p.wx + o) = cx[i];
+                    *reinterpret_cast<uint32_t *>(p.wz + o) = cz[i];
+                    if ((threadIdx.x & 7) == 0) {
+                        const int64_t e = p.lay.steps + (t + i) * p.lay.groups + (c >> 5);
+                        p.wx[e] = (uint8_t)ex[i];
+                        p.wz[e] = (uint8_t)ez[i];
+                    }
+                }
         }
     }
-    forward_tokens(p, map, r, t0, sub, c, x, a, b);
-
-    float A[8], B[8], tA[8], tB[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            B[k] = join(a[j][k], B[k], b[j][k]);
-            A[k] = times(a[j][k], A[k]);
+        for (int k = 0; k < kOwn; ++k) {
+            float f, g;
+            gates(a[j][k], f, g);
+            a[j][k] = f;
+            b[j][k] *= g;
         }
-    block_scan<false>(A, B, lds, tA, tB);
 
-    if constexpr (!APPLY) {
-        if (sub == 0)
+    float A[kOwn], B[kOwn];
+    uint32_t reset = 0;                                             // tokens that do not look back
+    if (!sh.map.some) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < left) p.pairs[blk * p.channels + c + k] = float2{tA[k], tB[k]};
+        for (int k = 0; k < kOwn; ++k) { A[k] = a[0][k]; B[k] = b[0][k]; }
+#pragma unroll
+        for (int j = 1; j < kRun; ++j)
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                B[k] = __builtin_fmaf(a[j][k], B[k], b[j][k]);
+                A[k] *= a[j][k];
+            }
+        block_scan<false, false>(A, B, sh);
     } else {
-        float h[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float in = k < left && p.blocks > 1 ? p.pairs[blk * p.channels + c + k].y : 0.0f;
-            if (sub == 0 && p.states && k < left) p.states[blk * p.channels + c + k] = in;
-            h[k] = join(A[k], in, B[k]);
+        for (int k = 0; k < kOwn; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+            const int64_t t = t0 + run + j;
+            const int s = sh.map.first[run + j];
+            if (t < r.begin || t >= r.end) {
+#pragma unroll
+                for (int k = 0; k < kOwn; ++k) b[j][k] = 0.0f;
+                reset |= 1u << j;
+            } else if (s >= 0) {
+                if (p.h0) {
+                    float h[kOwn];
+                    load_state(p.h0, s, p.channels, c, h);
+#pragma unroll
+                    for (int k = 0; k < kOwn; ++k) b[j][k] = __builtin_fmaf(a[j][k], h[k], b[j][k]);
+                }
+                reset |= 1u << j;
+            }
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                B[k] = reset >> j & 1 ? b[j][k] : __builtin_fmaf(a[j][k], B[k], b[j][k]);
+                A[k] *= a[j][k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) A[k] = reset ? 0.0f : __builtin_fmaxf(A[k], kTiny);
+        block_scan<false, true>(A, B, sh);
+    }
+    chain<false>(p, at.k, at.c0, sh);
+
+    float h[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        const float in = sh.carry[c - at.c0 + k];
+        h[k] = sh.map.some ? join<true>(A[k], in, B[k]) : join<false>(A[k], in, B[k]);
+    }
+    if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
+        p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+        const int64_t t = t0 + run + j;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) h[k] = reset >> j & 1 ? b[j][k] : __builtin_fmaf(a[j][k], h[k], b[j][k]);
+        if (t < p.tokens) store4<T>((T *)p.y + t * p.ldy + c, left, h);
+        if (p.h_last && sh.map.some && sh.map.last[run + j] >= 0)
+            store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, left, h);
+    }
+    pass_on(p, blk, at.c0, p.h0, p.h_last);
+}
+
+// ---- backward ----------------------------------------------------------------------------------
+// p_t = f_t d_t, d_t = dy_t + p_{t+1}, is a scan from right to left with the same factors as that of the states from left to
+// right; a run's pairs of both come from one walk: B of the right-to-left one is the sum of d_t times the product of the f
+// up to t.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
+{
+    __shared__ ScanShared sh;
+    const Place at = take(p, sh);
+    const int64_t blk = p.blocks - 1 - at.k, t0 = blk * kBlock;
+    const int run = threadIdx.x / kLanes * kRun;
+    const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
+
+    uint32_t qx[kRun], ex[kRun];
+    float d[kRun][kOwn], f[kRun][kOwn], g[kRun][kOwn];
+    {
+        uint32_t qz[kRun], ez[kRun];
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+            const int64_t t = t0 + run + j;
+            const bool there = t < p.tokens && c < p.lay.pitch;
+            const int64_t o = t * p.lay.pitch + c, e = p.lay.steps + t * p.lay.groups + (c >> 5);
+            qz[j] = there ? *reinterpret_cast<const uint32_t *>(p.rz + o) : 0u;
+            ez[j] = there ? p.rz[e] : 0u;
+            qx[j] = there ? *reinterpret_cast<const uint32_t *>(p.rx + o) : 0u;
+            ex[j] = there ? p.rx[e] : 0u;
+            load4<T>((const T *)p.dy + t * p.lddy + c, t < p.tokens ? left : 0, d[j]);
         }
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + sub * kRun + j;
+            float z[kOwn];
+            decode4(qz[j], act_step(ez[j]), z);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = join(a[j][k], h[k], b[j][k]);
-            if (t < p.tokens) store8((T *)p.y + t * p.ldy + c, left, h);
-            if (p.h_last && map.some && map.last[sub * kRun + j] >= 0)
-                store_row(p.h_last + (int64_t)map.last[sub * kRun + j] * p.channels + c, left, h);
+            for (int k = 0; k < kOwn; ++k) gates(z[k], f[j][k], g[j][k]);
         }
-        // empty sequences hand their states on
-        if (p.h_last && p.seq_start)
-            for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
-                if (p.seq_start[s] >= p.seq_start[s + 1] && c0 + lane < p.channels)
-                    p.h_last[s * p.channels + c0 + lane] = p.h0 ? p.h0[s * p.channels + c0 + lane] : 0.0f;
     }
-}
+    const Range r = block_map(p, blk, sh.map);
+    const bool some = sh.map.some;
 
-// From the blocks' pairs to the states that enter them, in y; REVERSE: from the last block to the first.
-template <bool REVERSE>
-__global__ __launch_bounds__(64) void k_scan_blocks(float2 *pairs, int64_t blocks, int64_t channels)
-{
-    const int64_t c = blockIdx.x * 64ll + threadIdx.x;
-    if (c >= channels) return;
-    float h = 0.0f;
-    for (int64_t i = 0; i < blocks; ++i) {
-        float2 *q = pairs + (REVERSE ? blocks - 1 - i : i) * channels + c;
-        const float2 v = *q;
-        q->y = h;
-        h = join(v.x, h, v.y);
-    }
-}
-
-template <typename T, bool APPLY>
-__global__ __launch_bounds__(kThreads, 2) void k_scan_backward(ScanArgs p)
-{
-    __shared__ BlockMap map;
-    __shared__ float2 lds[kWaves][kCh];
-    const int64_t blk = blockIdx.x / p.groups, c0 = (blockIdx.x - blk * p.groups) * kCh;
-    const int lane = threadIdx.x & 63, sub = threadIdx.x >> 3;
-    const int64_t c = c0 + (lane & 7) * 8, left = p.channels - c, t0 = blk * kBlock;
-    const Range r = block_map(p, blk, map);
-
-    u32x2 qx[kRun], qz[kRun];
-    uint32_t ex[kRun], ez[kRun];
-    float d[kRun][8], f[kRun][8], g[kRun][8];
+    float A[kOwn], H[kOwn], AR[kOwn], P[kOwn];                      // pairs (A, H) from the left, (AR, P) from the right
+    uint32_t outside = 0, first = 0, last = 0;                      // tokens, by bit
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + sub * kRun + j;
-        const bool there = t < p.tokens && c < p.lay.pitch;
-        const int64_t at = t * p.lay.pitch + c, step = p.lay.steps + t * p.lay.groups + (c >> 5);
-        qz[j] = there ? *reinterpret_cast<const u32x2 *>(p.rz + at) : u32x2{0, 0};
-        ez[j] = there ? p.rz[step] : 0u;
-        if (APPLY) {
-            qx[j] = there ? *reinterpret_cast<const u32x2 *>(p.rx + at) : u32x2{0, 0};
-            ex[j] = there ? p.rx[step] : 0u;
-        }
-        load8((const T *)p.dy + t * p.lddy + c, t < p.tokens ? left : 0, d[j]);
-    }
+    for (int k = 0; k < kOwn; ++k) { A[k] = 1.0f; H[k] = P[k] = 0.0f; }
+    if (!some) {
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        float z[8];
-        act_decode8(qz[j], act_step(ez[j]), z);
+        for (int j = 0; j < kRun; ++j) {
+            float x[kOwn];
+            decode4(qx[j], act_step(ex[j]), x);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) gates(z[k], f[j][k], g[j][k]);
-    }
-    // whether a token is outside all sequences, its sequence's last, its first
-    auto outside = [&](int j) { const int64_t t = t0 + sub * kRun + j; return map.some && (t < r.begin || t >= r.end); };
-    auto last = [&](int j) { return map.some && map.last[sub * kRun + j] >= 0; };
-    auto first = [&](int j) { return map.some && map.first[sub * kRun + j] >= 0; };
-
-    // p_t = f_t (d_t + p_{t+1}) from right to left
-    float A[8], B[8], tA[8], tB[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
-#pragma unroll
-    for (int j = kRun - 1; j >= 0; --j) {
-        if (outside(j)) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) A[k] = B[k] = 0.0f;
-            continue;
-        }
-        if (last(j)) {
-            float h[8];
-            load_row(p.dh_last ? p.dh_last + (int64_t)map.last[sub * kRun + j] * p.channels + c : nullptr, left, h);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { d[j][k] += h[k]; A[k] = B[k] = 0.0f; }
+            for (int k = 0; k < kOwn; ++k) {
+                A[k] *= f[j][k];
+                H[k] = __builtin_fmaf(f[j][k], H[k], g[j][k] * x[k]);
+                P[k] = __builtin_fmaf(A[k], d[j][k], P[k]);
+            }
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            B[k] = f[j][k] * (d[j][k] + B[k]);
-            A[k] = A[k] == 0.0f ? 0.0f : __builtin_fmaxf(f[j][k] * A[k], kTiny);
-        }
-    }
-    block_scan<true>(A, B, lds, tA, tB);
-    if constexpr (!APPLY) {
-        if (sub == 0)
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < left) p.pairs[blk * p.channels + c + k] = float2{tA[k], tB[k]};
-        return;
+        for (int k = 0; k < kOwn; ++k) AR[k] = A[k];
+        block_scan<true, false>(AR, P, sh);
     } else {
-        float q[8];
+        bool cut = false;                                           // a sequence has ended in this run
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float in = k < left && p.blocks > 1 ? p.pairs[blk * p.channels + c + k].y : 0.0f;
-            q[k] = join(A[k], in, B[k]);
-        }
-        // d becomes the gradient of each state
+        for (int j = 0; j < kRun; ++j) {
+            const int64_t t = t0 + run + j;
+            float x[kOwn];
+            decode4(qx[j], act_step(ex[j]), x);
+            if (t < r.begin || t >= r.end) {
+                outside |= 1u << j;
+                cut = true;
 #pragma unroll
-        for (int j = kRun - 1; j >= 0; --j) {
-            if (outside(j)) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) d[j][k] = q[k] = 0.0f;
+                for (int k = 0; k < kOwn; ++k) H[k] = 0.0f;
                 continue;
             }
-            const bool end = last(j);
+            if (sh.map.last[run + j] >= 0) {
+                last |= 1u << j;
+                float h[kOwn];
+                load_state(p.dh_last, sh.map.last[run + j], p.channels, c, h);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                d[j][k] = end ? d[j][k] : d[j][k] + q[k];
-                q[k] = f[j][k] * d[j][k];
+                for (int k = 0; k < kOwn; ++k) d[j][k] += h[k];
             }
-            if (p.dh0 && first(j)) store_row(p.dh0 + (int64_t)map.first[sub * kRun + j] * p.channels + c, left, q);
+            if (sh.map.first[run + j] >= 0) {
+                first |= 1u << j;
+                load_state(p.h0, sh.map.first[run + j], p.channels, c, H);
+            }
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                A[k] *= f[j][k];
+                H[k] = __builtin_fmaf(f[j][k], H[k], g[j][k] * x[k]);
+                P[k] = cut ? P[k] : __builtin_fmaf(A[k], d[j][k], P[k]);
+            }
+            cut |= last >> j & 1;
         }
-
-        // the states again, from the one that the forward pass kept
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            float x[8];
-            act_decode8(qx[j], act_step(ex[j]), x);
-            if (first(j) || outside(j)) {
-                float h[8];
-                load_row(p.h0 && first(j) ? p.h0 + (int64_t)map.first[sub * kRun + j] * p.channels + c : nullptr, left, h);
-                const bool out = outside(j);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    A[k] = 0.0f;
-                    B[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[j][k] * x[k]);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    B[k] = __builtin_fmaf(f[j][k], B[k], g[j][k] * x[k]);
-                    A[k] = A[k] == 0.0f ? 0.0f : __builtin_fmaxf(f[j][k] * A[k], kTiny);
-                }
-            }
+        for (int k = 0; k < kOwn; ++k) {
+            const float m = __builtin_fmaxf(A[k], kTiny);
+            A[k] = first | outside ? 0.0f : m;
+            AR[k] = cut ? 0.0f : m;
         }
-        block_scan<false>(A, B, lds, tA, tB);
-        float h[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = join(A[k], k < left ? p.states[blk * p.channels + c + k] : 0.0f, B[k]);
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + sub * kRun + j;
-            float x[8], dx[8], dz[8];
-            act_decode8(qx[j], act_step(ex[j]), x);
-            const bool out = outside(j);
-            if (first(j)) load_row(p.h0 ? p.h0 + (int64_t)map.first[sub * kRun + j] * p.channels + c : nullptr, left, h);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                dx[k] = out ? 0.0f : g[j][k] * d[j][k];
-                dz[k] = out ? 0.0f : f[j][k] * dx[k] * (h[k] - x[k]);
-                h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[j][k] * x[k]);
-            }
-            if (t < p.tokens) {
-                store8((T *)p.dx + t * p.lddx + c, left, dx);
-                store8((T *)p.dz + t * p.lddz + c, left, dz);
-            }
-        }
-        // empty sequences hand their gradients on
-        if (p.dh0 && p.seq_start)
-            for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
-                if (p.seq_start[s] >= p.seq_start[s + 1] && c0 + lane < p.channels)
-                    p.dh0[s * p.channels + c0 + lane] = p.dh_last ? p.dh_last[s * p.channels + c0 + lane] : 0.0f;
+        block_scan<true, true>(AR, P, sh);
     }
+    chain<true>(p, at.k, at.c0, sh);
+    float q[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        const float in = sh.carry[c - at.c0 + k];
+        q[k] = some ? join<true>(AR[k], in, P[k]) : join<false>(AR[k], in, P[k]);
+    }
+
+    // d becomes the gradient of each state
+#pragma unroll
+    for (int j = kRun - 1; j >= 0; --j) {
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            d[j][k] = outside >> j & 1 ? 0.0f : last >> j & 1 ? d[j][k] : d[j][k] + q[k];
+            q[k] = outside >> j & 1 ? 0.0f : f[j][k] * d[j][k];
+        }
+        if (p.dh0 && first >> j & 1) store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, left, q);
+    }
+
+    // the states again, from the one that the forward pass kept
+    if (!some) block_scan<false, false>(A, H, sh);
+    else block_scan<false, true>(A, H, sh);
+    float h[kOwn];
+    load_state(p.states, blk, p.channels, c, h);
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) h[k] = some ? join<true>(A[k], h[k], H[k]) : join<false>(A[k], h[k], H[k]);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+        const int64_t t = t0 + run + j;
+        float x[kOwn], dx[kOwn], dz[kOwn];
+        decode4(qx[j], act_step(ex[j]), x);
+        if (first >> j & 1) load_state(p.h0, sh.map.first[run + j], p.channels, c, h);
+        const bool out = outside >> j & 1;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            dx[k] = out ? 0.0f : g[j][k] * d[j][k];
+            dz[k] = out ? 0.0f : f[j][k] * dx[k] * (h[k] - x[k]);
+            h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[j][k] * x[k]);
+        }
+        if (t < p.tokens) {
+            store4<T>((T *)p.dx + t * p.lddx + c, left, dx);
+            store4<T>((T *)p.dz + t * p.lddz + c, left, dz);
+        }
+    }
+    pass_on(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
 // One token of each of `rows` requests: the state in slot slots[row] (or row) of the pool is taken one step on.
@@ -444,14 +617,14 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
         load8(x + row * ldx + c, left, xv);
         load8(z + row * ldz + c, left, zv);
         float *s = h + slot * channels + c;
-        load_row(s, left, v);
+        load8<float>(s, left, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             float f, g;
             gates(zv[k], f, g);
             v[k] = __builtin_fmaf(f, v[k], g * xv[k]);
         }
-        store_row(s, left, v);
+        store8<float>(s, left, v);
     }
     store8(y + row * ldy + c, left, v);
 }
@@ -459,32 +632,30 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
 static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
 static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 {
-    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) <= (1ll << 31) - 1;
+    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) <= (1ll << 31) / kThreads * 8;
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
-template <typename T>
-static int launch_forward(hipStream_t s, const ScanArgs &p)
+// The chain's words behind one another in the workspace.
+struct ScanSpace { int64_t pairs, supers, groups; size_t bytes() const { return (size_t)(pairs + supers) * 8 + (size_t)groups * 4; } };
+static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
-    const dim3 grid((uint32_t)(p.blocks * p.groups));
-    if (p.blocks > 1) {
-        hipLaunchKernelGGL((k_scan_forward<T, false>), grid, dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL(k_scan_blocks<false>, dim3((uint32_t)((p.channels + 63) / 64)), dim3(64), 0, s, p.pairs, p.blocks,
-                           p.channels);
-    }
-    hipLaunchKernelGGL((k_scan_forward<T, true>), grid, dim3(kThreads), 0, s, p);
-    return hip_check(hipGetLastError());
+    const int64_t blocks = scan_blocks(tokens);
+    if (blocks == 1) return ScanSpace{0, 0, 0};
+    return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + kCh - 1) / kCh};
 }
-template <typename T>
-static int launch_backward(hipStream_t s, const ScanArgs &p)
+static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, void (*kernel)(ScanArgs))
 {
-    const dim3 grid((uint32_t)(p.blocks * p.groups));
+    const ScanSpace w = scan_space(p.tokens, p.channels);
+    p.pairs = (uint64_t *)workspace;
+    p.supers = p.pairs + w.pairs;
+    p.counters = (uint32_t *)(p.supers + w.supers);
     if (p.blocks > 1) {
-        hipLaunchKernelGGL((k_scan_backward<T, false>), grid, dim3(kThreads), 0, s, p);
-        hipLaunchKernelGGL(k_scan_blocks<true>, dim3((uint32_t)((p.channels + 63) / 64)), dim3(64), 0, s, p.pairs, p.blocks,
-                           p.channels);
+        const int64_t n = w.pairs + w.supers, blocks = (n + 1023) / 1024;
+        hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
+                           w.groups);
     }
-    hipLaunchKernelGGL((k_scan_backward<T, true>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(kThreads), 0, s, p);
     return hip_check(hipGetLastError());
 }
 
@@ -495,8 +666,8 @@ using namespace zipml;
 extern "C" size_t zipml_scan_workspace_bytes(int64_t tokens, int64_t channels)
 {
     if (!scan_sizes_ok(tokens, channels)) return 0;
-    const int64_t blocks = scan_blocks(tokens);
-    return blocks > 1 ? (size_t)blocks * (size_t)channels * sizeof(float2) : 256;
+    const size_t b = scan_space(tokens, channels).bytes();
+    return b < 256 ? 256 : b;
 }
 
 extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,
@@ -523,12 +694,11 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.wx = (uint8_t *)act_x_dev; p.wz = (uint8_t *)act_z_dev; p.states = states_dev;
     p.lay = act_layout(tokens, channels);
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.h_last = h_last_dev;
-    p.pairs = (float2 *)workspace_dev;
     p.seed = seed; p.epoch = epoch; p.stream = kActStream + tag;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return dtype == ZIPML_F32 ? launch_forward<float>(s, p) : launch_forward<__bf16>(s, p);
+    return scan_launch(s, p, workspace_dev, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -555,11 +725,10 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.dy = dy_dev; p.dx = dx_dev; p.dz = dz_dev;
     p.lddy = lddy; p.lddx = lddx; p.lddz = lddz;
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.dh_last = dh_last_dev; p.dh0 = dh0_dev;
-    p.pairs = (float2 *)workspace_dev;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return dtype == ZIPML_F32 ? launch_backward<float>(s, p) : launch_backward<__bf16>(s, p);
+    return scan_launch(s, p, workspace_dev, dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>);
 }
 
 template <typename T>
