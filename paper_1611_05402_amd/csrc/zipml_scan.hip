@@ -26,13 +26,15 @@ constexpr int kCh = 64;                    // channels of a workgroup
 constexpr int kRun = 8;                    // tokens of a thread
 constexpr int kOwn = 4;                    // channels of a thread
 constexpr int kLanes = kCh / kOwn;         // lanes side by side
-constexpr int kThreads = kBlock / kRun * kLanes;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kRows = kWave / kLanes;      // runs of a wave
 constexpr int kSuper = 32;                 // blocks between two published states
+// A workgroup of W waves takes a block of W * kRows * kRun tokens.
+constexpr int kForwardWaves = 8, kBackwardWaves = 8;
+constexpr int kWaveTokens = kRows * kRun;
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1
-static_assert(kSuper % kWaves == 0, "the waves share the pairs of kSuper blocks");
+static_assert(kSuper % kBackwardWaves == 0 && kSuper % kForwardWaves == 0, "the waves share the pairs of kSuper blocks");
+static_assert(kBackwardWaves * kWaveTokens == kBlock && kBlock % (kForwardWaves * kWaveTokens) == 0, "states by the block");
 
 struct ScanArgs {
     const void *x, *z;                     // forward
@@ -79,26 +81,50 @@ __device__ __forceinline__ float times(float a, float b)
 
 // ---- four neighbouring values of a row, as fp32 -----------------------------------------------
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+// The loads of a block are all issued before the first is used, so none of them stands in a branch: a thread whose columns or
+// rows are not all there reads the last ones that are, and `settle` moves columns to their places.
+struct Columns {
+    int64_t c, at;     // the thread's first column, and where it reads
+    bool few;          // fewer than four columns in all: read one by one
+    bool tail;         // (for the workgroup) columns beyond the last
+    __device__ __forceinline__ Columns(int64_t c0, int64_t c_, int64_t channels)
+    {
+        c = c_;
+        few = channels < kOwn;
+        tail = c0 + kCh > channels;
+        at = c <= channels - kOwn ? c : channels - kOwn;
+    }
+};
 template <typename T>
-__device__ __forceinline__ void load4(const T *p, int64_t left, float (&v)[kOwn])
+__device__ __forceinline__ void load_few(const T *row, const Columns &q, int64_t channels, float (&v)[kOwn])
 {
-    if (left >= kOwn) {
-        if constexpr (sizeof(T) == 2) {
-            const u32x2 w = *reinterpret_cast<const u32x2_any *>(p);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                v[2 * k] = as_f32(w[k] << 16);
-                v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
-            }
-        } else {
-            const f32x4 w = *reinterpret_cast<const f32x4_any *>(p);
+    for (int k = 0; k < kOwn; ++k) v[k] = q.c + k < channels ? (float)row[q.c + k] : 0.0f;
+}
+template <typename T>
+__device__ __forceinline__ void load4(const T *row, const Columns &q, float (&v)[kOwn])
+{
+    if constexpr (sizeof(T) == 2) {
+        const u32x2 w = *reinterpret_cast<const u32x2_any *>(row + q.at);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = w[k];
+        for (int k = 0; k < 2; ++k) {
+            v[2 * k] = as_f32(w[k] << 16);
+            v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
         }
     } else {
+        const f32x4 w = *reinterpret_cast<const f32x4_any *>(row + q.at);
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k) v[k] = k < left ? (float)p[k] : 0.0f;
+        for (int k = 0; k < 4; ++k) v[k] = w[k];
     }
+}
+__device__ __forceinline__ void settle(const Columns &q, float (&v)[kOwn])
+{
+    if (!q.tail || q.few) return;
+    const int64_t s = q.c - q.at;
+    if (s & 1) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; v[3] = 0.0f; }
+    if (s & 2) { v[0] = v[2]; v[1] = v[3]; v[2] = v[3] = 0.0f; }
+    if (s >= kOwn) v[0] = v[1] = v[2] = v[3] = 0.0f;
 }
 template <typename T>
 __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn])
@@ -119,22 +145,25 @@ __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn
 // Row s of an [n_seq][channels] array that may be missing (zeros then).
 __device__ __forceinline__ void load_state(const float *a, int64_t s, int64_t channels, int64_t c, float (&v)[kOwn])
 {
-    load4<float>(a + s * channels + c, a ? channels - c : 0, v);
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) v[k] = a && c + k < channels ? a[s * channels + c + k] : 0.0f;
 }
 
 // ---- sequences ---------------------------------------------------------------------------------
+template <int W>
 struct BlockMap {
-    int first[kBlock], last[kBlock];       // the sequence of which a token is the first or last, or -1
+    int first[W * kWaveTokens], last[W * kWaveTokens];   // the sequence of which a token is the first or last, or -1
     int some;                              // some token is either, or outside
 };
 struct Range { int64_t begin, end; };      // tokens inside sequences
 
-__device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t blk, BlockMap &m)
+template <int W>
+__device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockMap<W> &m)
 {
+    constexpr int kBlock = W * kWaveTokens, kThreads = W * kWave;
     for (int i = threadIdx.x; i < kBlock; i += kThreads) m.first[i] = m.last[i] = -1;
     if (threadIdx.x == 0) m.some = 0;
     __syncthreads();
-    const int64_t t0 = blk * kBlock;
     Range r{0, a.tokens};
     if (a.seq_start) {
         r.begin = a.seq_start[0];
@@ -157,19 +186,21 @@ __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t blk, Block
 }
 
 // Empty sequences hand on what they are given.
+template <int W>
 __device__ __forceinline__ void pass_on(const ScanArgs &p, int64_t blk, int64_t c0, const float *from, float *to)
 {
     if (!to || !p.seq_start) return;
     const int64_t c = c0 + (threadIdx.x & 63);
-    for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
+    for (int64_t s = blk * W + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * W)
         if (p.seq_start[s] >= p.seq_start[s + 1] && c < p.channels)
             to[s * p.channels + c] = from ? from[s * p.channels + c] : 0.0f;
 }
 
 // ---- joining runs ------------------------------------------------------------------------------
+template <int W>
 struct ScanShared {
-    BlockMap map;
-    float2 waves[kWaves][kCh];             // pairs of the waves, later of the blocks before
+    BlockMap<W> map;
+    float2 waves[W][kCh];             // pairs of the waves, later of the blocks before
     float2 total[kCh];
     float carry[kCh];
     uint32_t ticket;
@@ -177,8 +208,8 @@ struct ScanShared {
 
 // A, B: in, the pair of each thread's run; out, that of all runs before it in the block (REVERSE: behind it).  sh.total gets
 // the whole block's.
-template <bool REVERSE, bool SOME>
-__device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], ScanShared &sh)
+template <bool REVERSE, bool SOME, int W>
+__device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], ScanShared<W> &sh)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cl = lane & (kLanes - 1);
     const int pos = REVERSE ? kRows - 1 - lane / kLanes : lane / kLanes;
@@ -206,8 +237,8 @@ __device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], S
     for (int k = 0; k < kOwn; ++k) {
         float wa = 1.0f, wb = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) {
-            const int w = REVERSE ? kWaves - 1 - i : i;
+        for (int i = 0; i < W; ++i) {
+            const int w = REVERSE ? W - 1 - i : i;
             const float2 p = sh.waves[w][cl * kOwn + k];
             if (w == wave) {               // (uniform over a wave)
                 B[k] = join<SOME>(A[k], wb, B[k]);
@@ -223,21 +254,20 @@ __device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], S
 constexpr uint64_t kAbsent = ~0ull;
 __device__ __forceinline__ uint64_t word(float a, float b) { return (uint64_t)as_u32(a) << 32 | as_u32(b); }
 // The word once it is there.  (The limit is never reached; a NaN would tell.)
-__device__ __forceinline__ float2 await(const uint64_t *p)
+__device__ __forceinline__ uint64_t await(const uint64_t *p)
 {
     uint64_t w = load_dev(p);
     for (int n = 0; w == kAbsent && n < (1 << 22); ++n) {
         __builtin_amdgcn_s_sleep(1);
         w = load_dev(p);
     }
-    if (w == kAbsent) return float2{0.0f, __builtin_nanf("")};
-    return float2{as_f32((uint32_t)(w >> 32)), as_f32((uint32_t)w)};
+    return w == kAbsent ? word(0.0f, __builtin_nanf("")) : w;
 }
 
 // The state that enters block `k` of the chain (k counts in the direction of the scan; at(k) is the block), in sh.carry, from
 // sh.total; the block's own pair, and the state behind it where one is due, are published.
-template <bool REVERSE>
-__device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared &sh)
+template <bool REVERSE, int W>
+__device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared<W> &sh)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = c0 + lane;
@@ -248,22 +278,25 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
     if (wave == 0 && live && p.blocks > 1) store_dev(p.pairs + at(k), word(own.x, own.y));
 
     // the pairs from the last multiple of kSuper on, a few of them to each wave
-    const int64_t base = k - k % kSuper;
+    constexpr int kEach = kSuper / W;
+    const int64_t base = k - k % kSuper, from = base + wave * kEach;
+    uint64_t w[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) w[i] = from + i < k && live ? load_dev(p.pairs + at(from + i)) : word(1.0f, 0.0f);
     float a = 1.0f, b = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kSuper / kWaves; ++i) {
-        const int64_t j = base + wave * (kSuper / kWaves) + i;
-        if (j >= k || !live) break;
-        const float2 w = await(p.pairs + at(j));
-        b = join<true>(w.x, b, w.y);
-        a = times<true>(w.x, a);
+    for (int i = 0; i < kEach; ++i) {
+        if (w[i] == kAbsent) w[i] = await(p.pairs + at(from + i));
+        const float wa = as_f32((uint32_t)(w[i] >> 32)), wb = as_f32((uint32_t)w[i]);
+        b = join<true>(wa, b, wb);
+        a = times<true>(wa, a);
     }
     sh.waves[wave][lane] = float2{a, b};
     __syncthreads();
     if (wave == 0) {
-        float h = base > 0 && live ? await(p.supers + (base / kSuper - 1) * p.channels + c).y : 0.0f;
+        float h = base > 0 && live ? as_f32((uint32_t)await(p.supers + (base / kSuper - 1) * p.channels + c)) : 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) h = join<true>(sh.waves[w][lane].x, h, sh.waves[w][lane].y);
+        for (int i = 0; i < W; ++i) h = join<true>(sh.waves[i][lane].x, h, sh.waves[i][lane].y);
         sh.carry[lane] = h;
         if (live && k % kSuper == kSuper - 1)
             store_dev(p.supers + k / kSuper * p.channels + c, word(0.0f, join<true>(own.x, h, own.y)));
@@ -274,7 +307,8 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
 // Which channels and which block a workgroup takes.  Workgroups go to the eight XCDs in turn; where there are enough channels,
 // two neighbouring groups of 64 stay on one XCD, since each writes half of a cache line of codes.
 struct Place { int64_t k, c0; };
-__device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
+template <int W>
+__device__ __forceinline__ Place take(const ScanArgs &p, ScanShared<W> &sh)
 {
     const uint32_t n = (uint32_t)p.groups, b = blockIdx.x;
     uint32_t g = b % n;
@@ -333,23 +367,38 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 
 // ---- forward -----------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
+__global__ __launch_bounds__(kForwardWaves * kWave, 4) void k_scan_forward(ScanArgs p)
 {
-    __shared__ ScanShared sh;
+    constexpr int W = kForwardWaves;
+    __shared__ ScanShared<W> sh;
     const Place at = take(p, sh);
-    const int64_t blk = at.k, t0 = blk * kBlock;
+    const int64_t blk = at.k, t0 = blk * (W * kWaveTokens);
     const int run = threadIdx.x / kLanes * kRun;                    // the first token of the thread's run, in the block
     const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
+    const Columns cols(at.c0, c, p.channels);
 
     float a[kRun][kOwn], b[kRun][kOwn];                             // z and x, later f and (1 - f) x
+    auto row = [&](int j) { return t0 + run + j < p.tokens ? t0 + run + j : p.tokens - 1; };
+    if (!cols.few) {
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+            load4((const T *)p.x + row(j) * p.ldx, cols, b[j]);
+            load4((const T *)p.z + row(j) * p.ldz, cols, a[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) {
+            load_few((const T *)p.x + row(j) * p.ldx, cols, p.channels, b[j]);
+            load_few((const T *)p.z + row(j) * p.ldz, cols, p.channels, a[j]);
+        }
+    }
+    const Range r = block_map(p, t0, sh.map);
+
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + run + j, n = t < p.tokens ? left : 0;
-        load4<T>((const T *)p.x + t * p.ldx + c, n, b[j]);
-        load4<T>((const T *)p.z + t * p.ldz + c, n, a[j]);
+        settle(cols, b[j]);
+        settle(cols, a[j]);
     }
-    const Range r = block_map(p, blk, sh.map);
-
     if (p.wx) {
 #pragma unroll
         for (int j = 0; j < kRun; j += 2) {
@@ -441,8 +490,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
         const float in = sh.carry[c - at.c0 + k];
         h[k] = sh.map.some ? join<true>(A[k], in, B[k]) : join<false>(A[k], in, B[k]);
     }
-    if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
-        p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
+    if (p.states && t0 % kBlock == 0 && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
+        p.states[t0 / kBlock * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
         const int64_t t = t0 + run + j;
@@ -452,7 +501,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
         if (p.h_last && sh.map.some && sh.map.last[run + j] >= 0)
             store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, left, h);
     }
-    pass_on(p, blk, at.c0, p.h0, p.h_last);
+    pass_on<W>(p, blk, at.c0, p.h0, p.h_last);
 }
 
 // ---- backward ----------------------------------------------------------------------------------
@@ -460,29 +509,39 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // right; a run's pairs of both come from one walk: B of the right-to-left one is the sum of d_t times the product of the f
 // up to t.
 template <typename T>
-__global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
+__global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(ScanArgs p)
 {
-    __shared__ ScanShared sh;
+    constexpr int W = kBackwardWaves;
+    __shared__ ScanShared<W> sh;
     const Place at = take(p, sh);
     const int64_t blk = p.blocks - 1 - at.k, t0 = blk * kBlock;
     const int run = threadIdx.x / kLanes * kRun;
     const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
+    const Columns cols(at.c0, c, p.channels);
 
     uint32_t qx[kRun], ex[kRun];
     float d[kRun][kOwn], f[kRun][kOwn], g[kRun][kOwn];
     {
         uint32_t qz[kRun], ez[kRun];
+        auto row = [&](int j) { return t0 + run + j < p.tokens ? t0 + run + j : p.tokens - 1; };
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + run + j;
-            const bool there = t < p.tokens && c < p.lay.pitch;
-            const int64_t o = t * p.lay.pitch + c, e = p.lay.steps + t * p.lay.groups + (c >> 5);
-            qz[j] = there ? *reinterpret_cast<const uint32_t *>(p.rz + o) : 0u;
-            ez[j] = there ? p.rz[e] : 0u;
-            qx[j] = there ? *reinterpret_cast<const uint32_t *>(p.rx + o) : 0u;
-            ex[j] = there ? p.rx[e] : 0u;
-            load4<T>((const T *)p.dy + t * p.lddy + c, t < p.tokens ? left : 0, d[j]);
+            const int64_t t = row(j), cc = c < p.lay.pitch ? c : p.lay.pitch - kOwn;
+            const int64_t o = t * p.lay.pitch + cc, e = p.lay.steps + t * p.lay.groups + (cc >> 5);
+            qz[j] = *reinterpret_cast<const uint32_t *>(p.rz + o);
+            ez[j] = p.rz[e];
+            qx[j] = *reinterpret_cast<const uint32_t *>(p.rx + o);
+            ex[j] = p.rx[e];
         }
+        if (!cols.few) {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) load4((const T *)p.dy + row(j) * p.lddy, cols, d[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) load_few((const T *)p.dy + row(j) * p.lddy, cols, p.channels, d[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) settle(cols, d[j]);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float z[kOwn];
@@ -491,7 +550,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             for (int k = 0; k < kOwn; ++k) gates(z[k], f[j][k], g[j][k]);
         }
     }
-    const Range r = block_map(p, blk, sh.map);
+    const Range r = block_map(p, t0, sh.map);
     const bool some = sh.map.some;
 
     float A[kOwn], H[kOwn], AR[kOwn], P[kOwn];                      // pairs (A, H) from the left, (AR, P) from the right
@@ -598,7 +657,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             store4<T>((T *)p.dz + t * p.lddz + c, left, dz);
         }
     }
-    pass_on(p, blk, at.c0, p.dh_last, p.dh0);
+    pass_on<W>(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
 // One token of each of `rows` requests: the state in slot slots[row] (or row) of the pool is taken one step on.
@@ -629,24 +688,25 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
     store8(y + row * ldy + c, left, v);
 }
 
-static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
+static int64_t scan_blocks(int64_t tokens, int waves) { return (tokens + waves * kWaveTokens - 1) / (waves * kWaveTokens); }
 static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 {
-    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) <= (1ll << 31) / kThreads * 8;
+    return act_sizes_ok(tokens, channels) && scan_blocks(tokens, kForwardWaves) * ((channels + kCh - 1) / kCh) <= (1ll << 31) - 1;
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
 // The chain's words behind one another in the workspace.
 struct ScanSpace { int64_t pairs, supers, groups; size_t bytes() const { return (size_t)(pairs + supers) * 8 + (size_t)groups * 4; } };
-static ScanSpace scan_space(int64_t tokens, int64_t channels)
+static ScanSpace scan_space(int64_t tokens, int64_t channels, int waves)
 {
-    const int64_t blocks = scan_blocks(tokens);
+    const int64_t blocks = scan_blocks(tokens, waves);
     if (blocks == 1) return ScanSpace{0, 0, 0};
     return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + kCh - 1) / kCh};
 }
-static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, void (*kernel)(ScanArgs))
+static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, int waves, void (*kernel)(ScanArgs))
 {
-    const ScanSpace w = scan_space(p.tokens, p.channels);
+    const ScanSpace w = scan_space(p.tokens, p.channels, waves);
+    p.blocks = scan_blocks(p.tokens, waves);
     p.pairs = (uint64_t *)workspace;
     p.supers = p.pairs + w.pairs;
     p.counters = (uint32_t *)(p.supers + w.supers);
@@ -655,7 +715,7 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, void (*kerne
         hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
                            w.groups);
     }
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(waves * kWave), 0, s, p);
     return hip_check(hipGetLastError());
 }
 
@@ -666,7 +726,8 @@ using namespace zipml;
 extern "C" size_t zipml_scan_workspace_bytes(int64_t tokens, int64_t channels)
 {
     if (!scan_sizes_ok(tokens, channels)) return 0;
-    const size_t b = scan_space(tokens, channels).bytes();
+    // (the forward pass has the more blocks)
+    const size_t b = scan_space(tokens, channels, kForwardWaves).bytes();
     return b < 256 ? 256 : b;
 }
 
@@ -696,9 +757,9 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.h_last = h_last_dev;
     p.seed = seed; p.epoch = epoch; p.stream = kActStream + tag;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
-    p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
+    p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return scan_launch(s, p, workspace_dev, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
+    return scan_launch(s, p, workspace_dev, kForwardWaves, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -726,9 +787,9 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.lddy = lddy; p.lddx = lddx; p.lddz = lddz;
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.dh_last = dh_last_dev; p.dh0 = dh0_dev;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
-    p.blocks = scan_blocks(tokens); p.groups = (channels + kCh - 1) / kCh;
+    p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return scan_launch(s, p, workspace_dev, dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>);
+    return scan_launch(s, p, workspace_dev, kBackwardWaves, dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>);
 }
 
 template <typename T>
