@@ -107,15 +107,40 @@ __device__ __forceinline__ ActStep act_step_of(uint32_t top)
     const bool finite = top < 0x7F800000u;
     return ActStep{finite ? (uint32_t)byte : 255u, as_f32((uint32_t)(254 - byte) << 23), finite};
 }
-// The code of a value from its 16-bit draw, in the low byte.  (k + 1/2) / 2^16 is exact, and so is the product, so that the
-// fused form rounds the sum as two operations would.
-__device__ __forceinline__ uint32_t act_code(float v, float inverse, uint32_t draw)
+// floor as an integer, in one operation.
+__device__ __forceinline__ int floor_int(float x)
 {
-    const float u = __builtin_fmaf((float)draw, 1.0f / 65536.0f, 1.0f / 131072.0f);
-    return (uint32_t)(int)__builtin_floorf(__builtin_fmaf(v, inverse, u));
+    int i;
+    __asm__("v_cvt_flr_i32_f32 %0, %1" : "=v"(i) : "v"(x));
+    return i;
 }
-__device__ __forceinline__ uint32_t act_pack4(const uint32_t (&c)[4])
+// Four codes from their 16-bit draws (the halves of w0, w1, low first).
+//   fp32: floor(v / step + (k + 1/2) / 2^16) as it stands; (k + 1/2) / 2^16 is exact, and so is the product, so the fused form
+//   rounds the sum as two operations would.
+//   bf16: floor(2^16 v / step + 1/2) + k, the code in bits 16 and up: two operations less.  A bf16 value has 8 bits, so that sum
+//   is rounded only where v / step is below 2^-16, and the two forms agree on all values but 255/256 * 2^-17 with
+//   k = 2^16 - 1, where the sum above rounds up to 1; with 1/2 + 2^-9 in place of 1/2 they agree there too, and nowhere else does
+//   the 2^-9 matter (it would take a fraction within 2^-9 below 1/2, which 8 bits cannot hold at any other value).
+//   Steps below 2^-109 would overflow 2^16 / step; then (top says) the fp32 form is taken.
+template <typename T>
+__device__ __forceinline__ uint32_t act_codes4(const float (&v)[4], const ActStep &s, uint32_t w0, uint32_t w1, uint32_t top)
 {
+    const uint32_t w[2] = {w0, w1};
+    uint32_t c[4];
+    if (sizeof(T) == 2 && (top == 0 || s.byte >= 17)) {
+        const uint32_t e = 270u - s.byte;
+        const float scale = as_f32((e < 254u ? e : 254u) << 23);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            c[k] = (uint32_t)floor_int(__builtin_fmaf(v[k], scale, 0.5f + 1.0f / 512.0f)) + (k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xFFFFu);
+        return __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0602u) | __builtin_amdgcn_perm(c[3], c[2], 0x06020C0Cu);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t draw = k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xFFFFu;
+        const float u = __builtin_fmaf((float)draw, 1.0f / 65536.0f, 1.0f / 131072.0f);
+        c[k] = (uint32_t)floor_int(__builtin_fmaf(v[k], s.inverse, u));
+    }
     return __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000C0Cu);
 }
 
@@ -127,6 +152,7 @@ struct ActCodes8 {
 // Four neighbouring lanes, the first a multiple of four, hold the 32 values of a group, eight each (zeros beyond the
 // row's end).  All four have to be active.  One Philox block gives the eight draws, 16 bits each: the chance of the
 // upper neighbour is right to 2^-17 of a step, and half the multiplies of 24-bit draws are saved.
+template <typename T>
 __device__ __forceinline__ ActCodes8 act_encode8(const float (&v)[8], uint64_t seed, uint32_t epoch, int64_t row,
                                                  uint32_t col8, uint32_t stream)
 {
@@ -145,13 +171,8 @@ __device__ __forceinline__ ActCodes8 act_encode8(const float (&v)[8], uint64_t s
     ActCodes8 out;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        uint32_t c[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t w = r.w[2 * q + (k >> 1)];
-            c[k] = act_code(v[4 * q + k], s.inverse, k & 1 ? w >> 16 : w & 0xFFFFu);
-        }
-        out.codes[q] = s.finite ? act_pack4(c) : 0u;
+        const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        out.codes[q] = s.finite ? act_codes4<T>(x, s, r.w[2 * q], r.w[2 * q + 1], top) : 0u;
     }
     out.byte = s.byte;
     return out;

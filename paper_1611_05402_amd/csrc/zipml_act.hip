@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, Act
         for (int q = 0; q < kRows; ++q) {
             const int64_t row = row0 + q * ny;
             if (row >= lay.rows) break;
-            const ActCodes8 c = act_encode8(v[q], seed, epoch, row, (uint32_t)unit, stream);
+            const ActCodes8 c = act_encode8<T>(v[q], seed, epoch, row, (uint32_t)unit, stream);
             *reinterpret_cast<u32x2 *>(act + row * lay.pitch + unit * 8) = c.codes;
             if ((unit & 3) == 0) act[lay.steps + row * lay.groups + (unit >> 2)] = (uint8_t)c.byte;
         }

@@ -28,13 +28,11 @@ constexpr int kOwn = 4;                    // channels of a thread
 constexpr int kLanes = kCh / kOwn;         // lanes side by side
 constexpr int kRows = kWave / kLanes;      // runs of a wave
 constexpr int kSuper = 32;                 // blocks between two published states
-// A workgroup of W waves takes a block of W * kRows * kRun tokens.
-constexpr int kForwardWaves = 8, kBackwardWaves = 8;
-constexpr int kWaveTokens = kRows * kRun;
+constexpr int kWaves = kBlock / (kRows * kRun);
+constexpr int kThreads = kWaves * kWave;
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1
-static_assert(kSuper % kBackwardWaves == 0 && kSuper % kForwardWaves == 0, "the waves share the pairs of kSuper blocks");
-static_assert(kBackwardWaves * kWaveTokens == kBlock && kBlock % (kForwardWaves * kWaveTokens) == 0, "states by the block");
+static_assert(kSuper % kWaves == 0, "the waves share the pairs of kSuper blocks");
 
 struct ScanArgs {
     const void *x, *z;                     // forward
@@ -79,53 +77,90 @@ __device__ __forceinline__ float times(float a, float b)
     return !SOME ? a * b : a == 0.0f || b == 0.0f ? 0.0f : __builtin_fmaxf(a * b, kTiny);
 }
 
-// ---- four neighbouring values of a row, as fp32 -----------------------------------------------
+// ---- four neighbouring values of a row -----------------------------------------------------------
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef u32x4 u32x4_four __attribute__((aligned(4)));
 
-// The loads of a block are all issued before the first is used, so none of them stands in a branch: a thread whose columns or
-// rows are not all there reads the last ones that are, and `settle` moves columns to their places.
-struct Columns {
-    int64_t c, at;     // the thread's first column, and where it reads
-    bool few;          // fewer than four columns in all: read one by one
-    bool tail;         // (for the workgroup) columns beyond the last
-    __device__ __forceinline__ Columns(int64_t c0, int64_t c_, int64_t channels)
+// As they lie in memory; of() is value k in fp32.
+template <typename T> struct Raw4;
+template <> struct Raw4<__bf16> {
+    u32x2 w;
+    __device__ __forceinline__ float of(int k) const { return as_f32(k & 1 ? w[k >> 1] & 0xFFFF0000u : w[k >> 1] << 16); }
+    __device__ __forceinline__ void load(const __bf16 *p) { w = *reinterpret_cast<const u32x2_any *>(p); }
+    __device__ __forceinline__ void move(int s)            // value k becomes value k + s
     {
-        c = c_;
-        few = channels < kOwn;
-        tail = c0 + kCh > channels;
-        at = c <= channels - kOwn ? c : channels - kOwn;
+        const uint64_t v = s >= kOwn ? 0 : __builtin_bit_cast(uint64_t, w) >> (16 * (s & 3));
+        w = __builtin_bit_cast(u32x2, v);
     }
 };
-template <typename T>
-__device__ __forceinline__ void load_few(const T *row, const Columns &q, int64_t channels, float (&v)[kOwn])
-{
-#pragma unroll
-    for (int k = 0; k < kOwn; ++k) v[k] = q.c + k < channels ? (float)row[q.c + k] : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void load4(const T *row, const Columns &q, float (&v)[kOwn])
-{
-    if constexpr (sizeof(T) == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2_any *>(row + q.at);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            v[2 * k] = as_f32(w[k] << 16);
-            v[2 * k + 1] = as_f32(w[k] & 0xFFFF0000u);
-        }
-    } else {
-        const f32x4 w = *reinterpret_cast<const f32x4_any *>(row + q.at);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = w[k];
+template <> struct Raw4<float> {
+    u32x4 w;
+    __device__ __forceinline__ float of(int k) const { return as_f32(w[k]); }
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const u32x4_four *>(p); }
+    __device__ __forceinline__ void move(int s)
+    {
+        if (s & 1) w = u32x4{w[1], w[2], w[3], 0u};
+        if (s & 2) w = u32x4{w[2], w[3], 0u, 0u};
+        if (s >= kOwn) w = u32x4{0u, 0u, 0u, 0u};
     }
-}
-__device__ __forceinline__ void settle(const Columns &q, float (&v)[kOwn])
-{
-    if (!q.tail || q.few) return;
-    const int64_t s = q.c - q.at;
-    if (s & 1) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; v[3] = 0.0f; }
-    if (s & 2) { v[0] = v[2]; v[1] = v[3]; v[2] = v[3] = 0.0f; }
-    if (s >= kOwn) v[0] = v[1] = v[2] = v[3] = 0.0f;
-}
+};
+
+// A thread's part of a block's rows.  The loads of a block are all issued before the first is used, so none of them stands in a
+// branch of its own: a thread whose rows or columns are not all there reads the last ones that are, and `settle` moves columns
+// to their places.  Fewer than four columns in all are read one by one.
+struct Part {
+    int64_t t, c;          // first token and first column
+    int64_t tokens, channels;
+    int64_t at;            // the column at which it reads
+    bool whole;            // (for the workgroup) all rows are there
+    __device__ __forceinline__ Part(const ScanArgs &p, int64_t t0, int64_t c0)
+    {
+        tokens = p.tokens;
+        channels = p.channels;
+        t = t0 + threadIdx.x / kLanes * kRun;
+        c = c0 + (threadIdx.x & (kLanes - 1)) * kOwn;
+        at = c <= channels - kOwn ? c : channels - kOwn;
+        whole = t0 + kBlock <= tokens;
+    }
+    __device__ __forceinline__ int64_t left() const { return channels - c; }
+    // what(j, element offset of row j at column `col`)
+    template <typename What>
+    __device__ __forceinline__ void rows(int64_t ld, int64_t col, What what) const
+    {
+        if (whole) {
+            int64_t o = t * ld + col;
+#pragma unroll
+            for (int j = 0; j < kRun; ++j, o += ld) what(j, o);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) what(j, (t + j < tokens ? t + j : tokens - 1) * ld + col);
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void load(const T *p, int64_t ld, Raw4<T> (&v)[kRun]) const
+    {
+        if (channels >= kOwn) {
+            rows(ld, at, [&](int j, int64_t o) { v[j].load(p + o); });
+        } else {
+            rows(ld, 0, [&](int j, int64_t o) {
+                T w[16 / sizeof(T)] = {};
+#pragma unroll
+                for (int k = 0; k < kOwn; ++k)
+                    if (c + k < channels) w[k] = p[o + c + k];
+                __builtin_memcpy(&v[j], w, sizeof v[j]);
+            });
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void settle(Raw4<T> (&v)[kRun], int64_t c0) const
+    {
+        if (c0 + kCh <= channels || channels < kOwn) return;
+        const int64_t d = c - at;
+        const int s = d < kOwn ? (int)d : kOwn;
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) v[j].move(s);
+    }
+};
 template <typename T>
 __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn])
 {
@@ -150,17 +185,14 @@ __device__ __forceinline__ void load_state(const float *a, int64_t s, int64_t ch
 }
 
 // ---- sequences ---------------------------------------------------------------------------------
-template <int W>
 struct BlockMap {
-    int first[W * kWaveTokens], last[W * kWaveTokens];   // the sequence of which a token is the first or last, or -1
+    int first[kBlock], last[kBlock];       // the sequence of which a token is the first or last, or -1
     int some;                              // some token is either, or outside
 };
 struct Range { int64_t begin, end; };      // tokens inside sequences
 
-template <int W>
-__device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockMap<W> &m)
+__device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockMap &m)
 {
-    constexpr int kBlock = W * kWaveTokens, kThreads = W * kWave;
     for (int i = threadIdx.x; i < kBlock; i += kThreads) m.first[i] = m.last[i] = -1;
     if (threadIdx.x == 0) m.some = 0;
     __syncthreads();
@@ -186,32 +218,32 @@ __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockM
 }
 
 // Empty sequences hand on what they are given.
-template <int W>
 __device__ __forceinline__ void pass_on(const ScanArgs &p, int64_t blk, int64_t c0, const float *from, float *to)
 {
     if (!to || !p.seq_start) return;
     const int64_t c = c0 + (threadIdx.x & 63);
-    for (int64_t s = blk * W + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * W)
+    for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
         if (p.seq_start[s] >= p.seq_start[s + 1] && c < p.channels)
             to[s * p.channels + c] = from ? from[s * p.channels + c] : 0.0f;
 }
 
 // ---- joining runs ------------------------------------------------------------------------------
-template <int W>
+typedef float2 WavePairs[kWaves][kCh];
 struct ScanShared {
-    BlockMap<W> map;
-    float2 waves[W][kCh];             // pairs of the waves, later of the blocks before
-    float2 total[kCh];
+    BlockMap map;
+    WavePairs left, right;                 // pairs of the waves in either direction, then of those before
+    WavePairs blocks;                      // pairs of the blocks before, a few to each wave
     float carry[kCh];
     uint32_t ticket;
 };
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
-// A, B: in, the pair of each thread's run; out, that of all runs before it in the block (REVERSE: behind it).  sh.total gets
-// the whole block's.
-template <bool REVERSE, bool SOME, int W>
-__device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], ScanShared<W> &sh)
+// A, B: in, the pair of each thread's run; out, that of the runs of its wave before it (REVERSE: behind it).  The wave's pair
+// goes to `waves`.
+template <bool REVERSE, bool SOME>
+__device__ __forceinline__ void wave_scan(float (&A)[kOwn], float (&B)[kOwn], WavePairs &waves)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cl = lane & (kLanes - 1);
+    const int lane = threadIdx.x & 63, cl = lane & (kLanes - 1);
     const int pos = REVERSE ? kRows - 1 - lane / kLanes : lane / kLanes;
     auto before = [&](float v, int s) { return __shfl(v, (REVERSE ? lane + kLanes * s : lane - kLanes * s) & 63, 64); };
 #pragma unroll
@@ -222,32 +254,44 @@ __device__ __forceinline__ void block_scan(float (&A)[kOwn], float (&B)[kOwn], S
             B[k] = pos >= s ? join<SOME>(A[k], pb, B[k]) : B[k];
             A[k] = pos >= s ? times<SOME>(A[k], pa) : A[k];
         }
-    __syncthreads();                       // (whatever was read from sh before)
     if (pos == kRows - 1)
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k) sh.waves[wave][cl * kOwn + k] = float2{A[k], B[k]};
+        for (int k = 0; k < kOwn; ++k) waves[wave_id()][cl * kOwn + k] = float2{A[k], B[k]};
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {       // of the runs before this one
+    for (int k = 0; k < kOwn; ++k) {
         const float pa = before(A[k], 1), pb = before(B[k], 1);
         A[k] = pos == 0 ? 1.0f : pa;
         B[k] = pos == 0 ? 0.0f : pb;
     }
-    __syncthreads();
+}
+// By one wave, a channel to each lane: the waves' pairs become those of all waves before; returns the whole block's.
+template <bool REVERSE, bool SOME>
+__device__ __forceinline__ float2 block_prefix(WavePairs &waves)
+{
+    const int lane = threadIdx.x & 63;
+    float2 p[kWaves];
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) p[i] = waves[i][lane];
+    float a = 1.0f, b = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        const int w = REVERSE ? kWaves - 1 - i : i;
+        waves[w][lane] = float2{a, b};
+        b = join<SOME>(p[w].x, b, p[w].y);
+        a = times<SOME>(p[w].x, a);
+    }
+    return float2{SOME ? a : __builtin_fmaxf(a, kTiny), b};
+}
+// The state that enters the thread's run, in A's place, from the one that enters the block.
+template <bool SOME>
+__device__ __forceinline__ void enter(const float (&A)[kOwn], const float (&B)[kOwn], const WavePairs &waves,
+                                      const float (&block)[kOwn], float (&h)[kOwn])
+{
+    const int cl = threadIdx.x & (kLanes - 1), wave = wave_id();
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
-        float wa = 1.0f, wb = 0.0f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int w = REVERSE ? W - 1 - i : i;
-            const float2 p = sh.waves[w][cl * kOwn + k];
-            if (w == wave) {               // (uniform over a wave)
-                B[k] = join<SOME>(A[k], wb, B[k]);
-                A[k] = times<SOME>(A[k], wa);
-            }
-            wb = join<SOME>(p.x, wb, p.y);
-            wa = times<SOME>(p.x, wa);
-        }
-        if (threadIdx.x < kLanes) sh.total[cl * kOwn + k] = float2{SOME ? wa : __builtin_fmaxf(wa, kTiny), wb};
+        const float2 w = waves[wave][cl * kOwn + k];
+        h[k] = join<SOME>(A[k], join<SOME>(w.x, block[k], w.y), B[k]);
     }
 }
 
@@ -264,25 +308,29 @@ __device__ __forceinline__ uint64_t await(const uint64_t *p)
     return w == kAbsent ? word(0.0f, __builtin_nanf("")) : w;
 }
 
-// The state that enters block `k` of the chain (k counts in the direction of the scan; at(k) is the block), in sh.carry, from
-// sh.total; the block's own pair, and the state behind it where one is due, are published.
-template <bool REVERSE, int W>
-__device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared<W> &sh)
+// From the waves' pairs to the state that enters block `k` of the chain (k counts in the direction of the scan), in sh.carry; the
+// block's own pair, and the state behind it where one is due, are published.  `other` is what a second wave does meanwhile.
+template <bool REVERSE, typename Other>
+__device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared &sh, WavePairs &waves, Other other)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_id();
     const int64_t c = c0 + lane;
     const bool live = c < p.channels;
-    __syncthreads();                       // sh.total is there, sh.waves free
     auto at = [&](int64_t i) { return (REVERSE ? p.blocks - 1 - i : i) * p.channels + c; };
-    const float2 own = sh.total[lane];
-    if (wave == 0 && live && p.blocks > 1) store_dev(p.pairs + at(k), word(own.x, own.y));
-
-    // the pairs from the last multiple of kSuper on, a few of them to each wave
-    constexpr int kEach = kSuper / W;
+    // the pairs from the last multiple of kSuper on are asked for first, a few by each wave
+    constexpr int kEach = kSuper / kWaves;
     const int64_t base = k - k % kSuper, from = base + wave * kEach;
     uint64_t w[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) w[i] = from + i < k && live ? load_dev(p.pairs + at(from + i)) : word(1.0f, 0.0f);
+    __syncthreads();                       // the waves' pairs are there
+    float2 own{};
+    if (wave == 0) {
+        own = sh.map.some ? block_prefix<REVERSE, true>(waves) : block_prefix<REVERSE, false>(waves);
+        if (live && p.blocks > 1) store_dev(p.pairs + at(k), word(own.x, own.y));
+    } else if (wave == 1) {
+        other();
+    }
     float a = 1.0f, b = 0.0f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -291,12 +339,15 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
         b = join<true>(wa, b, wb);
         a = times<true>(wa, a);
     }
-    sh.waves[wave][lane] = float2{a, b};
+    sh.blocks[wave][lane] = float2{a, b};
     __syncthreads();
     if (wave == 0) {
+        float2 q[kWaves];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) q[i] = sh.blocks[i][lane];
         float h = base > 0 && live ? as_f32((uint32_t)await(p.supers + (base / kSuper - 1) * p.channels + c)) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) h = join<true>(sh.waves[i][lane].x, h, sh.waves[i][lane].y);
+        for (int i = 0; i < kWaves; ++i) h = join<true>(q[i].x, h, q[i].y);
         sh.carry[lane] = h;
         if (live && k % kSuper == kSuper - 1)
             store_dev(p.supers + k / kSuper * p.channels + c, word(0.0f, join<true>(own.x, h, own.y)));
@@ -307,8 +358,7 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
 // Which channels and which block a workgroup takes.  Workgroups go to the eight XCDs in turn; where there are enough channels,
 // two neighbouring groups of 64 stay on one XCD, since each writes half of a cache line of codes.
 struct Place { int64_t k, c0; };
-template <int W>
-__device__ __forceinline__ Place take(const ScanArgs &p, ScanShared<W> &sh)
+__device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
 {
     const uint32_t n = (uint32_t)p.groups, b = blockIdx.x;
     uint32_t g = b % n;
@@ -328,36 +378,67 @@ __global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, 
 }
 
 // ---- storing and reading the inputs ---------------------------------------------------------------
-// Two tokens (rows row, row + 1) of four columns; eight lanes hold a group's 32 columns.  A Philox block serves eight columns:
-// the two lanes that share them make that of one token each and exchange halves.
-__device__ __forceinline__ void encode_two(const float (&v)[2][kOwn], uint64_t seed, uint32_t epoch, int64_t row, uint32_t col8,
-                                           uint32_t stream, uint32_t (&codes)[2], uint32_t (&byte)[2])
+// The draws of two tokens (rows row, row + 1) of four columns, four halves each.  A Philox block serves eight columns: the two
+// lanes that share them make that of one token each and exchange words.
+__device__ __forceinline__ void draw_two(uint64_t seed, uint32_t epoch, int64_t row, uint32_t col8, uint32_t stream,
+                                         uint32_t (&w)[2][2])
 {
     const bool odd = threadIdx.x & 1;
     const Philox4 r = philox_block(seed, epoch, (uint64_t)(row + (odd ? 1 : 0)), col8, stream);
     const uint32_t x0 = dpp_move<0xB1>(odd ? r.w[0] : r.w[2]), x1 = dpp_move<0xB1>(odd ? r.w[1] : r.w[3]);
-    const uint32_t w[2][2] = {{odd ? x0 : r.w[0], odd ? x1 : r.w[1]}, {odd ? r.w[2] : x0, odd ? r.w[3] : x1}};
+    w[0][0] = odd ? x0 : r.w[0];
+    w[0][1] = odd ? x1 : r.w[1];
+    w[1][0] = odd ? r.w[2] : x0;
+    w[1][1] = odd ? r.w[3] : x1;
+}
+// Largest magnitudes of two tokens over a group's 32 columns (eight lanes), as fp32 bits.
+__device__ __forceinline__ void top_two(const Raw4<float> &v0, const Raw4<float> &v1, uint32_t (&top)[2])
+{
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            const uint32_t m = as_u32(v[t][k]) & 0x7FFFFFFFu;
-            top = top > m ? top : m;
-        }
-        uint32_t o = dpp_move<0xB1>(top);
-        top = top > o ? top : o;
-        o = dpp_move<0x4E>(top);
-        top = top > o ? top : o;
-        o = dpp_move<0x141>(top);
-        top = top > o ? top : o;
-        const ActStep s = act_step_of(top);
-        uint32_t c[kOwn];
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) c[k] = act_code(v[t][k], s.inverse, k & 1 ? w[t][k >> 1] >> 16 : w[t][k >> 1] & 0xFFFFu);
-        codes[t] = s.finite ? act_pack4(c) : 0u;
-        byte[t] = s.byte;
+        const u32x4 v = (t ? v1.w : v0.w) & 0x7FFFFFFFu;
+        uint32_t m = v[0] > v[1] ? v[0] : v[1];
+        const uint32_t n = v[2] > v[3] ? v[2] : v[3];
+        m = m > n ? m : n;
+        auto most = [&](uint32_t o) { m = m > o ? m : o; };
+        most(dpp_move<0xB1>(m));
+        most(dpp_move<0x4E>(m));
+        most(dpp_move<0x141>(m));
+        top[t] = m;
     }
+}
+__device__ __forceinline__ void top_two(const Raw4<__bf16> &v0, const Raw4<__bf16> &v1, uint32_t (&top)[2])
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    auto most = [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    };
+    const u32x2 a = v0.w & 0x7FFF7FFFu, b = v1.w & 0x7FFF7FFFu;
+    const uint32_t m = most(a[0], a[1]), n = most(b[0], b[1]);
+    // both tokens side by side: 0 in the low half, 1 in the high one
+    uint32_t r = most(__builtin_amdgcn_perm(n, m, 0x05040100u), __builtin_amdgcn_perm(n, m, 0x07060302u));
+    r = most(r, dpp_move<0xB1>(r));
+    r = most(r, dpp_move<0x4E>(r));
+    r = most(r, dpp_move<0x141>(r));
+    top[0] = r << 16;
+    top[1] = r & 0xFFFF0000u;
+}
+// Codes and step of four columns of a token.  CLAMP: the values are taken as clamped to +-kZMax (a NaN stays one).
+template <bool CLAMP, typename T>
+__device__ __forceinline__ void encode4(const Raw4<T> &v, uint32_t top, const uint32_t (&w)[2], uint32_t &codes, uint32_t &byte)
+{
+    bool finite = top < 0x7F800000u;
+    if (CLAMP) {
+        finite = top <= 0x7F800000u;
+        const uint32_t most = as_u32(kZMax);
+        top = top < most ? top : most;
+    }
+    const ActStep s = act_step_of(top);
+    float x[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) x[k] = CLAMP ? __builtin_amdgcn_fmed3f(v.of(k), -kZMax, kZMax) : v.of(k);
+    codes = finite ? act_codes4<T>(x, s, w[0], w[1], top) : 0u;
+    byte = finite ? s.byte : 255u;
 }
 __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[kOwn])
 {
@@ -367,81 +448,63 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 
 // ---- forward -----------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kForwardWaves * kWave, 4) void k_scan_forward(ScanArgs p)
+__global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 {
-    constexpr int W = kForwardWaves;
-    __shared__ ScanShared<W> sh;
+    __shared__ ScanShared sh;
     const Place at = take(p, sh);
-    const int64_t blk = at.k, t0 = blk * (W * kWaveTokens);
+    const int64_t blk = at.k, t0 = blk * kBlock;
     const int run = threadIdx.x / kLanes * kRun;                    // the first token of the thread's run, in the block
-    const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
-    const Columns cols(at.c0, c, p.channels);
+    const Part part(p, t0, at.c0);
+    const int64_t c = part.c;
 
-    float a[kRun][kOwn], b[kRun][kOwn];                             // z and x, later f and (1 - f) x
-    auto row = [&](int j) { return t0 + run + j < p.tokens ? t0 + run + j : p.tokens - 1; };
-    if (!cols.few) {
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            load4((const T *)p.x + row(j) * p.ldx, cols, b[j]);
-            load4((const T *)p.z + row(j) * p.ldz, cols, a[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            load_few((const T *)p.x + row(j) * p.ldx, cols, p.channels, b[j]);
-            load_few((const T *)p.z + row(j) * p.ldz, cols, p.channels, a[j]);
-        }
-    }
+    Raw4<T> x[kRun], z[kRun];
+    part.load((const T *)p.x, p.ldx, x);
+    part.load((const T *)p.z, p.ldz, z);
     const Range r = block_map(p, t0, sh.map);
+    part.settle(x, at.c0);
+    part.settle(z, at.c0);
 
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        settle(cols, b[j]);
-        settle(cols, a[j]);
-    }
-    if (p.wx) {
+    if (p.wx && c < p.lay.pitch) {
+        const int64_t o = part.t * p.lay.pitch + c, e = p.lay.steps + part.t * p.lay.groups + (c >> 5);
+        auto put = [&](uint8_t *a, int j, uint32_t codes, uint32_t byte) {
+            if (!part.whole && part.t + j >= p.tokens) return;
+            *reinterpret_cast<uint32_t *>(a + o + j * p.lay.pitch) = codes;
+            if ((threadIdx.x & 7) == 0) a[e + j * p.lay.groups] = (uint8_t)byte;
+        };
 #pragma unroll
         for (int j = 0; j < kRun; j += 2) {
-            float v[2][kOwn], z[2][kOwn];
+            uint32_t w[2][2], top[2], codes, byte;
+            draw_two(p.seed, p.epoch, part.t + j, (uint32_t)(c >> 3), p.stream, w);
+            top_two(x[j], x[j + 1], top);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+                encode4<false>(x[j + i], top[i], w[i], codes, byte);
+                put(p.wx, j + i, codes, byte);
+            }
+            draw_two(p.seed, p.epoch, part.t + j, (uint32_t)(c >> 3), p.stream + 1, w);
+            top_two(z[j], z[j + 1], top);
 #pragma unroll
-                for (int k = 0; k < kOwn; ++k) {
-                    const float q = a[j + i][k];
-                    v[i][k] = b[j + i][k];
-                    z[i][k] = q > kZMax ? kZMax : q < -kZMax ? -kZMax : q;
-                }
-            const int64_t t = t0 + run + j;
-            uint32_t cx[2], cz[2], ex[2], ez[2];
-            encode_two(v, p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream, cx, ex);
-            encode_two(z, p.seed, p.epoch, t, (uint32_t)(c >> 3), p.stream + 1, cz, ez);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (t + i < p.tokens && c < p.lay.pitch) {
-                    const int64_t o = (t + i) * p.lay.pitch + c;
-                    *reinterpret_cast<uint32_t *>(p.wx + o) = cx[i];
-                    *reinterpret_cast<uint32_t *>(p.wz + o) = cz[i];
-                    if ((threadIdx.x & 7) == 0) {
-                        const int64_t e = p.lay.steps + (t + i) * p.lay.groups + (c >> 5);
-                        p.wx[e] = (uint8_t)ex[i];
-                        p.wz[e] = (uint8_t)ez[i];
-                    }
-                }
+            for (int i = 0; i < 2; ++i) {
+                encode4<true>(z[j + i], top[i], w[i], codes, byte);
+                put(p.wz, j + i, codes, byte);
+            }
         }
     }
+    float a[kRun][kOwn], b[kRun][kOwn];                             // f and (1 - f) x
 #pragma unroll
     for (int j = 0; j < kRun; ++j)
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             float f, g;
-            gates(a[j][k], f, g);
+            gates(z[j].of(k), f, g);
             a[j][k] = f;
-            b[j][k] *= g;
+            b[j][k] = g * x[j].of(k);
         }
 
+    const bool some = sh.map.some;
     float A[kOwn], B[kOwn];
     uint32_t reset = 0;                                             // tokens that do not look back
-    if (!sh.map.some) {
+    if (!some) {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) { A[k] = a[0][k]; B[k] = b[0][k]; }
 #pragma unroll
@@ -451,13 +514,13 @@ __global__ __launch_bounds__(kForwardWaves * kWave, 4) void k_scan_forward(ScanA
                 B[k] = __builtin_fmaf(a[j][k], B[k], b[j][k]);
                 A[k] *= a[j][k];
             }
-        block_scan<false, false>(A, B, sh);
+        wave_scan<false, false>(A, B, sh.left);
     } else {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + run + j;
+            const int64_t t = part.t + j;
             const int s = sh.map.first[run + j];
             if (t < r.begin || t >= r.end) {
 #pragma unroll
@@ -480,78 +543,81 @@ __global__ __launch_bounds__(kForwardWaves * kWave, 4) void k_scan_forward(ScanA
         }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) A[k] = reset ? 0.0f : __builtin_fmaxf(A[k], kTiny);
-        block_scan<false, true>(A, B, sh);
+        wave_scan<false, true>(A, B, sh.left);
     }
-    chain<false>(p, at.k, at.c0, sh);
+    chain<false>(p, at.k, at.c0, sh, sh.left, [] {});
 
-    float h[kOwn];
+    float in[kOwn], h[kOwn];
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-        const float in = sh.carry[c - at.c0 + k];
-        h[k] = sh.map.some ? join<true>(A[k], in, B[k]) : join<false>(A[k], in, B[k]);
-    }
-    if (p.states && t0 % kBlock == 0 && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
-        p.states[t0 / kBlock * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
+    for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
+    if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
+        p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
+    if (!some) enter<false>(A, B, sh.left, in, h);
+    else enter<true>(A, B, sh.left, in, h);
+    T *y = (T *)p.y + part.t * p.ldy + c;
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + run + j;
+    for (int j = 0; j < kRun; ++j, y += p.ldy) {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) h[k] = reset >> j & 1 ? b[j][k] : __builtin_fmaf(a[j][k], h[k], b[j][k]);
-        if (t < p.tokens) store4<T>((T *)p.y + t * p.ldy + c, left, h);
-        if (p.h_last && sh.map.some && sh.map.last[run + j] >= 0)
-            store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, left, h);
+        if (part.whole || part.t + j < p.tokens) store4<T>(y, part.left(), h);
+        if (some && p.h_last && sh.map.last[run + j] >= 0)
+            store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, part.left(), h);
     }
-    pass_on<W>(p, blk, at.c0, p.h0, p.h_last);
+    pass_on(p, blk, at.c0, p.h0, p.h_last);
 }
 
 // ---- backward ----------------------------------------------------------------------------------
 // p_t = f_t d_t, d_t = dy_t + p_{t+1}, is a scan from right to left with the same factors as that of the states from left to
 // right; a run's pairs of both come from one walk: B of the right-to-left one is the sum of d_t times the product of the f
-// up to t.
+// up to t.  g = 1 - f waits in LDS, each thread's own in its place, so that two workgroups fit a compute unit.
+struct BackwardShared {
+    ScanShared s;
+    f32x4 g[kRun][kThreads];
+};
 template <typename T>
-__global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(ScanArgs p)
+__global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
 {
-    constexpr int W = kBackwardWaves;
-    __shared__ ScanShared<W> sh;
+    extern __shared__ __align__(16) char lds[];
+    BackwardShared &all = *reinterpret_cast<BackwardShared *>(lds);
+    ScanShared &sh = all.s;
     const Place at = take(p, sh);
     const int64_t blk = p.blocks - 1 - at.k, t0 = blk * kBlock;
     const int run = threadIdx.x / kLanes * kRun;
-    const int64_t c = at.c0 + (threadIdx.x & (kLanes - 1)) * kOwn, left = p.channels - c;
-    const Columns cols(at.c0, c, p.channels);
+    const Part part(p, t0, at.c0);
+    const int64_t c = part.c;
 
     uint32_t qx[kRun], ex[kRun];
-    float d[kRun][kOwn], f[kRun][kOwn], g[kRun][kOwn];
+    float f[kRun][kOwn];
+    Raw4<T> dy[kRun];
     {
         uint32_t qz[kRun], ez[kRun];
-        auto row = [&](int j) { return t0 + run + j < p.tokens ? t0 + run + j : p.tokens - 1; };
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            const int64_t t = row(j), cc = c < p.lay.pitch ? c : p.lay.pitch - kOwn;
-            const int64_t o = t * p.lay.pitch + cc, e = p.lay.steps + t * p.lay.groups + (cc >> 5);
+        const int64_t cc = c < p.lay.pitch ? c : p.lay.pitch - kOwn;
+        part.rows(p.lay.pitch, cc, [&](int j, int64_t o) {
             qz[j] = *reinterpret_cast<const uint32_t *>(p.rz + o);
-            ez[j] = p.rz[e];
             qx[j] = *reinterpret_cast<const uint32_t *>(p.rx + o);
-            ex[j] = p.rx[e];
-        }
-        if (!cols.few) {
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) load4((const T *)p.dy + row(j) * p.lddy, cols, d[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kRun; ++j) load_few((const T *)p.dy + row(j) * p.lddy, cols, p.channels, d[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) settle(cols, d[j]);
+        });
+        part.rows(p.lay.groups, p.lay.steps + (cc >> 5), [&](int j, int64_t o) {
+            ez[j] = p.rz[o];
+            ex[j] = p.rx[o];
+        });
+        part.load((const T *)p.dy, p.lddy, dy);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float z[kOwn];
+            f32x4 g;
             decode4(qz[j], act_step(ez[j]), z);
 #pragma unroll
-            for (int k = 0; k < kOwn; ++k) gates(z[k], f[j][k], g[j][k]);
+            for (int k = 0; k < kOwn; ++k) {
+                const float e = __expf(-z[k]);                      // |z| <= kZMax
+                f[j][k] = __builtin_amdgcn_rcpf(1.0f + e);
+                g[k] = e * f[j][k];
+            }
+            all.g[j][threadIdx.x] = g;
         }
     }
     const Range r = block_map(p, t0, sh.map);
     const bool some = sh.map.some;
+    part.settle(dy, at.c0);
 
     float A[kOwn], H[kOwn], AR[kOwn], P[kOwn];                      // pairs (A, H) from the left, (AR, P) from the right
     uint32_t outside = 0, first = 0, last = 0;                      // tokens, by bit
@@ -561,23 +627,26 @@ __global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(Sca
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float x[kOwn];
+            const f32x4 g = all.g[j][threadIdx.x];
             decode4(qx[j], act_step(ex[j]), x);
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
                 A[k] *= f[j][k];
-                H[k] = __builtin_fmaf(f[j][k], H[k], g[j][k] * x[k]);
-                P[k] = __builtin_fmaf(A[k], d[j][k], P[k]);
+                H[k] = __builtin_fmaf(f[j][k], H[k], g[k] * x[k]);
+                P[k] = __builtin_fmaf(A[k], dy[j].of(k), P[k]);
             }
         }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) AR[k] = A[k];
-        block_scan<true, false>(AR, P, sh);
+        wave_scan<false, false>(A, H, sh.left);
+        wave_scan<true, false>(AR, P, sh.right);
     } else {
         bool cut = false;                                           // a sequence has ended in this run
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
-            const int64_t t = t0 + run + j;
-            float x[kOwn];
+            const int64_t t = part.t + j;
+            float x[kOwn], d[kOwn];
+            const f32x4 g = all.g[j][threadIdx.x];
             decode4(qx[j], act_step(ex[j]), x);
             if (t < r.begin || t >= r.end) {
                 outside |= 1u << j;
@@ -586,12 +655,14 @@ __global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(Sca
                 for (int k = 0; k < kOwn; ++k) H[k] = 0.0f;
                 continue;
             }
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) d[k] = dy[j].of(k);
             if (sh.map.last[run + j] >= 0) {
                 last |= 1u << j;
                 float h[kOwn];
                 load_state(p.dh_last, sh.map.last[run + j], p.channels, c, h);
 #pragma unroll
-                for (int k = 0; k < kOwn; ++k) d[j][k] += h[k];
+                for (int k = 0; k < kOwn; ++k) d[k] += h[k];
             }
             if (sh.map.first[run + j] >= 0) {
                 first |= 1u << j;
@@ -600,8 +671,8 @@ __global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(Sca
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
                 A[k] *= f[j][k];
-                H[k] = __builtin_fmaf(f[j][k], H[k], g[j][k] * x[k]);
-                P[k] = cut ? P[k] : __builtin_fmaf(A[k], d[j][k], P[k]);
+                H[k] = __builtin_fmaf(f[j][k], H[k], g[k] * x[k]);
+                P[k] = cut ? P[k] : __builtin_fmaf(A[k], d[k], P[k]);
             }
             cut |= last >> j & 1;
         }
@@ -611,53 +682,59 @@ __global__ __launch_bounds__(kBackwardWaves * kWave, 2) void k_scan_backward(Sca
             A[k] = first | outside ? 0.0f : m;
             AR[k] = cut ? 0.0f : m;
         }
-        block_scan<true, true>(AR, P, sh);
+        wave_scan<false, true>(A, H, sh.left);
+        wave_scan<true, true>(AR, P, sh.right);
     }
-    chain<true>(p, at.k, at.c0, sh);
-    float q[kOwn];
-#pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-        const float in = sh.carry[c - at.c0 + k];
-        q[k] = some ? join<true>(AR[k], in, P[k]) : join<false>(AR[k], in, P[k]);
-    }
+    chain<true>(p, at.k, at.c0, sh, sh.right, [&] {
+        if (some) (void)block_prefix<false, true>(sh.left);
+        else (void)block_prefix<false, false>(sh.left);
+    });
 
-    // d becomes the gradient of each state
+    float in[kOwn], q[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
+    if (!some) enter<false>(AR, P, sh.right, in, q);
+    else enter<true>(AR, P, sh.right, in, q);
+    // the gradient of each state
+    float d[kRun][kOwn];
 #pragma unroll
     for (int j = kRun - 1; j >= 0; --j) {
+        float h[kOwn] = {};
+        if (last >> j & 1) load_state(p.dh_last, sh.map.last[run + j], p.channels, c, h);
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            d[j][k] = outside >> j & 1 ? 0.0f : last >> j & 1 ? d[j][k] : d[j][k] + q[k];
+            d[j][k] = outside >> j & 1 ? 0.0f : dy[j].of(k) + (last >> j & 1 ? h[k] : q[k]);
             q[k] = outside >> j & 1 ? 0.0f : f[j][k] * d[j][k];
         }
-        if (p.dh0 && first >> j & 1) store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, left, q);
+        if (p.dh0 && first >> j & 1)
+            store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, part.left(), q);
     }
 
     // the states again, from the one that the forward pass kept
-    if (!some) block_scan<false, false>(A, H, sh);
-    else block_scan<false, true>(A, H, sh);
     float h[kOwn];
-    load_state(p.states, blk, p.channels, c, h);
+    load_state(p.states, blk, p.channels, c, in);
+    if (!some) enter<false>(A, H, sh.left, in, h);
+    else enter<true>(A, H, sh.left, in, h);
+    T *px = (T *)p.dx + part.t * p.lddx + c, *pz = (T *)p.dz + part.t * p.lddz + c;
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) h[k] = some ? join<true>(A[k], h[k], H[k]) : join<false>(A[k], h[k], H[k]);
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        const int64_t t = t0 + run + j;
+    for (int j = 0; j < kRun; ++j, px += p.lddx, pz += p.lddz) {
         float x[kOwn], dx[kOwn], dz[kOwn];
+        const f32x4 g = all.g[j][threadIdx.x];
         decode4(qx[j], act_step(ex[j]), x);
         if (first >> j & 1) load_state(p.h0, sh.map.first[run + j], p.channels, c, h);
         const bool out = outside >> j & 1;
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            dx[k] = out ? 0.0f : g[j][k] * d[j][k];
+            dx[k] = out ? 0.0f : g[k] * d[j][k];
             dz[k] = out ? 0.0f : f[j][k] * dx[k] * (h[k] - x[k]);
-            h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[j][k] * x[k]);
+            h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[k] * x[k]);
         }
-        if (t < p.tokens) {
-            store4<T>((T *)p.dx + t * p.lddx + c, left, dx);
-            store4<T>((T *)p.dz + t * p.lddz + c, left, dz);
+        if (part.whole || part.t + j < p.tokens) {
+            store4<T>(px, part.left(), dx);
+            store4<T>(pz, part.left(), dz);
         }
     }
-    pass_on<W>(p, blk, at.c0, p.dh_last, p.dh0);
+    pass_on(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
 // One token of each of `rows` requests: the state in slot slots[row] (or row) of the pool is taken one step on.
@@ -688,25 +765,25 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
     store8(y + row * ldy + c, left, v);
 }
 
-static int64_t scan_blocks(int64_t tokens, int waves) { return (tokens + waves * kWaveTokens - 1) / (waves * kWaveTokens); }
+static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
 static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 {
-    return act_sizes_ok(tokens, channels) && scan_blocks(tokens, kForwardWaves) * ((channels + kCh - 1) / kCh) <= (1ll << 31) - 1;
+    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) <= (1ll << 31) - 1;
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
 // The chain's words behind one another in the workspace.
 struct ScanSpace { int64_t pairs, supers, groups; size_t bytes() const { return (size_t)(pairs + supers) * 8 + (size_t)groups * 4; } };
-static ScanSpace scan_space(int64_t tokens, int64_t channels, int waves)
+static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
-    const int64_t blocks = scan_blocks(tokens, waves);
+    const int64_t blocks = scan_blocks(tokens);
     if (blocks == 1) return ScanSpace{0, 0, 0};
     return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + kCh - 1) / kCh};
 }
-static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, int waves, void (*kernel)(ScanArgs))
+static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, void (*kernel)(ScanArgs))
 {
-    const ScanSpace w = scan_space(p.tokens, p.channels, waves);
-    p.blocks = scan_blocks(p.tokens, waves);
+    const ScanSpace w = scan_space(p.tokens, p.channels);
+    p.blocks = scan_blocks(p.tokens);
     p.pairs = (uint64_t *)workspace;
     p.supers = p.pairs + w.pairs;
     p.counters = (uint32_t *)(p.supers + w.supers);
@@ -715,7 +792,7 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, int waves, v
         hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
                            w.groups);
     }
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(waves * kWave), 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(kThreads), lds, s, p);
     return hip_check(hipGetLastError());
 }
 
@@ -726,8 +803,7 @@ using namespace zipml;
 extern "C" size_t zipml_scan_workspace_bytes(int64_t tokens, int64_t channels)
 {
     if (!scan_sizes_ok(tokens, channels)) return 0;
-    // (the forward pass has the more blocks)
-    const size_t b = scan_space(tokens, channels, kForwardWaves).bytes();
+    const size_t b = scan_space(tokens, channels).bytes();
     return b < 256 ? 256 : b;
 }
 
@@ -759,7 +835,7 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return scan_launch(s, p, workspace_dev, kForwardWaves, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
+    return scan_launch(s, p, workspace_dev, 0, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -789,7 +865,10 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return scan_launch(s, p, workspace_dev, kBackwardWaves, dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>);
+    const auto k = dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>;
+    if (HIP_FAILED(hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(BackwardShared))))
+        return ZIPML_ELAUNCH;
+    return scan_launch(s, p, workspace_dev, sizeof(BackwardShared), k);
 }
 
 template <typename T>
