@@ -109,17 +109,17 @@ template <> struct Raw4<float> {
 // branch of its own: a thread whose rows or columns are not all there reads the last ones that are, and `settle` moves columns
 // to their places.  Fewer than four columns in all are read one by one.
 struct Part {
-    int64_t t, c;          // first token and first column
     int64_t tokens, channels;
-    int64_t at;            // the column at which it reads
+    int64_t t;             // first token
+    int c, at;             // first column, and the column at which it reads
     bool whole;            // (for the workgroup) all rows are there
     __device__ __forceinline__ Part(const ScanArgs &p, int64_t t0, int64_t c0)
     {
         tokens = p.tokens;
         channels = p.channels;
         t = t0 + threadIdx.x / kLanes * kRun;
-        c = c0 + (threadIdx.x & (kLanes - 1)) * kOwn;
-        at = c <= channels - kOwn ? c : channels - kOwn;
+        c = (int)c0 + (threadIdx.x & (kLanes - 1)) * kOwn;
+        at = c <= channels - kOwn ? c : (int)channels - kOwn;
         whole = t0 + kBlock <= tokens;
     }
     __device__ __forceinline__ int64_t left() const { return channels - c; }
@@ -155,8 +155,7 @@ struct Part {
     __device__ __forceinline__ void settle(Raw4<T> (&v)[kRun], int64_t c0) const
     {
         if (c0 + kCh <= channels || channels < kOwn) return;
-        const int64_t d = c - at;
-        const int s = d < kOwn ? (int)d : kOwn;
+        const int s = c - at < kOwn ? c - at : kOwn;
 #pragma unroll
         for (int j = 0; j < kRun; ++j) v[j].move(s);
     }
@@ -455,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     const int64_t blk = at.k, t0 = blk * kBlock;
     const int run = threadIdx.x / kLanes * kRun;                    // the first token of the thread's run, in the block
     const Part part(p, t0, at.c0);
-    const int64_t c = part.c;
+    const int c = part.c;
 
     Raw4<T> x[kRun], z[kRun];
     part.load((const T *)p.x, p.ldx, x);
@@ -584,21 +583,22 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     const int64_t blk = p.blocks - 1 - at.k, t0 = blk * kBlock;
     const int run = threadIdx.x / kLanes * kRun;
     const Part part(p, t0, at.c0);
-    const int64_t c = part.c;
+    const int c = part.c;
 
-    uint32_t qx[kRun], ex[kRun];
+    uint32_t qx[kRun], ex[kRun / 4] = {};                             // codes, and the steps' bytes
+    auto step_x = [&](int j) { return act_step(ex[j >> 2] >> (8 * (j & 3)) & 255u); };
     float f[kRun][kOwn];
     Raw4<T> dy[kRun];
     {
-        uint32_t qz[kRun], ez[kRun];
-        const int64_t cc = c < p.lay.pitch ? c : p.lay.pitch - kOwn;
+        uint32_t qz[kRun], ez[kRun], eb[kRun];
+        const int cc = c < p.lay.pitch ? c : (int)p.lay.pitch - kOwn;
         part.rows(p.lay.pitch, cc, [&](int j, int64_t o) {
             qz[j] = *reinterpret_cast<const uint32_t *>(p.rz + o);
             qx[j] = *reinterpret_cast<const uint32_t *>(p.rx + o);
         });
         part.rows(p.lay.groups, p.lay.steps + (cc >> 5), [&](int j, int64_t o) {
             ez[j] = p.rz[o];
-            ex[j] = p.rx[o];
+            eb[j] = p.rx[o];
         });
         part.load((const T *)p.dy, p.lddy, dy);
 #pragma unroll
@@ -613,6 +613,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
                 g[k] = e * f[j][k];
             }
             all.g[j][threadIdx.x] = g;
+            ex[j >> 2] |= eb[j] << (8 * (j & 3));
         }
     }
     const Range r = block_map(p, t0, sh.map);
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         for (int j = 0; j < kRun; ++j) {
             float x[kOwn];
             const f32x4 g = all.g[j][threadIdx.x];
-            decode4(qx[j], act_step(ex[j]), x);
+            decode4(qx[j], step_x(j), x);
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
                 A[k] *= f[j][k];
@@ -647,7 +648,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             const int64_t t = part.t + j;
             float x[kOwn], d[kOwn];
             const f32x4 g = all.g[j][threadIdx.x];
-            decode4(qx[j], act_step(ex[j]), x);
+            decode4(qx[j], step_x(j), x);
             if (t < r.begin || t >= r.end) {
                 outside |= 1u << j;
                 cut = true;
@@ -697,6 +698,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     else enter<true>(AR, P, sh.right, in, q);
     // the gradient of each state
     float d[kRun][kOwn];
+    if constexpr (sizeof(T) == 2)
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(dy[j].w));
 #pragma unroll
     for (int j = kRun - 1; j >= 0; --j) {
         float h[kOwn] = {};
@@ -710,8 +714,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, part.left(), q);
     }
 
-    // the states again, from the one that the forward pass kept
+    // the states again, from the one that the forward pass kept (x decoded anew: kept from above it would not fit the registers)
     float h[kOwn];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(qx[j]));
     load_state(p.states, blk, p.channels, c, in);
     if (!some) enter<false>(A, H, sh.left, in, h);
     else enter<true>(A, H, sh.left, in, h);
@@ -720,7 +726,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     for (int j = 0; j < kRun; ++j, px += p.lddx, pz += p.lddz) {
         float x[kOwn], dx[kOwn], dz[kOwn];
         const f32x4 g = all.g[j][threadIdx.x];
-        decode4(qx[j], act_step(ex[j]), x);
+        decode4(qx[j], step_x(j), x);
         if (first >> j & 1) load_state(p.h0, sh.map.first[run + j], p.channels, c, h);
         const bool out = outside >> j & 1;
 #pragma unroll
