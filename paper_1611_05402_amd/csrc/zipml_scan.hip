@@ -234,7 +234,32 @@ struct ScanShared {
     WavePairs blocks;                      // pairs of the blocks before, a few to each wave
     float carry[kCh];
     uint32_t ticket;
+    __align__(8) uint8_t steps[2][kCh / kActGroup][kBlock];   // of x and z: the stored inputs' exponents
 };
+// The exponents of a block, between global memory (a token's side by side) and LDS (a group's side by side, so that a thread has
+// those of its run in one piece).  Each thread takes one token of x or z.
+__device__ __forceinline__ void steps_in(const ScanArgs &p, int64_t t0, int64_t c0, ScanShared &sh)
+{
+    const int which = threadIdx.x / kBlock, i = threadIdx.x % kBlock;
+    const int64_t t = t0 + i < p.tokens ? t0 + i : p.tokens - 1, g = c0 / kActGroup;
+    const uint8_t *a = (which ? p.rz : p.rx) + p.lay.steps + t * p.lay.groups + g;
+    uint8_t e[kCh / kActGroup];
+#pragma unroll
+    for (int k = 0; k < kCh / kActGroup; ++k) e[k] = a[g + k < p.lay.groups ? k : 0];
+#pragma unroll
+    for (int k = 0; k < kCh / kActGroup; ++k) sh.steps[which][k][i] = e[k];
+}
+__device__ __forceinline__ void steps_out(const ScanArgs &p, int64_t t0, int64_t c0, const ScanShared &sh)
+{
+    const int which = threadIdx.x / kBlock, i = threadIdx.x % kBlock;
+    const int64_t g = c0 / kActGroup;
+    if (t0 + i >= p.tokens) return;
+    uint8_t *a = (which ? p.wz : p.wx) + p.lay.steps + (t0 + i) * p.lay.groups + g;
+#pragma unroll
+    for (int k = 0; k < kCh / kActGroup; ++k)
+        if (g + k < p.lay.groups) a[k] = sh.steps[which][k][i];
+}
+static_assert(kThreads == 2 * kBlock && kRun == 8, "a thread for each token of x and z; eight exponents in one piece");
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
 // A, B: in, the pair of each thread's run; out, that of the runs of its wave before it (REVERSE: behind it).  The wave's pair
@@ -464,11 +489,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     part.settle(z, at.c0);
 
     if (p.wx && c < p.lay.pitch) {
-        const int64_t o = part.t * p.lay.pitch + c, e = p.lay.steps + part.t * p.lay.groups + (c >> 5);
-        auto put = [&](uint8_t *a, int j, uint32_t codes, uint32_t byte) {
-            if (!part.whole && part.t + j >= p.tokens) return;
-            *reinterpret_cast<uint32_t *>(a + o + j * p.lay.pitch) = codes;
-            if ((threadIdx.x & 7) == 0) a[e + j * p.lay.groups] = (uint8_t)byte;
+        const int64_t o = part.t * p.lay.pitch + c;
+        uint32_t e[2][kRun / 4] = {};                               // steps of x and z, a byte a token
+        auto put = [&](uint8_t *a, int which, int j, uint32_t codes, uint32_t byte) {
+            e[which][j >> 2] |= byte << (8 * (j & 3));
+            if (part.whole || part.t + j < p.tokens) *reinterpret_cast<uint32_t *>(a + o + j * p.lay.pitch) = codes;
         };
 #pragma unroll
         for (int j = 0; j < kRun; j += 2) {
@@ -478,16 +503,20 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 encode4<false>(x[j + i], top[i], w[i], codes, byte);
-                put(p.wx, j + i, codes, byte);
+                put(p.wx, 0, j + i, codes, byte);
             }
             draw_two(p.seed, p.epoch, part.t + j, (uint32_t)(c >> 3), p.stream + 1, w);
             top_two(z[j], z[j + 1], top);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 encode4<true>(z[j + i], top[i], w[i], codes, byte);
-                put(p.wz, j + i, codes, byte);
+                put(p.wz, 1, j + i, codes, byte);
             }
         }
+        if (c % kActGroup == 0)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<u32x2 *>(&sh.steps[i][(c - (int)at.c0) / kActGroup][run]) = u32x2{e[i][0], e[i][1]};
     }
     float a[kRun][kOwn], b[kRun][kOwn];                             // f and (1 - f) x
 #pragma unroll
@@ -549,6 +578,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     float in[kOwn], h[kOwn];
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
+    if (p.wx) steps_out(p, t0, at.c0, sh);
     if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
         p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
     if (!some) enter<false>(A, B, sh.left, in, h);
@@ -585,27 +615,30 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     const Part part(p, t0, at.c0);
     const int c = part.c;
 
-    uint32_t qx[kRun], ex[kRun / 4] = {};                             // codes, and the steps' bytes
+    uint32_t qx[kRun];
+    u32x2 ex;                                                       // the steps of x, a byte a token
+    Range r;
     auto step_x = [&](int j) { return act_step(ex[j >> 2] >> (8 * (j & 3)) & 255u); };
     float f[kRun][kOwn];
     Raw4<T> dy[kRun];
     {
-        uint32_t qz[kRun], ez[kRun], eb[kRun];
+        uint32_t qz[kRun];
         const int cc = c < p.lay.pitch ? c : (int)p.lay.pitch - kOwn;
         part.rows(p.lay.pitch, cc, [&](int j, int64_t o) {
             qz[j] = *reinterpret_cast<const uint32_t *>(p.rz + o);
             qx[j] = *reinterpret_cast<const uint32_t *>(p.rx + o);
         });
-        part.rows(p.lay.groups, p.lay.steps + (cc >> 5), [&](int j, int64_t o) {
-            ez[j] = p.rz[o];
-            eb[j] = p.rx[o];
-        });
         part.load((const T *)p.dy, p.lddy, dy);
+        steps_in(p, t0, at.c0, sh);
+        r = block_map(p, t0, sh.map);
+        const int group = (c - (int)at.c0) / kActGroup;
+        const u32x2 ez = *reinterpret_cast<const u32x2 *>(&sh.steps[1][group][run]);
+        ex = *reinterpret_cast<const u32x2 *>(&sh.steps[0][group][run]);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float z[kOwn];
             f32x4 g;
-            decode4(qz[j], act_step(ez[j]), z);
+            decode4(qz[j], act_step(ez[j >> 2] >> (8 * (j & 3)) & 255u), z);
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
                 const float e = __expf(-z[k]);                      // |z| <= kZMax
@@ -613,10 +646,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
                 g[k] = e * f[j][k];
             }
             all.g[j][threadIdx.x] = g;
-            ex[j >> 2] |= eb[j] << (8 * (j & 3));
         }
     }
-    const Range r = block_map(p, t0, sh.map);
     const bool some = sh.map.some;
     part.settle(dy, at.c0);
 
