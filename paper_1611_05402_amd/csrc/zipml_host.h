@@ -121,4 +121,18 @@ inline int hip_check_at(hipError_t e, const char *file, int line)
 #define hip_check(e) hip_check_at((e), __FILE__, __LINE__)
 #define HIP_FAILED(e) (hip_check_at((e), __FILE__, __LINE__) != ZIPML_OK)
 
+// Lets a kernel use more than 64 KiB of LDS; asked of the runtime once for each device (`done`: bits, one variable for each
+// kernel).
+inline int allow_lds(const void *kernel, size_t bytes, std::atomic<uint64_t> &done)
+{
+    if (bytes <= 64 * 1024) return ZIPML_OK;
+    int device = 0;
+    if (HIP_FAILED(hipGetDevice(&device))) return ZIPML_ELAUNCH;
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return ZIPML_OK;
+    if (HIP_FAILED(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return ZIPML_ELAUNCH;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return ZIPML_OK;
+}
+
 }  // namespace zipml

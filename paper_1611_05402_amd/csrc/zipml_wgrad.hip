@@ -340,8 +340,8 @@ static int launch_wgrad(hipStream_t s, const WgradArgs &a, int splits)
     const int64_t es = sizeof(T);
     const bool wide = a.lddy * es % 4 == 0 && a.d_out * es % 4 == 0 && a.lddy * es < (1 << 24);
     auto k = wide ? k_act_wgrad<T, S, true> : k_act_wgrad<T, S, false>;
-    if (HIP_FAILED(hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * S::kStage)))
-        return ZIPML_ELAUNCH;
+    static std::atomic<uint64_t> done[2];
+    if (allow_lds((const void *)k, 2 * S::kStage, done[wide])) return ZIPML_ELAUNCH;
     hipLaunchKernelGGL(k, dim3(a.tiles_o * a.tiles_i * splits), dim3(S::kThreads), 2 * S::kStage, s, a);
     return hip_check(hipGetLastError());
 }
