@@ -127,7 +127,7 @@ struct Part {
     template <typename What>
     __device__ __forceinline__ void rows(int64_t ld, int64_t col, What what) const
     {
-        if (whole) {
+        if (__builtin_expect(whole, 1)) {
             int64_t o = t * ld + col;
 #pragma unroll
             for (int j = 0; j < kRun; ++j, o += ld) what(j, o);
@@ -139,7 +139,7 @@ struct Part {
     template <typename T>
     __device__ __forceinline__ void load(const T *p, int64_t ld, Raw4<T> (&v)[kRun]) const
     {
-        if (channels >= kOwn) {
+        if (__builtin_expect(channels >= kOwn, 1)) {
             rows(ld, at, [&](int j, int64_t o) { v[j].load(p + o); });
         } else {
             rows(ld, 0, [&](int j, int64_t o) {
@@ -165,7 +165,7 @@ __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn
 {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
-    if (left >= kOwn) {
+    if (__builtin_expect(left >= kOwn, 1)) {
         if constexpr (sizeof(T) == 2)
             *reinterpret_cast<bf16x4_any *>(p) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
         else
@@ -379,14 +379,14 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
     __syncthreads();
 }
 
-// Which channels and which block a workgroup takes.  Workgroups go to the eight XCDs in turn; where there are enough channels,
-// two neighbouring groups of 64 stay on one XCD, since each writes half of a cache line of codes.
+// Which channels and which block a workgroup takes.  Workgroups go to the eight XCDs in turn.  Each XCD gets every group of 64
+// channels in turn, not some of them always: rows lie a power of two apart more often than not, so that a group's 128 bytes of
+// all rows fall on one or two of an L2's sixteen channels.
 struct Place { int64_t k, c0; };
 __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
 {
-    const uint32_t n = (uint32_t)p.groups, b = blockIdx.x;
-    uint32_t g = b % n;
-    if (n % 16 == 0) g = (g & ~15u) | (g & 7) << 1 | (g >> 3 & 1);
+    const uint32_t n = (uint32_t)p.groups, b = blockIdx.x, even = (uint32_t)p.blocks / 8 * 8 * n;
+    const uint32_t g = (b < even ? b >> 3 : b - even) % n;
     if (p.blocks == 1) return Place{0, g * (int64_t)kCh};
     if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     const bool some = sh.map.some;
     float A[kOwn], B[kOwn];
     uint32_t reset = 0;                                             // tokens that do not look back
-    if (!some) {
+    if (__builtin_expect(!some, 1)) {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) { A[k] = a[0][k]; B[k] = b[0][k]; }
 #pragma unroll
@@ -581,17 +581,22 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     if (p.wx) steps_out(p, t0, at.c0, sh);
     if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
         p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
-    if (!some) enter<false>(A, B, sh.left, in, h);
-    else enter<true>(A, B, sh.left, in, h);
-    T *y = (T *)p.y + part.t * p.ldy + c;
+    auto walk = [&](auto flag) {
+        constexpr bool SOME = decltype(flag)::value;                // (a block with all its rows has it false)
+        enter<SOME>(A, B, sh.left, in, h);
+        T *y = (T *)p.y + part.t * p.ldy + c;
 #pragma unroll
-    for (int j = 0; j < kRun; ++j, y += p.ldy) {
+        for (int j = 0; j < kRun; ++j, y += p.ldy) {
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k) h[k] = reset >> j & 1 ? b[j][k] : __builtin_fmaf(a[j][k], h[k], b[j][k]);
-        if (part.whole || part.t + j < p.tokens) store4<T>(y, part.left(), h);
-        if (some && p.h_last && sh.map.last[run + j] >= 0)
-            store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, part.left(), h);
-    }
+            for (int k = 0; k < kOwn; ++k) h[k] = SOME && reset >> j & 1 ? b[j][k] : __builtin_fmaf(a[j][k], h[k], b[j][k]);
+            if (!SOME || part.t + j < p.tokens) store4<T>(y, part.left(), h);
+            __builtin_amdgcn_sched_barrier(0);
+            if (SOME && p.h_last && sh.map.last[run + j] >= 0)
+                store4<float>(p.h_last + (int64_t)sh.map.last[run + j] * p.channels + c, part.left(), h);
+        }
+    };
+    if (__builtin_expect(some, 0)) walk(std::true_type());
+    else walk(std::false_type());
     pass_on(p, blk, at.c0, p.h0, p.h_last);
 }
 
@@ -655,7 +660,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     uint32_t outside = 0, first = 0, last = 0;                      // tokens, by bit
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) { A[k] = 1.0f; H[k] = P[k] = 0.0f; }
-    if (!some) {
+    if (__builtin_expect(!some, 1)) {
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float x[kOwn];
@@ -722,55 +727,60 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         else (void)block_prefix<false, false>(sh.left);
     });
 
-    float in[kOwn], q[kOwn];
+    auto walk = [&](auto flag) {
+        constexpr bool SOME = decltype(flag)::value;                // (a block with all its rows has it false)
+        float in[kOwn], q[kOwn];
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
-    if (!some) enter<false>(AR, P, sh.right, in, q);
-    else enter<true>(AR, P, sh.right, in, q);
-    // the gradient of each state
-    float d[kRun][kOwn];
-    if constexpr (sizeof(T) == 2)
+        for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
+        enter<SOME>(AR, P, sh.right, in, q);
+        // the gradient of each state
+        float d[kRun][kOwn];
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(dy[j].w));
+        for (int j = kRun - 1; j >= 0; --j) {
+            float h[kOwn] = {};
+            if (SOME && last >> j & 1) load_state(p.dh_last, sh.map.last[run + j], p.channels, c, h);
 #pragma unroll
-    for (int j = kRun - 1; j >= 0; --j) {
-        float h[kOwn] = {};
-        if (last >> j & 1) load_state(p.dh_last, sh.map.last[run + j], p.channels, c, h);
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            d[j][k] = outside >> j & 1 ? 0.0f : dy[j].of(k) + (last >> j & 1 ? h[k] : q[k]);
-            q[k] = outside >> j & 1 ? 0.0f : f[j][k] * d[j][k];
+            for (int k = 0; k < kOwn; ++k) {
+                d[j][k] = dy[j].of(k) + (SOME && last >> j & 1 ? h[k] : q[k]);
+                if (SOME && outside >> j & 1) d[j][k] = 0.0f;
+                q[k] = SOME && outside >> j & 1 ? 0.0f : f[j][k] * d[j][k];
+            }
+            if (SOME && p.dh0 && first >> j & 1)
+                store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, part.left(), q);
         }
-        if (p.dh0 && first >> j & 1)
-            store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, part.left(), q);
+        // the states again, from the one that the forward pass kept (x decoded anew: kept from above it would not fit the
+        // registers)
+        float h[kOwn];
+        load_state(p.states, blk, p.channels, c, in);
+        enter<SOME>(A, H, sh.left, in, h);
+        T *px = (T *)p.dx + part.t * p.lddx + c, *pz = (T *)p.dz + part.t * p.lddz + c;
+#pragma unroll
+        for (int j = 0; j < kRun; ++j, px += p.lddx, pz += p.lddz) {
+            float x[kOwn], dx[kOwn], dz[kOwn];
+            const f32x4 g = all.g[j][threadIdx.x];
+            decode4(qx[j], step_x(j), x);
+            if (SOME && first >> j & 1) load_state(p.h0, sh.map.first[run + j], p.channels, c, h);
+            const bool out = SOME && outside >> j & 1;
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                dx[k] = out ? 0.0f : g[k] * d[j][k];
+                dz[k] = out ? 0.0f : f[j][k] * dx[k] * (h[k] - x[k]);
+                h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[k] * x[k]);
+            }
+            if (!SOME || part.t + j < p.tokens) {
+                store4<T>(px, part.left(), dx);
+                store4<T>(pz, part.left(), dz);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+        __asm__ volatile("" : "+v"(qx[j]));
+        if constexpr (sizeof(T) == 2) __asm__ volatile("" : "+v"(dy[j].w));
     }
-
-    // the states again, from the one that the forward pass kept (x decoded anew: kept from above it would not fit the registers)
-    float h[kOwn];
-#pragma unroll
-    for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(qx[j]));
-    load_state(p.states, blk, p.channels, c, in);
-    if (!some) enter<false>(A, H, sh.left, in, h);
-    else enter<true>(A, H, sh.left, in, h);
-    T *px = (T *)p.dx + part.t * p.lddx + c, *pz = (T *)p.dz + part.t * p.lddz + c;
-#pragma unroll
-    for (int j = 0; j < kRun; ++j, px += p.lddx, pz += p.lddz) {
-        float x[kOwn], dx[kOwn], dz[kOwn];
-        const f32x4 g = all.g[j][threadIdx.x];
-        decode4(qx[j], step_x(j), x);
-        if (first >> j & 1) load_state(p.h0, sh.map.first[run + j], p.channels, c, h);
-        const bool out = outside >> j & 1;
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
-            dx[k] = out ? 0.0f : g[k] * d[j][k];
-            dz[k] = out ? 0.0f : f[j][k] * dx[k] * (h[k] - x[k]);
-            h[k] = out ? 0.0f : __builtin_fmaf(f[j][k], h[k], g[k] * x[k]);
-        }
-        if (part.whole || part.t + j < p.tokens) {
-            store4<T>(px, part.left(), dx);
-            store4<T>(pz, part.left(), dz);
-        }
-    }
+    if (__builtin_expect(some, 0)) walk(std::true_type());
+    else walk(std::false_type());
     pass_on(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
@@ -903,8 +913,8 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
     const auto k = dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>;
-    if (HIP_FAILED(hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(BackwardShared))))
-        return ZIPML_ELAUNCH;
+    static std::atomic<uint64_t> done[2];
+    if (allow_lds((const void *)k, sizeof(BackwardShared), done[dtype == ZIPML_F32])) return ZIPML_ELAUNCH;
     return scan_launch(s, p, workspace_dev, sizeof(BackwardShared), k);
 }
 
