@@ -50,7 +50,8 @@ struct ScanArgs {
     float *h_last, *dh0;
     uint64_t *pairs;                       // [blocks][channels], then
     uint64_t *supers;                      // [blocks / kSuper][channels], then
-    uint32_t *counters;                    // [groups]
+    uint32_t *counters;                    // [groups], side by side: a line to each has blocks start more evenly, and phases of
+                                           // neighbours then coincide (2 % slower at 32,768 tokens x 2,048 channels)
     uint64_t seed;
     uint32_t epoch, stream;
     int64_t tokens, channels, n_seq, blocks, groups;
@@ -393,12 +394,13 @@ __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
     return Place{sh.ticket, g * (int64_t)kCh};
 }
 
-// The words and counters of a chain before it starts.
+// The words (an even number of them) and counters of a chain before it starts.
 __global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, uint32_t *counters, int64_t groups)
 {
-    const int64_t step = (int64_t)gridDim.x * 256;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += step) words[i] = kAbsent;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups; i += step) counters[i] = 0;
+    const int64_t step = (int64_t)gridDim.x * 256, i0 = blockIdx.x * 256ll + threadIdx.x;
+    u32x4 *w = reinterpret_cast<u32x4 *>(words);
+    for (int64_t i = i0; i < n / 2; i += step) w[i] = u32x4{~0u, ~0u, ~0u, ~0u};
+    for (int64_t i = i0; i < groups; i += step) counters[i] = 0;
 }
 
 // ---- storing and reading the inputs ---------------------------------------------------------------
@@ -820,7 +822,11 @@ static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
 // The chain's words behind one another in the workspace.
-struct ScanSpace { int64_t pairs, supers, groups; size_t bytes() const { return (size_t)(pairs + supers) * 8 + (size_t)groups * 4; } };
+struct ScanSpace {
+    int64_t pairs, supers, groups;
+    int64_t words() const { return (pairs + supers + 1) / 2 * 2; }
+    size_t bytes() const { return (size_t)words() * 8 + (size_t)groups * 4; }
+};
 static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
     const int64_t blocks = scan_blocks(tokens);
@@ -833,9 +839,9 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, 
     p.blocks = scan_blocks(p.tokens);
     p.pairs = (uint64_t *)workspace;
     p.supers = p.pairs + w.pairs;
-    p.counters = (uint32_t *)(p.supers + w.supers);
+    p.counters = (uint32_t *)(p.pairs + w.words());
     if (p.blocks > 1) {
-        const int64_t n = w.pairs + w.supers, blocks = (n + 1023) / 1024;
+        const int64_t n = w.words(), blocks = (n + 511) / 512;
         hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
                            w.groups);
     }

@@ -308,10 +308,15 @@ def unpack_codes(packed, copy, n, d, bits, codes_out, stream=None):
                                     _ptr(codes_out)), "zipml_unpack_codes")
 
 
+_DTYPES: dict = {}
+
+
 def _dtype(t) -> int:
     """ZIPML_F32 or ZIPML_BF16 for a tensor (or a torch dtype); the library refuses -1."""
-    import torch
-    return {torch.float32: F32, torch.bfloat16: BF16}.get(t if isinstance(t, torch.dtype) else t.dtype, -1)
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    return _DTYPES.get(getattr(t, "dtype", t), -1)
 
 
 def act_bytes(rows: int, cols: int) -> int:
@@ -345,9 +350,9 @@ def scan_workspace_bytes(tokens: int, channels: int) -> int:
     return int(lib().zipml_scan_workspace_bytes(tokens, channels))
 
 
-def _same_dtype(*tensors) -> int:
+def _same_dtype(a, b, c) -> int:
     """The common type of x, z and y (or of the gradients); -1, which the library refuses, if they differ."""
-    return _dtype(tensors[0]) if all(t.dtype == tensors[0].dtype for t in tensors) else -1
+    return _dtype(a) if a.dtype == b.dtype == c.dtype else -1
 
 
 def scan_forward(x, ldx, z, ldz, tokens, channels, y, ldy, workspace, *, seq_start=None, n_seq=1, h0=None, h_last=None,
