@@ -191,6 +191,20 @@ struct BlockMap {
 };
 struct Range { int64_t begin, end; };      // tokens inside sequences
 
+// With many sequences the one that holds the block's first token is searched for, kThreads probes at a time; the offsets
+// from it on are looked at up to the block's end.
+constexpr int64_t kManySeqs = 4 * kThreads;
+__device__ __forceinline__ int64_t first_seq(const ScanArgs &a, int64_t t0)
+{
+    int64_t lo = 0, hi = a.n_seq;          // the last s in [lo, hi) with seq_start[s] <= t0, or 0
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + kThreads - 1) / kThreads, at = lo + threadIdx.x * step;
+        const int n = __syncthreads_count(at < hi && a.seq_start[at] <= t0);
+        lo += n > 0 ? (n - 1) * step : 0;
+        hi = n > 0 && lo + step < hi ? lo + step : n > 0 ? hi : lo + 1;
+    }
+    return lo;
+}
 __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockMap &m)
 {
     for (int i = threadIdx.x; i < kBlock; i += kThreads) m.first[i] = m.last[i] = -1;
@@ -208,7 +222,12 @@ __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockM
         if (q > t0 && q <= t0 + kBlock) { m.last[q - 1 - t0] = (int)s; m.some = 1; }
     };
     if (a.seq_start) {
-        for (int64_t s = threadIdx.x; s < a.n_seq; s += kThreads) mark(s, a.seq_start[s], a.seq_start[s + 1]);
+        const int64_t from = __builtin_expect(a.n_seq > kManySeqs, 0) ? first_seq(a, t0) : 0;
+        for (int64_t s = from + threadIdx.x; s < a.n_seq; s += kThreads) {
+            const int64_t p = a.seq_start[s], q = a.seq_start[s + 1];
+            mark(s, p, q);
+            if (p >= t0 + kBlock) break;
+        }
     } else if (threadIdx.x == 0) {
         mark(0, 0, a.tokens);
     }
@@ -817,7 +836,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
 static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
 static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 {
-    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) <= (1ll << 31) - 1;
+    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) < (1ll << 32) / kThreads;
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
 
@@ -939,7 +958,7 @@ extern "C" int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, con
                                void *y_dev, int64_t ldy)
 {
     if (!x_dev || !z_dev || !h_dev || !y_dev || !valid_dtype(dtype) || !act_sizes_ok(rows, channels)) return ZIPML_EINVAL;
-    if (rows > (1ll << 38) / channels) return ZIPML_EINVAL;
+    if (rows > ((1ll << 32) - 256) / ((channels + 7) / 8)) return ZIPML_EINVAL;   // threads of a launch
     if (!stride_ok(ldx, rows, channels) || !stride_ok(ldz, rows, channels) || !stride_ok(ldy, rows, channels))
         return ZIPML_EINVAL;
     if (n_slots < 1 || n_slots > (1ll << 60) / channels || (!slots_dev && n_slots < rows)) return ZIPML_EINVAL;

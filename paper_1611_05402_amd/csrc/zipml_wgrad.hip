@@ -318,7 +318,8 @@ static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype
     double least = 0;
     for (const auto &c : shapes[dtype == ZIPML_F32]) {
         const int64_t to = (d_out + c.tile - 1) / c.tile, ti = (d_in + c.tile - 1) / c.tile;
-        for (int64_t s = 1; s <= 256 && (s == 1 || (s - 1) * 128 < rows); s *= 2) {
+        // (ranges only where dW is at most 2^16 tiles, so that the partial sums can be counted in 32 bits)
+        for (int64_t s = 1; s <= 256 && (s == 1 || ((s - 1) * 128 < rows && to * ti <= 1 << 16)); s *= 2) {
             const int64_t rows_split = round_up((rows + s - 1) / s, 64), splits = (rows + rows_split - 1) / rows_split;
             const double k = (double)((to * ti * splits + 255) / 256), rounds = (double)((rows_split + round - 1) / round);
             const double us = 5.0 + rounds * (k > 1 ? k * c.shared : c.lone) +
@@ -361,7 +362,7 @@ using namespace zipml;
 static bool wgrad_sizes_ok(int64_t rows, int64_t d_out, int64_t d_in)
 {
     return act_sizes_ok(rows, d_in) && d_out > 0 && d_out <= (1 << 24) && d_in <= (1 << 24) &&
-           ((d_out + 63) / 64) * ((d_in + 63) / 64) <= (1ll << 30);
+           d_out <= (1ll << 37) / d_in;
 }
 
 extern "C" size_t zipml_act_wgrad_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in, int dtype)

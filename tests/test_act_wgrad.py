@@ -78,6 +78,16 @@ def test_large_layers(kind, rows, d_out, d_in):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d_out,d_in", [(2500, 520, 390), (700, 1030, 900), (6000, 260, 700), (20000, 130, 250),
+                                             (1990, 2100, 1500), (40000, 500, 256)])
+def test_middle_sizes(kind, rows, d_out, d_in):
+    """Where tiles of 128 and 256, in one range of tokens and in several, take over from each other."""
+    dy, codes, byte = inputs(rows, d_out, d_in, kind)
+    check(dy, codes, byte, d_in, wgrad(dy, codes, byte, d_in, 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,d_out,d_in", [(5, 9, 40), (3000, 100, 65)])
 def test_adding_to_what_is_there(kind, rows, d_out, d_in):
     dy, codes, byte = inputs(rows, d_out, d_in, kind)
@@ -150,7 +160,7 @@ def test_sizes(lib):
     f, b = torch.float32, torch.bfloat16
     assert zipml.act_wgrad_workspace_bytes(1, 1, 1, b) > 0
     assert zipml.act_wgrad_workspace_bytes(65536, 512, 256, b) >= 512 * 256 * 4
-    for rows, o, i in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, (1 << 24) + 1, 1), (1, 1, (1 << 24) + 1)):
+    for rows, o, i in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, (1 << 24) + 1, 1), (1, 1, (1 << 24) + 1), (1, 1 << 20, 1 << 20)):
         assert zipml.act_wgrad_workspace_bytes(rows, o, i, f) == 0
     assert zipml.act_wgrad_workspace_bytes(4, 4, 4, torch.float16) == 0
 

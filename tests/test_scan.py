@@ -153,9 +153,11 @@ def test_without_the_optional_arrays(tokens):
 
 
 @pytest.mark.gpu
-def test_many_sequences():
-    """More sequences than threads, of 0 to 7 tokens each."""
-    lengths = np.random.default_rng(2).integers(0, 8, 3000)
+@pytest.mark.parametrize("n", [600, 3000])
+def test_many_sequences(n):
+    """More sequences than threads, and so many that a block searches for its first, of 0 to 7 tokens each."""
+    lengths = np.random.default_rng(2).integers(0, 8, n)
+    lengths[n // 2:n // 2 + 90] = 0
     start = np.concatenate([[0], np.cumsum(lengths)])
     p = Problem(int(start[-1]), 20, start, "f32")
     y = p.forward(train=True)
@@ -403,7 +405,7 @@ def test_in_a_graph():
 def test_sizes(lib):
     assert zipml.scan_workspace_bytes(1, 1) > 0
     assert zipml.scan_workspace_bytes(100000, 64) >= (100000 // 256) * 64 * 8
-    for t, c in ((0, 1), (1, 0), (-1, 4), (1 << 41, 1), (1 << 40, 1 << 15)):
+    for t, c in ((0, 1), (1, 0), (-1, 4), (1 << 41, 1), (1 << 40, 1 << 15), (1 << 31, 64)):
         assert zipml.scan_workspace_bytes(t, c) == 0
 
 
@@ -435,7 +437,7 @@ def test_refusals(lib):
     def step(x=FAKE, ldx=40, z=FAKE, ldz=40, dtype=zipml.F32, rows=4, c=40, h=FAKE, n=8, slots=FAKE, y=FAKE, ldy=40):
         return lib.zipml_scan_step(None, x, ldx, z, ldz, dtype, rows, c, h, n, slots, y, ldy)
     for kw in ({"x": None}, {"z": None}, {"h": None}, {"y": None}, {"ldx": 39}, {"ldz": 39}, {"ldy": 39}, {"dtype": 2},
-               {"rows": 0}, {"c": 0}, {"n": 0}, {"slots": None, "n": 3}):
+               {"rows": 0}, {"c": 0}, {"n": 0}, {"slots": None, "n": 3}, {"rows": 1 << 32}):
         assert step(**kw) == zipml.EINVAL, kw
     for k in ("x", "z", "h", "slots", "y"):
         assert step(**{k: ODD}) == zipml.EALIGN, k
