@@ -24,15 +24,22 @@ __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, Act
         if (unit * 8 >= lay.pitch) continue;               // whole groups of four lanes
         const int64_t row0 = rb * (ny * kRows) + ty;
         float v[kRows][8];
+        // (where all is there the loads stand in no branch of their own, or each would wait for the one before)
+        const bool whole = (rb + 1) * (ny * kRows) <= lay.rows && (unit - tx + (1 << g.tx_log)) * 8 <= lay.cols;
+        if (__builtin_expect(whole, 1)) {
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
-            const int64_t row = row0 + q * ny;
-            load8(x + row * ldx + unit * 8, row < lay.rows ? lay.cols - unit * 8 : 0, v[q]);
+            for (int q = 0; q < kRows; ++q) load8(x + (row0 + q * ny) * ldx + unit * 8, 8, v[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kRows; ++q) {
+                const int64_t row = row0 + q * ny;
+                load8(x + row * ldx + unit * 8, row < lay.rows ? lay.cols - unit * 8 : 0, v[q]);
+            }
         }
 #pragma unroll
         for (int q = 0; q < kRows; ++q) {
             const int64_t row = row0 + q * ny;
-            if (row >= lay.rows) break;
+            if (!whole && row >= lay.rows) break;
             const ActCodes8 c = act_encode8<T>(v[q], seed, epoch, row, (uint32_t)unit, stream);
             *reinterpret_cast<u32x2 *>(act + row * lay.pitch + unit * 8) = c.codes;
             if ((unit & 3) == 0) act[lay.steps + row * lay.groups + (unit >> 2)] = (uint8_t)c.byte;

@@ -37,7 +37,7 @@ def encode(x, seed=0, epoch=0, tag=0):
     e = np.maximum(e, -126)
     step = np.exp2(e.astype(float))[..., None]
     k = draws(rows, wide, seed, epoch, tag).reshape(g.shape)
-    with np.errstate(invalid="ignore"):
+    with np.errstate(invalid="ignore", over="ignore"):
         # the sum is rounded to fp32, as the definition has it
         t = ((g / step).astype(np.float32) + ((k + 0.5) / 65536.0).astype(np.float32)).astype(np.float32)
         codes = np.where(bad[..., None], 0.0, np.floor(t))
