@@ -44,6 +44,9 @@ struct WgradShape {
     static constexpr int kLoadsA = BK * MT / 8 / kThreads;        // eight dY values each
     static constexpr int kLoadsB = BK * NT / 8 / kThreads;        // eight codes each
     static constexpr int kSteps = BK / 16 * kPlanes;              // steps of a product: sixteen tokens, one term
+    // Whether a step's reads, stores and products stay in this order; otherwise the compiler mixes them.  Measured: in order 4 to 10 %
+    // faster with fp32 dY and on tiles of 64, 4 to 8 % slower on the others.
+    static constexpr bool kInOrder = kPlanes == 3 || MT == 64;
     static constexpr int TM = MT / WM / 32, TN = NT / WN / 32;    // 32 x 32 tiles of a wave
     static_assert(kLoadsA * 8 * kThreads == BK * MT && kLoadsB * 8 * kThreads == BK * NT, "whole loads");
     static_assert(MT % 64 == 0 && NT % 64 == 0, "LDS rows");
@@ -134,13 +137,15 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
     const int64_t t_end = t_begin + a.rows_split < a.rows ? t_begin + a.rows_split : a.rows;
     const T *dy = (const T *)a.dy;
 
-    Raw8<T> va[S::kLoadsA];
-    u32x2 vb[S::kLoadsB];
-    uint32_t step[S::kLoadsB];
+    struct Tile {                          // a thread's part of one round
+        Raw8<T> va[S::kLoadsA];
+        u32x2 vb[S::kLoadsB];
+        uint32_t step[S::kLoadsB];
+    };
 
     // The loads and the stores of a tile are dealt over the steps of a round but the last.
     constexpr int kDeals = S::kSteps - 1;
-    auto load = [&](int64_t t0, int k) {
+    auto load = [&](Tile &tile, int64_t t0, int k) {
         const int64_t left = t_end - t0;
         const Rows ra(dy + t0 * a.lddy + o0, WIDE ? ((left - 1) * a.lddy + a.d_out - o0) * (int64_t)sizeof(T) : 0);
         const Rows rb(a.act + t0 * a.pitch + i0, left * a.pitch - i0);
@@ -151,37 +156,37 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
             const int c = tid + q * S::kThreads, r = c / (S::MT / 8), col = c % (S::MT / 8) * 8;
             if constexpr (WIDE) {
                 const int at = (r * (int)a.lddy + col) * (int)sizeof(T);
-                va[q].w = ra.load16(at);
-                if constexpr (sizeof(T) == 4) va[q].w2 = ra.load16(at + 16);
+                tile.va[q].w = ra.load16(at);
+                if constexpr (sizeof(T) == 4) tile.va[q].w2 = ra.load16(at + 16);
             } else {
                 const T *p = dy + (t0 + r) * a.lddy + o0 + col;
                 const int n = r < left ? a.d_out - o0 - col : 0;
                 T v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (T)0.0f;
-                va[q] = __builtin_bit_cast(Raw8<T>, v);
+                tile.va[q] = __builtin_bit_cast(Raw8<T>, v);
             }
         }
 #pragma unroll
         for (int q = 0; q < S::kLoadsB; ++q) {
             if (q * kDeals / S::kLoadsB != k) continue;
             const int c = tid + q * S::kThreads, r = c / (S::NT / 8), col = c % (S::NT / 8) * 8;
-            vb[q] = rb.load8(r * (int)a.pitch + col);
-            step[q] = rs.load1(r * (int)a.groups + (col >> 5));
+            tile.vb[q] = rb.load8(r * (int)a.pitch + col);
+            tile.step[q] = rs.load1(r * (int)a.groups + (col >> 5));
         }
     };
-    auto store = [&](char *stage, int k) {
+    auto store = [&](const Tile &tile, char *stage, int k) {
 #pragma unroll
         for (int q = 0; q < S::kLoadsA; ++q) {
             if (q * kDeals / S::kLoadsA != k) continue;
             const int c = tid + q * S::kThreads, r = c / (S::MT / 8), col = c % (S::MT / 8) * 8;
             char *p = stage + r * S::kRowA + col * 2;
             if constexpr (sizeof(T) == 2) {
-                *reinterpret_cast<u32x4 *>(p) = va[q].w;
+                *reinterpret_cast<u32x4 *>(p) = tile.va[q].w;
             } else {
                 uint32_t x[3][2], y[3][2];
-                split4(va[q].w, x);
-                split4(va[q].w2, y);
+                split4(tile.va[q].w, x);
+                split4(tile.va[q].w2, y);
 #pragma unroll
                 for (int t = 0; t < 3; ++t)
                     *reinterpret_cast<u32x4 *>(p + t * S::kBytesA) = u32x4{x[t][0], x[t][1], y[t][0], y[t][1]};
@@ -191,11 +196,11 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         for (int q = 0; q < S::kLoadsB; ++q) {
             if (q * kDeals / S::kLoadsB != k) continue;
             const int c = tid + q * S::kThreads, r = c / (S::NT / 8), col = c % (S::NT / 8) * 8;
-            const float s = act_step(step[q]);
+            const float s = act_step(tile.step[q]);
             u32x4 o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t w = vb[q][j >> 1];
+                const uint32_t w = tile.vb[q][j >> 1];
                 const float x = (float)(int8_t)(w >> (16 * (j & 1))) * s, y = (float)(int8_t)(w >> (16 * (j & 1) + 8)) * s;
                 o[j] = __builtin_amdgcn_perm(as_u32(y), as_u32(x), 0x07060302u);
             }
@@ -227,12 +232,23 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
     // compiler otherwise moves all loads to a round's end, where their latency shows (555 us in place of 460 for 16,384
     // tokens, 4,096 x 4,096, in the same arrangement).
     char *here = lds, *next = lds + S::kStage;
+    Tile tile;
+    if constexpr (S::MT < 256) {           // both rounds asked for at once: the memory's latency once, not twice
+        Tile first;
 #pragma unroll
-    for (int k = 0; k < kDeals; ++k) load(t_begin, k);
+        for (int k = 0; k < kDeals; ++k) load(first, t_begin, k);
 #pragma unroll
-    for (int k = 0; k < kDeals; ++k) {
-        store(here, k);
-        load(t_begin + S::BK, k);
+        for (int k = 0; k < kDeals; ++k) load(tile, t_begin + S::BK, k);
+#pragma unroll
+        for (int k = 0; k < kDeals; ++k) store(first, here, k);
+    } else {                               // (no registers for two; 1 % on the whole kernel)
+#pragma unroll
+        for (int k = 0; k < kDeals; ++k) load(tile, t_begin, k);
+#pragma unroll
+        for (int k = 0; k < kDeals; ++k) {
+            store(tile, here, k);
+            load(tile, t_begin + S::BK, k);
+        }
     }
     lds_barrier();
     read(here, 0);
@@ -241,12 +257,14 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         for (int s = 0; s < S::kSteps; ++s) {
             if (s < kDeals) {
                 read(here, s + 1);
-                store(next, s);
-                load(t0 + 2 * S::BK, s);
+                if (S::kInOrder) __builtin_amdgcn_sched_barrier(0);
+                store(tile, next, s);
+                load(tile, t0 + 2 * S::BK, s);
             } else {
                 lds_barrier();
                 read(next, 0);
             }
+            if (S::kInOrder) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int m = 0; m < S::TM; ++m)
 #pragma unroll
