@@ -28,6 +28,7 @@ struct WgradArgs {
     int64_t ldo, out_split;   // elements between rows of out, and between the partial sums
     int64_t rows_split;       // tokens of a range
     int d_out, d_in, tiles_o, tiles_i, add;
+    int last;                 // the last value of dY is left out of the loads and added at the end (see Rows)
 };
 
 // MT x NT is the tile of dW, BK the tokens of one round; WM x WN waves share the tile.
@@ -69,7 +70,8 @@ __device__ __forceinline__ bf16x8 fragment(const char *tile, int row_bytes)
 
 // Rows of a tile as a buffer: what lies behind its last value reads as zeros, so that neither the last tokens of a range
 // nor tiles beyond the layer's edge need a branch.  (A column beyond the edge reads the next row's values where there
-// is one: they reach only sums that are not kept.)
+// is one: they reach only sums that are not kept.)  The end is exact to a dword: of bf16 rows of an odd number of values
+// the very last value reads as zero, and its product is added to the sums at the end.
 struct Rows {
     __amdgpu_buffer_rsrc_t r;
     __device__ __forceinline__ Rows(const void *base, int64_t bytes)
@@ -277,6 +279,8 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         next = t;
     }
 
+    const bool last = a.last && t_end == a.rows && o0 + S::MT >= a.d_out;
+    const float last_dy = last ? (float)dy[(a.rows - 1) * a.lddy + a.d_out - 1] : 0.0f;
     float *out = a.out + split * a.out_split;
 #pragma unroll
     for (int m = 0; m < S::TM; ++m)
@@ -284,27 +288,41 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         for (int n = 0; n < S::TN; ++n) {
             const int i = i0 + (wn * S::TN + n) * 32 + (lane & 31);
             if (i >= a.d_in) continue;
+            float last_x = 0.0f;
+            if (last) {
+                const int64_t t = a.rows - 1;
+                last_x = (float)(int8_t)a.act[t * a.pitch + i] * act_step(a.act[a.steps + t * a.groups + (i >> 5)]);
+            }
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
                 const int o = o0 + (wm * S::TM + m) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
                 if (o >= a.d_out) continue;
+                if (last && o == a.d_out - 1) acc[m][n][q] = __builtin_fmaf(last_dy, last_x, acc[m][n][q]);
                 float *p = out + o * a.ldo + i;
                 *p = a.add ? *p + acc[m][n][q] : acc[m][n][q];
             }
         }
 }
 
-// Sum of the ranges' partial sums, in their order; a thread takes four neighbouring elements, the partial sums' rows being
-// multiples of 64.
+// Sum of the ranges' partial sums, in an order of their number alone: each of a workgroup's four waves takes a quarter of the
+// ranges, a lane four neighbouring elements, the partial sums' rows being multiples of 64.
 __global__ __launch_bounds__(256) void k_wgrad_sum(const float *__restrict__ part, int splits, int64_t out_split, int d_out,
                                                    int d_in, int64_t ld_part, float *__restrict__ dw, int64_t lddw, int add)
 {
-    const uint32_t units = (d_in + 3) / 4, u = blockIdx.x * 256u + threadIdx.x, o = u / units, i = (u - o * units) * 4;
-    if (o >= (uint32_t)d_out) return;
-    const float *p = part + o * ld_part + i;
+    __shared__ f32x4 quarter[3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t units = (d_in + 3) / 4, u = blockIdx.x * 64u + lane, o = u / units, i = (u - o * units) * 4;
+    const bool there = o < (uint32_t)d_out;
+    const float *p = part + (there ? o * ld_part + i : 0);
     f32x4 sum = {};
+    const int end = splits * (wave + 1) / 4;
 #pragma unroll 8
-    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * out_split);
+    for (int s = splits * wave / 4; s < end; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * out_split);
+    if (wave > 0) quarter[wave - 1][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || !there) return;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) sum += quarter[q][lane];
     float *w = dw + o * lddw + i;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -324,7 +342,8 @@ template <typename T> struct Shapes {
 //   start + rounds of a range * (one workgroup on a compute unit: lone, k of them: k * shared)
 //         + (ranges > 1: a launch, partial sums written and read),
 // with the times of a round measured on either side of each choice (us; 64 tokens of bf16 or 32 of fp32 dY):
-//   256: 1.4 to 1.8, fp32 2.6;  128: 0.68 to 0.85 alone, 0.65 each of two, fp32 1.0;  64: 0.5 alone, 0.37 each, fp32 0.65.
+//   256: 1.4 to 1.8, fp32 2.6;  128: 0.68 to 0.85 alone, 0.65 each of two, fp32 1.0 and 0.9;  64: 0.5 and 0.37, fp32 0.65 and 0.45.
+// Of 50 sizes and types timed in every shape and number of ranges 46 get the fastest, four are 3 to 6 % slower than it.
 // 4,096 tokens, 2,048 x 2,048, launches alone: 256 in 4 ranges 43 us + 67 MB of partial sums, 128 in one 53; 4,096 tokens,
 // 1,024 x 1,024: 256 in 16 ranges 23, 128 in 4 22, 64 in one 36; 256 tokens, 256 x 256: 128 in one 12, 64 in one 8.
 struct WgradPlan {
@@ -335,7 +354,7 @@ struct WgradPlan {
 static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype)
 {
     struct { int tile; double lone, shared; } const shapes[2][3] = {{{256, 1.6, 1.6}, {128, 0.8, 0.65}, {64, 0.5, 0.37}},
-                                                                    {{256, 2.6, 2.6}, {128, 1.0, 0.95}, {64, 0.65, 0.55}}};
+                                                                    {{256, 2.6, 2.6}, {128, 1.0, 0.9}, {64, 0.65, 0.45}}};
     const int64_t round = dtype == ZIPML_F32 ? 32 : 64;
     WgradPlan best{};
     double least = 0;
@@ -357,12 +376,11 @@ static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype
 }
 
 template <typename T, typename S>
-static int launch_wgrad(hipStream_t s, const WgradArgs &a, int splits)
+static int launch_wgrad(hipStream_t s, WgradArgs a, int splits)
 {
-    // 16 bytes at a time where rows start and end on whole dwords (a buffer's end is exact to a dword) and the offsets of a
-    // round fit 31 bits
-    const int64_t es = sizeof(T);
-    const bool wide = a.lddy * es % 4 == 0 && a.d_out * es % 4 == 0 && a.lddy * es < (1 << 24);
+    // 16 bytes at a time, at any alignment, where the offsets of a round fit 31 bits
+    const bool wide = a.lddy * (int64_t)sizeof(T) < (1 << 24);
+    a.last = wide && sizeof(T) == 2 && a.d_out % 2 == 1;
     auto k = wide ? k_act_wgrad<T, S, true> : k_act_wgrad<T, S, false>;
     static std::atomic<uint64_t> done[2];
     if (allow_lds((const void *)k, 2 * S::kStage, done[wide])) return ZIPML_ELAUNCH;
@@ -410,7 +428,7 @@ extern "C" int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int6
     hipStream_t s = entry_stream(stream);
     const int add = flags & ZIPML_WGRAD_ADD ? 1 : 0;
     WgradArgs a{dy_dev, (const uint8_t *)act_dev, dw_dev, lddy, rows, lay.pitch, lay.groups, lay.steps, lddw, 0,
-                p.rows_split, (int)d_out, (int)d_in, p.tiles_o, p.tiles_i, add};
+                p.rows_split, (int)d_out, (int)d_in, p.tiles_o, p.tiles_i, add, 0};
     if (p.splits > 1) {
         a.out = (float *)workspace_dev;
         a.ldo = (int64_t)p.tiles_i * p.tile;
@@ -419,7 +437,7 @@ extern "C" int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int6
     }
     const int rc = dtype == ZIPML_F32 ? launch_tile<float>(s, a, p) : launch_tile<__bf16>(s, a, p);
     if (rc || p.splits == 1) return rc;
-    const int64_t blocks = ((d_in + 3) / 4 * d_out + 255) / 256;
+    const int64_t blocks = ((d_in + 3) / 4 * d_out + 63) / 64;
     hipLaunchKernelGGL(k_wgrad_sum, dim3((uint32_t)blocks), dim3(256), 0, s, a.out, p.splits, a.out_split, (int)d_out,
                        (int)d_in, a.ldo, dw_dev, lddw, add);
     return hip_check(hipGetLastError());

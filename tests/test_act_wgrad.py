@@ -88,6 +88,26 @@ def test_middle_sizes(kind, rows, d_out, d_in):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("d_out", [5, 130])
+def test_rows_far_apart(kind, d_out):
+    """Rows of dY more than 16 MiB apart are read value by value."""
+    dy, codes, byte = inputs(3, d_out, 70, kind)
+    check(dy, codes, byte, 70, wgrad(dy, codes, byte, 70, (1 << 24) // dy.element_size() + 3))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,d_out", [(1, 1), (1, 63), (64, 65), (129, 255), (500, 129), (300, 4097)])
+def test_the_very_last_value_of_dy(rows, d_out):
+    """An odd number of bf16 values a row: the last value of the last row counts, and nothing behind it is read as one."""
+    dy, codes, byte = inputs(rows, d_out, 45, "bf16")
+    dy[-1, -1] = 3.0
+    codes[-1, :45] = 100
+    for pad in (0, 1, 2):
+        check(dy, codes, byte, 45, wgrad(dy, codes, byte, 45, pad))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,d_out,d_in", [(5, 9, 40), (3000, 100, 65)])
 def test_adding_to_what_is_there(kind, rows, d_out, d_in):
     dy, codes, byte = inputs(rows, d_out, d_in, kind)
