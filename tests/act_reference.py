@@ -15,16 +15,16 @@ def philox(row, col8, stream, seed, epoch):
     return c
 
 
-def draws(rows, wide, seed, epoch, tag):
-    """The 16-bit draw of every value of a rows x wide tensor (wide a multiple of 8)."""
-    row = np.repeat(np.arange(rows, dtype=U), wide // 8)
+def draws(rows, wide, seed, epoch, tag, row0=0):
+    """The 16-bit draw of every value of `rows` rows of a tensor from row0 on (wide, its width, a multiple of 8)."""
+    row = np.repeat(np.arange(row0, row0 + rows, dtype=U), wide // 8)
     col8 = np.tile(np.arange(wide // 8, dtype=U), rows)
     w = np.stack(philox(row, col8, 16 + tag, seed, epoch), -1)
     return np.stack([w & U(0xFFFF), w >> U(16)], -1).reshape(rows, wide).astype(np.int64)
 
 
-def encode(x, seed=0, epoch=0, tag=0):
-    """(codes int8 [rows][padded], exponent bytes uint8 [rows][padded / 32]) of fp32 values x."""
+def encode(x, seed=0, epoch=0, tag=0, row0=0):
+    """(codes int8 [rows][padded], exponent bytes uint8 [rows][padded / 32]) of fp32 values x, rows of a tensor from row0 on."""
     rows, cols = x.shape
     wide = -(-cols // 32) * 32
     v = np.zeros((rows, wide))
@@ -36,7 +36,7 @@ def encode(x, seed=0, epoch=0, tag=0):
     e = np.where(top > 0, exp - 7 + (mant > 127.0 / 128.0), -126)
     e = np.maximum(e, -126)
     step = np.exp2(e.astype(float))[..., None]
-    k = draws(rows, wide, seed, epoch, tag).reshape(g.shape)
+    k = draws(rows, wide, seed, epoch, tag, row0).reshape(g.shape)
     with np.errstate(invalid="ignore", over="ignore"):
         # the sum is rounded to fp32, as the definition has it
         t = ((g / step).astype(np.float32) + ((k + 0.5) / 65536.0).astype(np.float32)).astype(np.float32)
