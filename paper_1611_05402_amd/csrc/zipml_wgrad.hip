@@ -28,7 +28,6 @@ struct WgradArgs {
     int64_t ldo, out_split;   // elements between rows of out, and between the partial sums
     int64_t rows_split;       // tokens of a range
     int d_out, d_in, tiles_o, tiles_i, add;
-    int last;                 // the last value of dY is left out of the loads and added at the end (see Rows)
 };
 
 // MT x NT is the tile of dW, BK the tokens of one round; WM x WN waves share the tile.
@@ -125,8 +124,9 @@ __device__ __forceinline__ void place_of(const WgradArgs &a, int &split, int &o,
     i = in / deep;
 }
 
-// WIDE: rows of dY are read 16 bytes at a time; otherwise value by value.
-template <typename T, typename S, bool WIDE>
+// WIDE: rows of dY are read 16 bytes at a time; otherwise value by value.  LAST: the last value of dY is not among what the
+// loads bring (see Rows); a kernel of its own, since the others lose 2 to 10 % with these lines in them.
+template <typename T, typename S, bool WIDE, bool LAST>
 __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
 {
     extern __shared__ __align__(16) char lds[];
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         next = t;
     }
 
-    const bool last = a.last && t_end == a.rows && o0 + S::MT >= a.d_out;
+    const bool last = LAST && t_end == a.rows && o0 + S::MT >= a.d_out;
     const float last_dy = last ? (float)dy[(a.rows - 1) * a.lddy + a.d_out - 1] : 0.0f;
     float *out = a.out + split * a.out_split;
 #pragma unroll
@@ -380,10 +380,10 @@ static int launch_wgrad(hipStream_t s, WgradArgs a, int splits)
 {
     // 16 bytes at a time, at any alignment, where the offsets of a round fit 31 bits
     const bool wide = a.lddy * (int64_t)sizeof(T) < (1 << 24);
-    a.last = wide && sizeof(T) == 2 && a.d_out % 2 == 1;
-    auto k = wide ? k_act_wgrad<T, S, true> : k_act_wgrad<T, S, false>;
-    static std::atomic<uint64_t> done[2];
-    if (allow_lds((const void *)k, 2 * S::kStage, done[wide])) return ZIPML_ELAUNCH;
+    const bool last = wide && sizeof(T) == 2 && a.d_out % 2 == 1;
+    auto k = !wide ? k_act_wgrad<T, S, false, false> : !last ? k_act_wgrad<T, S, true, false> : k_act_wgrad<T, S, true, sizeof(T) == 2>;
+    static std::atomic<uint64_t> done[3];
+    if (allow_lds((const void *)k, 2 * S::kStage, done[wide + last])) return ZIPML_ELAUNCH;
     hipLaunchKernelGGL(k, dim3(a.tiles_o * a.tiles_i * splits), dim3(S::kThreads), 2 * S::kStage, s, a);
     return hip_check(hipGetLastError());
 }
@@ -428,7 +428,7 @@ extern "C" int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int6
     hipStream_t s = entry_stream(stream);
     const int add = flags & ZIPML_WGRAD_ADD ? 1 : 0;
     WgradArgs a{dy_dev, (const uint8_t *)act_dev, dw_dev, lddy, rows, lay.pitch, lay.groups, lay.steps, lddw, 0,
-                p.rows_split, (int)d_out, (int)d_in, p.tiles_o, p.tiles_i, add, 0};
+                p.rows_split, (int)d_out, (int)d_in, p.tiles_o, p.tiles_i, add};
     if (p.splits > 1) {
         a.out = (float *)workspace_dev;
         a.ldo = (int64_t)p.tiles_i * p.tile;
