@@ -253,6 +253,7 @@ struct ScanShared {
     WavePairs left, right;                 // pairs of the waves in either direction, then of those before
     WavePairs blocks;                      // pairs of the blocks before, a few to each wave
     float carry[kCh];
+    float kept[kCh];                       // backward: the state that the forward pass kept
     uint32_t ticket;
     __align__(8) uint8_t steps[2][kCh / kActGroup][kBlock];   // of x and z: the stored inputs' exponents
 };
@@ -628,7 +629,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // ---- backward ----------------------------------------------------------------------------------
 // p_t = f_t d_t, d_t = dy_t + p_{t+1}, is a scan from right to left with the same factors as that of the states from left to
 // right; a run's pairs of both come from one walk: B of the right-to-left one is the sum of d_t times the product of the f
-// up to t.  g = 1 - f waits in LDS, each thread's own in its place, so that two workgroups fit a compute unit.
+// up to t.  What waits for the chain has to fit 128 registers, so that two workgroups fit a compute unit: f does; g = 1 - f waits in
+// LDS, each thread's own in its place; x is decoded and dy read a second time behind the chain (kept in registers, dy costs 2 %
+// at 32,768 tokens x 2,048 channels of bf16 and, with 69 registers spilled, 18 % of fp32).
 // What bounds it: as in the forward direction, what a block does one after the other, at two blocks to a compute unit (128
 // registers a thread; 32,768 tokens x 2,048 channels: 170 us, 3.2 TB/s; 386 MB are read for 273, the two halves of a line of
 // codes often by different XCDs).  With one block of 232 registers to a compute unit it took 321 us against 230 in the same form.  A block in
@@ -664,7 +667,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             qx[j] = *reinterpret_cast<const uint32_t *>(p.rx + o);
         });
         part.load((const T *)p.dy, p.lddy, dy);
+        const bool keeper = threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels;
+        const float kept = keeper ? p.states[blk * p.channels + at.c0 + threadIdx.x] : 0.0f;
         steps_in(p, t0, at.c0, sh);
+        if (threadIdx.x < kCh) sh.kept[threadIdx.x] = kept;
         r = block_map(p, t0, sh.map);
         const int group = (c - (int)at.c0) / kActGroup;
         const u32x2 ez = *reinterpret_cast<const u32x2 *>(&sh.steps[1][group][run]);
@@ -742,6 +748,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
                 P[k] = cut ? P[k] : __builtin_fmaf(A[k], d[k], P[k]);
             }
             cut |= last >> j & 1;
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
@@ -760,6 +767,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     auto walk = [&](auto flag) {
         constexpr bool SOME = decltype(flag)::value;                // (a block with all its rows has it false)
         float in[kOwn], q[kOwn];
+        part.load((const T *)p.dy, p.lddy, dy);                     // again, out of the caches
+        part.settle(dy, at.c0);
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
         enter<SOME>(AR, P, sh.right, in, q);
@@ -775,13 +784,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
                 if (SOME && outside >> j & 1) d[j][k] = 0.0f;
                 q[k] = SOME && outside >> j & 1 ? 0.0f : f[j][k] * d[j][k];
             }
+            if (SOME) __builtin_amdgcn_sched_barrier(0);
             if (SOME && p.dh0 && first >> j & 1)
                 store4<float>(p.dh0 + (int64_t)sh.map.first[run + j] * p.channels + c, part.left(), q);
         }
-        // the states again, from the one that the forward pass kept (x decoded anew: kept from above it would not fit the
-        // registers)
+        // the states again, from the one that the forward pass kept
         float h[kOwn];
-        load_state(p.states, blk, p.channels, c, in);
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) in[k] = sh.kept[c - at.c0 + k];
         enter<SOME>(A, H, sh.left, in, h);
         T *px = (T *)p.dx + part.t * p.lddx + c, *pz = (T *)p.dz + part.t * p.lddz + c;
 #pragma unroll
@@ -805,10 +815,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         }
     };
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) {
-        __asm__ volatile("" : "+v"(qx[j]));
-        if constexpr (sizeof(T) == 2) __asm__ volatile("" : "+v"(dy[j].w));
-    }
+    for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(qx[j]));   // codes wait for the chain, not the values decoded above
     if (__builtin_expect(some, 0)) walk(std::true_type());
     else walk(std::false_type());
     pass_on(p, blk, at.c0, p.dh_last, p.dh0);
