@@ -149,7 +149,9 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
     constexpr int kDeals = S::kSteps - 1;
     auto load = [&](Tile &tile, int64_t t0, int k) {
         const int64_t left = t_end - t0;
-        const Rows ra(dy + t0 * a.lddy + o0, WIDE ? ((left - 1) * a.lddy + a.d_out - o0) * (int64_t)sizeof(T) : 0);
+        // (of an odd width, the dword of a row's last value is there to its end while rows follow)
+        const int64_t values = (left - 1) * a.lddy + a.d_out - o0 + (LAST && t_end < a.rows ? 1 : 0);
+        const Rows ra(dy + t0 * a.lddy + o0, WIDE ? values * (int64_t)sizeof(T) : 0);
         const Rows rb(a.act + t0 * a.pitch + i0, left * a.pitch - i0);
         const Rows rs(a.act + a.steps + t0 * a.groups + (i0 >> 5), left * a.groups - (i0 >> 5));
 #pragma unroll

@@ -107,6 +107,17 @@ def test_the_very_last_value_of_dy(rows, d_out):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,d_out,d_in", [(2500, 521, 390), (6000, 257, 700), (20000, 131, 250), (5000, 1, 3000)])
+def test_the_last_value_of_every_range_of_tokens(rows, d_out, d_in):
+    """The same where the tokens are taken in several ranges, which end at multiples of 64 tokens."""
+    dy, codes, byte = inputs(rows, d_out, d_in, "bf16")
+    dy[:, -1] = 0
+    dy[63::64, -1] = 3.0
+    for pad in (0, 1, 2):
+        check(dy, codes, byte, d_in, wgrad(dy, codes, byte, d_in, pad))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,d_out,d_in", [(5, 9, 40), (3000, 100, 65)])
 def test_adding_to_what_is_there(kind, rows, d_out, d_in):
