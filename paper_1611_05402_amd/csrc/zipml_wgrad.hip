@@ -30,11 +30,12 @@ struct WgradArgs {
     int d_out, d_in, tiles_o, tiles_i, add;
 };
 
-// MT x NT is the tile of dW, BK the tokens of one round; WM x WN waves share the tile.
-template <typename T, int MT_, int NT_, int BK_, int WM_, int WN_>
+// MT x NT is the tile of dW, BK the tokens of one round; WM x WN waves share the tile.  TEAMS such sets of waves take the
+// rounds by turns, each with its own LDS, and add up their sums at the end.
+template <typename T, int MT_, int NT_, int BK_, int WM_, int WN_, int TEAMS_ = 1>
 struct WgradShape {
-    static constexpr int MT = MT_, NT = NT_, BK = BK_, WM = WM_, WN = WN_;
-    static constexpr int kThreads = 64 * WM * WN;
+    static constexpr int MT = MT_, NT = NT_, BK = BK_, WM = WM_, WN = WN_, TEAMS = TEAMS_;
+    static constexpr int kThreads = 64 * WM * WN;                 // of a team
     static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;        // bf16 terms of a dY value
     // LDS rows of 64 or 192 bytes more than a multiple of 256: the four rows that 16 lanes of a transposing read touch, and
     // the 64 bytes that the neighbouring 16 lanes add to each, then fall on all banks once.
@@ -50,7 +51,8 @@ struct WgradShape {
     static constexpr int TM = MT / WM / 32, TN = NT / WN / 32;    // 32 x 32 tiles of a wave
     static_assert(kLoadsA * 8 * kThreads == BK * MT && kLoadsB * 8 * kThreads == BK * NT, "whole loads");
     static_assert(MT % 64 == 0 && NT % 64 == 0, "LDS rows");
-    static_assert(2 * kStage <= 160 * 1024, "LDS");
+    static constexpr int kLds = 2 * kStage * TEAMS;
+    static_assert(kLds <= 160 * 1024 && (TEAMS - 1) * MT * NT * 4 <= kLds, "LDS");
     static_assert(kSteps % 2 == 0 && BK / 16 % 2 == 0, "operands of the steps by turns");
 };
 
@@ -127,10 +129,11 @@ __device__ __forceinline__ void place_of(const WgradArgs &a, int &split, int &o,
 // WIDE: rows of dY are read 16 bytes at a time; otherwise value by value.  LAST: the last value of dY is not among what the
 // loads bring (see Rows); a kernel of its own, since the others lose 2 to 10 % with these lines in them.
 template <typename T, typename S, bool WIDE, bool LAST>
-__global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
+__global__ __launch_bounds__(S::kThreads * S::TEAMS) void k_act_wgrad(WgradArgs a)
 {
     extern __shared__ __align__(16) char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int team = S::TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / S::kThreads);
+    const int tid = threadIdx.x - team * S::kThreads, lane = tid & 63, wave = tid >> 6;
     int split, o0, i0;
     place_of(a, split, o0, i0);
     o0 *= S::MT;
@@ -235,35 +238,37 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
     // barrier stands before a round's last step, whose own are in registers by then.  The steps are kept apart, since the
     // compiler otherwise moves all loads to a round's end, where their latency shows (555 us in place of 460 for 16,384
     // tokens, 4,096 x 4,096, in the same arrangement).
-    char *here = lds, *next = lds + S::kStage;
+    char *here = lds + team * 2 * S::kStage, *next = here + S::kStage;
+    const int64_t t_first = t_begin + team * S::BK;
+    constexpr int kTurn = S::TEAMS * S::BK;
     Tile tile;
     if constexpr (S::MT < 256) {           // both rounds asked for at once: the memory's latency once, not twice
         Tile first;
 #pragma unroll
-        for (int k = 0; k < kDeals; ++k) load(first, t_begin, k);
+        for (int k = 0; k < kDeals; ++k) load(first, t_first, k);
 #pragma unroll
-        for (int k = 0; k < kDeals; ++k) load(tile, t_begin + S::BK, k);
+        for (int k = 0; k < kDeals; ++k) load(tile, t_first + kTurn, k);
 #pragma unroll
         for (int k = 0; k < kDeals; ++k) store(first, here, k);
     } else {                               // (no registers for two; 1 % on the whole kernel)
 #pragma unroll
-        for (int k = 0; k < kDeals; ++k) load(tile, t_begin, k);
+        for (int k = 0; k < kDeals; ++k) load(tile, t_first, k);
 #pragma unroll
         for (int k = 0; k < kDeals; ++k) {
             store(tile, here, k);
-            load(tile, t_begin + S::BK, k);
+            load(tile, t_first + kTurn, k);
         }
     }
     lds_barrier();
     read(here, 0);
-    for (int64_t t0 = t_begin; t0 < t_end; t0 += S::BK) {
+    for (int64_t t0 = t_begin; t0 < t_end; t0 += kTurn) {
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) {
             if (s < kDeals) {
                 read(here, s + 1);
                 if (S::kInOrder) __builtin_amdgcn_sched_barrier(0);
                 store(tile, next, s);
-                load(tile, t0 + 2 * S::BK, s);
+                load(tile, t0 + team * S::BK + 2 * kTurn, s);
             } else {
                 lds_barrier();
                 read(next, 0);
@@ -281,6 +286,24 @@ __global__ __launch_bounds__(S::kThreads) void k_act_wgrad(WgradArgs a)
         next = t;
     }
 
+    if constexpr (S::TEAMS > 1) {
+        lds_barrier();
+        f32x16 *const sums = reinterpret_cast<f32x16 *>(lds);
+        const auto slot = [&](int other, int m, int n) { return (((other - 1) * S::TM + m) * S::TN + n) * S::kThreads + tid; };
+        if (team > 0)
+#pragma unroll
+            for (int m = 0; m < S::TM; ++m)
+#pragma unroll
+                for (int n = 0; n < S::TN; ++n) sums[slot(team, m, n)] = acc[m][n];
+        lds_barrier();
+        if (team > 0) return;
+#pragma unroll
+        for (int other = 1; other < S::TEAMS; ++other)
+#pragma unroll
+            for (int m = 0; m < S::TM; ++m)
+#pragma unroll
+                for (int n = 0; n < S::TN; ++n) acc[m][n] += sums[slot(other, m, n)];
+    }
     const bool last = LAST && t_end == a.rows && o0 + S::MT >= a.d_out;
     const float last_dy = last ? (float)dy[(a.rows - 1) * a.lddy + a.d_out - 1] : 0.0f;
     float *out = a.out + split * a.out_split;
@@ -332,45 +355,47 @@ __global__ __launch_bounds__(256) void k_wgrad_sum(const float *__restrict__ par
 }
 
 // The shapes.  256 x 256: per value of an operand the most products, one workgroup a compute unit; the smaller ones fill
-// the machine where dW is small, two or more workgroups to a compute unit.
+// the machine where dW is small, two or more workgroups to a compute unit; two teams on a tile where there are not that many.
 template <typename T> struct Shapes {
     static constexpr int BK = sizeof(T) == 4 ? 32 : 64;
     typedef WgradShape<T, 256, 256, BK, 2, 4> Large;
     typedef WgradShape<T, 128, 128, BK, 2, 4> Middle;
     typedef WgradShape<T, 64, 64, BK, 2, 2> Small;
+    typedef WgradShape<T, 64, 64, BK, 2, 2, 2> Teams;
 };
 
 // Which shape, and in how many ranges the tokens are taken (whose partial sums a second launch joins): the least of
-//   start + rounds of a range * (one workgroup on a compute unit: lone, k of them: k * shared)
+//   start + turns of a range * (one workgroup on a compute unit: lone, k of them: k * shared)
 //         + (ranges > 1: a launch, partial sums written and read),
-// with the times of a round measured on either side of each choice (us; 64 tokens of bf16 or 32 of fp32 dY):
-//   256: 1.4 to 1.8, fp32 2.6;  128: 0.68 to 0.85 alone, 0.65 each of two, fp32 1.0 and 0.9;  64: 0.5 and 0.37, fp32 0.65 and 0.45.
-// Of 50 sizes and types timed in every shape and number of ranges 46 get the fastest, four are 3 to 6 % slower than it.
-// 4,096 tokens, 2,048 x 2,048, launches alone: 256 in 4 ranges 43 us + 67 MB of partial sums, 128 in one 53; 4,096 tokens,
-// 1,024 x 1,024: 256 in 16 ranges 23, 128 in 4 22, 64 in one 36; 256 tokens, 256 x 256: 128 in one 12, 64 in one 8.
+// a turn being 64 tokens of bf16 or 32 of fp32 dY, twice that with two teams.  The constants (us) are those that come nearest to 1,978
+// times measured over 55 sizes, both types, all shapes and numbers of ranges; the choice is then 1.4 % (bf16) and 0.3 % (fp32)
+// slower than the fastest on average, 15 % at most.  Without teams it was 4.4 and 3.8 %, 34 % at most: 1,000 tokens, 1,001 x 520 12.8 in
+// place of 9.6 us with bf16 and 19.9 in place of 16.7 with fp32; 4,096 tokens, 1,024 x 1,024 28 in place of 22.  A team alone
+// is faster up to some hundred tokens (128 tokens, 512 x 512: 4.8 us against 5.2).
 struct WgradPlan {
-    int tile, splits, tiles_o, tiles_i;
+    int tile, teams, splits, tiles_o, tiles_i;
     int64_t rows_split;
     size_t workspace() const { return splits > 1 ? (size_t)splits * tiles_o * tiles_i * tile * tile * 4 : 0; }
 };
 static WgradPlan wgrad_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype)
 {
-    struct { int tile; double lone, shared; } const shapes[2][3] = {{{256, 1.6, 1.6}, {128, 0.8, 0.65}, {64, 0.5, 0.37}},
-                                                                    {{256, 2.6, 2.6}, {128, 1.0, 0.9}, {64, 0.65, 0.45}}};
+    struct { int tile, teams; double start, lone, shared; } const shapes[2][4] = {
+        {{256, 1, 6.2, 1.35, 1.35}, {128, 1, 4.5, 0.69, 0.54}, {64, 1, 4.1, 0.44, 0.30}, {64, 2, 4.7, 0.61, 0.61}},
+        {{256, 1, 5.2, 2.5, 2.5}, {128, 1, 3.5, 1.03, 0.84}, {64, 1, 3.9, 0.57, 0.37}, {64, 2, 4.8, 0.74, 0.74}}};
     const int64_t round = dtype == ZIPML_F32 ? 32 : 64;
     WgradPlan best{};
     double least = 0;
     for (const auto &c : shapes[dtype == ZIPML_F32]) {
-        const int64_t to = (d_out + c.tile - 1) / c.tile, ti = (d_in + c.tile - 1) / c.tile;
+        const int64_t to = (d_out + c.tile - 1) / c.tile, ti = (d_in + c.tile - 1) / c.tile, turn = round * c.teams;
         // (ranges only where dW is at most 2^16 tiles, so that the partial sums can be counted in 32 bits)
         for (int64_t s = 1; s <= 256 && (s == 1 || ((s - 1) * 128 < rows && to * ti <= 1 << 16)); s *= 2) {
             const int64_t rows_split = round_up((rows + s - 1) / s, 64), splits = (rows + rows_split - 1) / rows_split;
-            const double k = (double)((to * ti * splits + 255) / 256), rounds = (double)((rows_split + round - 1) / round);
-            const double us = 5.0 + rounds * (k > 1 ? k * c.shared : c.lone) +
-                              (splits > 1 ? 4.0 + (double)splits * to * ti * c.tile * c.tile * 8.0 / 4.5e6 : 0.0);
+            const double k = (double)((to * ti * splits + 255) / 256), turns = (double)((rows_split + turn - 1) / turn);
+            const double us = c.start + turns * (k > 1 ? k * c.shared : c.lone) +
+                              (splits > 1 ? 3.0 + (double)splits * to * ti * c.tile * c.tile * 8.0 / 6e6 : 0.0);
             if (best.tile == 0 || us < least) {
                 least = us;
-                best = WgradPlan{c.tile, (int)splits, (int)to, (int)ti, rows_split};
+                best = WgradPlan{c.tile, c.teams, (int)splits, (int)to, (int)ti, rows_split};
             }
         }
     }
@@ -385,8 +410,8 @@ static int launch_wgrad(hipStream_t s, WgradArgs a, int splits)
     const bool last = wide && sizeof(T) == 2 && a.d_out % 2 == 1;
     auto k = !wide ? k_act_wgrad<T, S, false, false> : !last ? k_act_wgrad<T, S, true, false> : k_act_wgrad<T, S, true, sizeof(T) == 2>;
     static std::atomic<uint64_t> done[3];
-    if (allow_lds((const void *)k, 2 * S::kStage, done[wide + last])) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3(a.tiles_o * a.tiles_i * splits), dim3(S::kThreads), 2 * S::kStage, s, a);
+    if (allow_lds((const void *)k, S::kLds, done[wide + last])) return ZIPML_ELAUNCH;
+    hipLaunchKernelGGL(k, dim3(a.tiles_o * a.tiles_i * splits), dim3(S::kThreads * S::TEAMS), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
 
@@ -395,6 +420,7 @@ static int launch_tile(hipStream_t s, const WgradArgs &a, const WgradPlan &p)
 {
     if (p.tile == 256) return launch_wgrad<T, typename Shapes<T>::Large>(s, a, p.splits);
     if (p.tile == 128) return launch_wgrad<T, typename Shapes<T>::Middle>(s, a, p.splits);
+    if (p.teams == 2) return launch_wgrad<T, typename Shapes<T>::Teams>(s, a, p.splits);
     return launch_wgrad<T, typename Shapes<T>::Small>(s, a, p.splits);
 }
 

@@ -88,6 +88,16 @@ def test_middle_sizes(kind, rows, d_out, d_in):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [321, 384, 400, 449, 512, 577, 640, 700, 961])
+def test_rounds_of_tokens_shared_by_turns(kind, rows):
+    """Numbers of tokens that leave some of a turn's rounds short or empty."""
+    dy, codes, byte = inputs(rows, 131, 70, kind)
+    for flags, before in ((0, None), (zipml.WGRAD_ADD, np.full((131, 70), 0.25, np.float32))):
+        check(dy, codes, byte, 70, wgrad(dy, codes, byte, 70, 1, 1, flags, before), before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("d_out", [5, 130])
 def test_rows_far_apart(kind, d_out):
     """Rows of dY more than 16 MiB apart are read value by value."""
