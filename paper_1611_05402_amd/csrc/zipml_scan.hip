@@ -3,14 +3,14 @@
 // Both directions are scans of pairs: a run of tokens takes a state h to A h + B, and two runs one after the other
 // to (A2 A1) h + (A2 B1 + B2).  A workgroup owns 64 channels and a block of 256 tokens: sixteen lanes side by side take four
 // channels each (128 bytes of a bf16 row), 32 such rows of lanes eight tokens each, which a thread walks through in
-// registers.  Everything is read and written once: the rows of lanes are joined by shuffles and LDS, the blocks by a chain in
+// registers (with few blocks 32 channels: eight lanes side by side, four tokens each).  Everything is read and written once: the rows of lanes are joined by shuffles and LDS, the blocks by a chain in
 // global memory while their tokens stay in registers.
 //
 // The chain.  A block publishes its pair, takes the pairs of the blocks before it up to the last multiple of kSuper and the
 // state there, which the block before that multiple has published, and so has the state that enters it.  What is
 // joined in which order depends on the block's number alone, so the results do not depend on timing.  A word is a pair of
 // floats stored and polled as 64 bits, all ones before it is there (A is never a NaN).  Blocks are handed out by a
-// counter for each 64 channels, in the chain's order: a block waits only for blocks that were handed out before it, to
+// counter for each group of channels, in the chain's order: a block waits only for blocks that were handed out before it, to
 // workgroups that run, and those wait for nothing that is behind them, so every wait ends.
 //
 // A = 0 marks a run that contains the start of a sequence (or lies outside all): what is before it does not matter, and
@@ -22,17 +22,27 @@
 namespace zipml {
 
 constexpr int kBlock = ZIPML_SCAN_BLOCK;   // tokens of a workgroup
-constexpr int kCh = 64;                    // channels of a workgroup
-constexpr int kRun = 8;                    // tokens of a thread
 constexpr int kOwn = 4;                    // channels of a thread
-constexpr int kLanes = kCh / kOwn;         // lanes side by side
-constexpr int kRows = kWave / kLanes;      // runs of a wave
 constexpr int kSuper = 32;                 // blocks between two published states
-constexpr int kWaves = kBlock / (kRows * kRun);
+constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
+constexpr int kMostCh = 64;
 constexpr float kTiny = 1.17549435e-38f;
 constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1
 static_assert(kSuper % kWaves == 0, "the waves share the pairs of kSuper blocks");
+static_assert(kThreads == 2 * kBlock, "a thread for each token of x and z");
+
+// How a block is cut up: channels of a workgroup and tokens of a thread.
+template <int CH, int RUN> struct Cut {
+    static constexpr int kCh = CH, kRun = RUN;
+    static constexpr int kLanes = kCh / kOwn;      // lanes side by side
+    static constexpr int kRows = kWave / kLanes;   // runs of a wave
+    static_assert(kWaves * kRows * kRun == kBlock && kRun % 4 == 0 && kCh % kActGroup == 0 && kCh <= kMostCh, "whole blocks");
+    static __device__ __forceinline__ int lane() { return threadIdx.x & (kLanes - 1); }
+    static __device__ __forceinline__ int run() { return threadIdx.x / kLanes * kRun; }   // the thread's first token, in the block
+};
+typedef Cut<64, 8> Wide;
+typedef Cut<32, 4> Narrow;
 
 struct ScanArgs {
     const void *x, *z;                     // forward
@@ -109,7 +119,9 @@ template <> struct Raw4<float> {
 // A thread's part of a block's rows.  The loads of a block are all issued before the first is used, so none of them stands in a
 // branch of its own: a thread whose rows or columns are not all there reads the last ones that are, and `settle` moves columns
 // to their places.  Fewer than four columns in all are read one by one.
+template <typename S>
 struct Part {
+    static constexpr int kRun = S::kRun;
     int64_t tokens, channels;
     int64_t t;             // first token
     int c, at;             // first column, and the column at which it reads
@@ -118,8 +130,8 @@ struct Part {
     {
         tokens = p.tokens;
         channels = p.channels;
-        t = t0 + threadIdx.x / kLanes * kRun;
-        c = (int)c0 + (threadIdx.x & (kLanes - 1)) * kOwn;
+        t = t0 + S::run();
+        c = (int)c0 + S::lane() * kOwn;
         at = c <= channels - kOwn ? c : (int)channels - kOwn;
         whole = t0 + kBlock <= tokens;
     }
@@ -155,7 +167,7 @@ struct Part {
     template <typename T>
     __device__ __forceinline__ void settle(Raw4<T> (&v)[kRun], int64_t c0) const
     {
-        if (c0 + kCh <= channels || channels < kOwn) return;
+        if (c0 + S::kCh <= channels || channels < kOwn) return;
         const int s = c - at < kOwn ? c - at : kOwn;
 #pragma unroll
         for (int j = 0; j < kRun; ++j) v[j].move(s);
@@ -237,39 +249,42 @@ __device__ __forceinline__ Range block_map(const ScanArgs &a, int64_t t0, BlockM
 }
 
 // Empty sequences hand on what they are given.
+template <typename S>
 __device__ __forceinline__ void pass_on(const ScanArgs &p, int64_t blk, int64_t c0, const float *from, float *to)
 {
     if (!to || !p.seq_start) return;
     const int64_t c = c0 + (threadIdx.x & 63);
     for (int64_t s = blk * kWaves + (threadIdx.x >> 6); s < p.n_seq; s += p.blocks * kWaves)
-        if (p.seq_start[s] >= p.seq_start[s + 1] && c < p.channels)
+        if (p.seq_start[s] >= p.seq_start[s + 1] && (threadIdx.x & 63) < S::kCh && c < p.channels)
             to[s * p.channels + c] = from ? from[s * p.channels + c] : 0.0f;
 }
 
 // ---- joining runs ------------------------------------------------------------------------------
-typedef float2 WavePairs[kWaves][kCh];
+typedef float2 WavePairs[kWaves][kMostCh];
 struct ScanShared {
     BlockMap map;
     WavePairs left, right;                 // pairs of the waves in either direction, then of those before
     WavePairs blocks;                      // pairs of the blocks before, a few to each wave
-    float carry[kCh];
-    float kept[kCh];                       // backward: the state that the forward pass kept
+    float carry[kMostCh];
+    float kept[kMostCh];                       // backward: the state that the forward pass kept
     uint32_t ticket;
-    __align__(8) uint8_t steps[2][kCh / kActGroup][kBlock];   // of x and z: the stored inputs' exponents
+    __align__(8) uint8_t steps[2][kMostCh / kActGroup][kBlock];   // of x and z: the stored inputs' exponents
 };
 // The exponents of a block, between global memory (a token's side by side) and LDS (a group's side by side, so that a thread has
 // those of its run in one piece).  Each thread takes one token of x or z.
+template <typename S>
 __device__ __forceinline__ void steps_in(const ScanArgs &p, int64_t t0, int64_t c0, ScanShared &sh)
 {
     const int which = threadIdx.x / kBlock, i = threadIdx.x % kBlock;
     const int64_t t = t0 + i < p.tokens ? t0 + i : p.tokens - 1, g = c0 / kActGroup;
     const uint8_t *a = (which ? p.rz : p.rx) + p.lay.steps + t * p.lay.groups + g;
-    uint8_t e[kCh / kActGroup];
+    uint8_t e[S::kCh / kActGroup];
 #pragma unroll
-    for (int k = 0; k < kCh / kActGroup; ++k) e[k] = a[g + k < p.lay.groups ? k : 0];
+    for (int k = 0; k < S::kCh / kActGroup; ++k) e[k] = a[g + k < p.lay.groups ? k : 0];
 #pragma unroll
-    for (int k = 0; k < kCh / kActGroup; ++k) sh.steps[which][k][i] = e[k];
+    for (int k = 0; k < S::kCh / kActGroup; ++k) sh.steps[which][k][i] = e[k];
 }
+template <typename S>
 __device__ __forceinline__ void steps_out(const ScanArgs &p, int64_t t0, int64_t c0, const ScanShared &sh)
 {
     const int which = threadIdx.x / kBlock, i = threadIdx.x % kBlock;
@@ -277,18 +292,18 @@ __device__ __forceinline__ void steps_out(const ScanArgs &p, int64_t t0, int64_t
     if (t0 + i >= p.tokens) return;
     uint8_t *a = (which ? p.wz : p.wx) + p.lay.steps + (t0 + i) * p.lay.groups + g;
 #pragma unroll
-    for (int k = 0; k < kCh / kActGroup; ++k)
+    for (int k = 0; k < S::kCh / kActGroup; ++k)
         if (g + k < p.lay.groups) a[k] = sh.steps[which][k][i];
 }
-static_assert(kThreads == 2 * kBlock && kRun == 8, "a thread for each token of x and z; eight exponents in one piece");
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
 // A, B: in, the pair of each thread's run; out, that of the runs of its wave before it (REVERSE: behind it).  The wave's pair
 // goes to `waves`.
-template <bool REVERSE, bool SOME>
+template <typename S, bool REVERSE, bool SOME>
 __device__ __forceinline__ void wave_scan(float (&A)[kOwn], float (&B)[kOwn], WavePairs &waves)
 {
-    const int lane = threadIdx.x & 63, cl = lane & (kLanes - 1);
+    constexpr int kLanes = S::kLanes, kRows = S::kRows;
+    const int lane = threadIdx.x & 63, cl = S::lane();
     const int pos = REVERSE ? kRows - 1 - lane / kLanes : lane / kLanes;
     auto before = [&](float v, int s) { return __shfl(v, (REVERSE ? lane + kLanes * s : lane - kLanes * s) & 63, 64); };
 #pragma unroll
@@ -328,11 +343,11 @@ __device__ __forceinline__ float2 block_prefix(WavePairs &waves)
     return float2{SOME ? a : __builtin_fmaxf(a, kTiny), b};
 }
 // The state that enters the thread's run, in A's place, from the one that enters the block.
-template <bool SOME>
+template <typename S, bool SOME>
 __device__ __forceinline__ void enter(const float (&A)[kOwn], const float (&B)[kOwn], const WavePairs &waves,
                                       const float (&block)[kOwn], float (&h)[kOwn])
 {
-    const int cl = threadIdx.x & (kLanes - 1), wave = wave_id();
+    const int cl = S::lane(), wave = wave_id();
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
         const float2 w = waves[wave][cl * kOwn + k];
@@ -355,12 +370,12 @@ __device__ __forceinline__ uint64_t await(const uint64_t *p)
 
 // From the waves' pairs to the state that enters block `k` of the chain (k counts in the direction of the scan), in sh.carry; the
 // block's own pair, and the state behind it where one is due, are published.  `other` is what a second wave does meanwhile.
-template <bool REVERSE, typename Other>
+template <typename S, bool REVERSE, typename Other>
 __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, ScanShared &sh, WavePairs &waves, Other other)
 {
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int64_t c = c0 + lane;
-    const bool live = c < p.channels;
+    const bool live = lane < S::kCh && c < p.channels;
     auto at = [&](int64_t i) { return (REVERSE ? p.blocks - 1 - i : i) * p.channels + c; };
     // the pairs from the last multiple of kSuper on are asked for first, a few by each wave
     constexpr int kEach = kSuper / kWaves;
@@ -404,14 +419,15 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
 // channels in turn, not some of them always: rows lie a power of two apart more often than not, so that a group's 128 bytes of
 // all rows fall on one or two of an L2's sixteen channels.
 struct Place { int64_t k, c0; };
+template <typename S>
 __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
 {
     const uint32_t n = (uint32_t)p.groups, b = blockIdx.x, even = (uint32_t)p.blocks / 8 * 8 * n;
     const uint32_t g = (b < even ? b >> 3 : b - even) % n;
-    if (p.blocks == 1) return Place{0, g * (int64_t)kCh};
+    if (p.blocks == 1) return Place{0, g * (int64_t)S::kCh};
     if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    return Place{sh.ticket, g * (int64_t)kCh};
+    return Place{sh.ticket, g * (int64_t)S::kCh};
 }
 
 // The words (an even number of them) and counters of a chain before it starts: a launch, 2 to 5 us.
@@ -497,14 +513,15 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 // 32,768 tokens x 2,048 channels, 165 us, 3.3 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
 // pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 57 us, 3.5 TB/s; a copy reaches 4.9).  128 tokens to
 // a workgroup in place of 256: 241 and 98 us against 229 and 85 (an earlier form), the chain being twice as long.
-template <typename T>
+template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 {
+    constexpr int kRun = S::kRun, kCh = S::kCh;
     __shared__ ScanShared sh;
-    const Place at = take(p, sh);
+    const Place at = take<S>(p, sh);
     const int64_t blk = at.k, t0 = blk * kBlock;
-    const int run = threadIdx.x / kLanes * kRun;                    // the first token of the thread's run, in the block
-    const Part part(p, t0, at.c0);
+    const int run = S::run();
+    const Part<S> part(p, t0, at.c0);
     const int c = part.c;
 
     Raw4<T> x[kRun], z[kRun];
@@ -542,7 +559,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
         if (c % kActGroup == 0)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                *reinterpret_cast<u32x2 *>(&sh.steps[i][(c - (int)at.c0) / kActGroup][run]) = u32x2{e[i][0], e[i][1]};
+                __builtin_memcpy(__builtin_assume_aligned(&sh.steps[i][(c - (int)at.c0) / kActGroup][run], kRun), e[i], kRun);
     }
     float a[kRun][kOwn], b[kRun][kOwn];                             // f and (1 - f) x
 #pragma unroll
@@ -568,7 +585,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
                 B[k] = __builtin_fmaf(a[j][k], B[k], b[j][k]);
                 A[k] *= a[j][k];
             }
-        wave_scan<false, false>(A, B, sh.left);
+        wave_scan<S, false, false>(A, B, sh.left);
     } else {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) { A[k] = 1.0f; B[k] = 0.0f; }
@@ -597,19 +614,19 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
         }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) A[k] = reset ? 0.0f : __builtin_fmaxf(A[k], kTiny);
-        wave_scan<false, true>(A, B, sh.left);
+        wave_scan<S, false, true>(A, B, sh.left);
     }
-    chain<false>(p, at.k, at.c0, sh, sh.left, [] {});
+    chain<S, false>(p, at.k, at.c0, sh, sh.left, [] {});
 
     float in[kOwn], h[kOwn];
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
-    if (p.wx) steps_out(p, t0, at.c0, sh);
+    if (p.wx) steps_out<S>(p, t0, at.c0, sh);
     if (p.states && threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels)
         p.states[blk * p.channels + at.c0 + threadIdx.x] = sh.carry[threadIdx.x];
     auto walk = [&](auto flag) {
         constexpr bool SOME = decltype(flag)::value;                // (a block with all its rows has it false)
-        enter<SOME>(A, B, sh.left, in, h);
+        enter<S, SOME>(A, B, sh.left, in, h);
         T *y = (T *)p.y + part.t * p.ldy + c;
 #pragma unroll
         for (int j = 0; j < kRun; ++j, y += p.ldy) {
@@ -623,7 +640,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
     };
     if (__builtin_expect(some, 0)) walk(std::true_type());
     else walk(std::false_type());
-    pass_on(p, blk, at.c0, p.h0, p.h_last);
+    pass_on<S>(p, blk, at.c0, p.h0, p.h_last);
 }
 
 // ---- backward ----------------------------------------------------------------------------------
@@ -637,24 +654,26 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // codes often by different XCDs).  With one block of 232 registers to a compute unit it took 321 us against 230 in the same form.  A block in
 // which sequences begin or end takes a path of its own from the pairs on: it is the rarer one, and the registers of both together
 // would not fit (stores and loads are counted together, so a register fetched back after a store waits for that store).
+template <typename S>
 struct BackwardShared {
     ScanShared s;
-    f32x4 g[kRun][kThreads];
+    f32x4 g[S::kRun][kThreads];
 };
-template <typename T>
+template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
 {
+    constexpr int kRun = S::kRun, kCh = S::kCh;
     extern __shared__ __align__(16) char lds[];
-    BackwardShared &all = *reinterpret_cast<BackwardShared *>(lds);
+    BackwardShared<S> &all = *reinterpret_cast<BackwardShared<S> *>(lds);
     ScanShared &sh = all.s;
-    const Place at = take(p, sh);
+    const Place at = take<S>(p, sh);
     const int64_t blk = p.blocks - 1 - at.k, t0 = blk * kBlock;
-    const int run = threadIdx.x / kLanes * kRun;
-    const Part part(p, t0, at.c0);
+    const int run = S::run();
+    const Part<S> part(p, t0, at.c0);
     const int c = part.c;
 
     uint32_t qx[kRun];
-    u32x2 ex;                                                       // the steps of x, a byte a token
+    uint32_t ex[kRun / 4];                                          // the steps of x, a byte a token
     Range r;
     auto step_x = [&](int j) { return act_step(ex[j >> 2] >> (8 * (j & 3)) & 255u); };
     float f[kRun][kOwn];
@@ -669,12 +688,13 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         part.load((const T *)p.dy, p.lddy, dy);
         const bool keeper = threadIdx.x < kCh && at.c0 + threadIdx.x < p.channels;
         const float kept = keeper ? p.states[blk * p.channels + at.c0 + threadIdx.x] : 0.0f;
-        steps_in(p, t0, at.c0, sh);
+        steps_in<S>(p, t0, at.c0, sh);
         if (threadIdx.x < kCh) sh.kept[threadIdx.x] = kept;
         r = block_map(p, t0, sh.map);
         const int group = (c - (int)at.c0) / kActGroup;
-        const u32x2 ez = *reinterpret_cast<const u32x2 *>(&sh.steps[1][group][run]);
-        ex = *reinterpret_cast<const u32x2 *>(&sh.steps[0][group][run]);
+        uint32_t ez[kRun / 4];
+        __builtin_memcpy(ez, __builtin_assume_aligned(&sh.steps[1][group][run], kRun), kRun);
+        __builtin_memcpy(ex, __builtin_assume_aligned(&sh.steps[0][group][run], kRun), kRun);
 #pragma unroll
         for (int j = 0; j < kRun; ++j) {
             float z[kOwn];
@@ -711,8 +731,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         }
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) AR[k] = A[k];
-        wave_scan<false, false>(A, H, sh.left);
-        wave_scan<true, false>(AR, P, sh.right);
+        wave_scan<S, false, false>(A, H, sh.left);
+        wave_scan<S, true, false>(AR, P, sh.right);
     } else {
         bool cut = false;                                           // a sequence has ended in this run
 #pragma unroll
@@ -756,10 +776,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
             A[k] = first | outside ? 0.0f : m;
             AR[k] = cut ? 0.0f : m;
         }
-        wave_scan<false, true>(A, H, sh.left);
-        wave_scan<true, true>(AR, P, sh.right);
+        wave_scan<S, false, true>(A, H, sh.left);
+        wave_scan<S, true, true>(AR, P, sh.right);
     }
-    chain<true>(p, at.k, at.c0, sh, sh.right, [&] {
+    chain<S, true>(p, at.k, at.c0, sh, sh.right, [&] {
         if (some) (void)block_prefix<false, true>(sh.left);
         else (void)block_prefix<false, false>(sh.left);
     });
@@ -771,7 +791,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         part.settle(dy, at.c0);
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) in[k] = sh.carry[c - at.c0 + k];
-        enter<SOME>(AR, P, sh.right, in, q);
+        enter<S, SOME>(AR, P, sh.right, in, q);
         // the gradient of each state
         float d[kRun][kOwn];
 #pragma unroll
@@ -792,7 +812,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
         float h[kOwn];
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) in[k] = sh.kept[c - at.c0 + k];
-        enter<SOME>(A, H, sh.left, in, h);
+        enter<S, SOME>(A, H, sh.left, in, h);
         T *px = (T *)p.dx + part.t * p.lddx + c, *pz = (T *)p.dz + part.t * p.lddz + c;
 #pragma unroll
         for (int j = 0; j < kRun; ++j, px += p.lddx, pz += p.lddz) {
@@ -818,7 +838,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_backward(ScanArgs p)
     for (int j = 0; j < kRun; ++j) __asm__ volatile("" : "+v"(qx[j]));   // codes wait for the chain, not the values decoded above
     if (__builtin_expect(some, 0)) walk(std::true_type());
     else walk(std::false_type());
-    pass_on(p, blk, at.c0, p.dh_last, p.dh0);
+    pass_on<S>(p, blk, at.c0, p.dh_last, p.dh0);
 }
 
 // (64 requests x 2,048 channels: 3.3 us, a launch.)
@@ -853,9 +873,15 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
 static int64_t scan_blocks(int64_t tokens) { return (tokens + kBlock - 1) / kBlock; }
 static bool scan_sizes_ok(int64_t tokens, int64_t channels)
 {
-    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + kCh - 1) / kCh) < (1ll << 32) / kThreads;
+    return act_sizes_ok(tokens, channels) && scan_blocks(tokens) * ((channels + Wide::kCh - 1) / Wide::kCh) < (1ll << 32) / kThreads;
 }
 static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= cols && ld <= (1ll << 60) / rows; }
+
+// Narrow blocks as long as no compute unit gets two of them: a thread has half as much to do one after the other.  Forward and
+// backward, bf16: 64 tokens x 2,048 channels 20 us against 27, 1,000 x 512 28 against 35, 2,000 x 1,024 (128 wide blocks) 34
+// against 41; above that wide ones read whole lines of codes: 4,000 x 2,048 (512) 71 us narrow, 64 wide.  Without storing the kernel alone
+// gains 0 to 10 % and loses as much above.
+constexpr int64_t kNarrowMost = 128;
 
 // The chain's words behind one another in the workspace.
 struct ScanSpace {
@@ -867,12 +893,18 @@ static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
     const int64_t blocks = scan_blocks(tokens);
     if (blocks == 1) return ScanSpace{0, 0, 0};
-    return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + kCh - 1) / kCh};
+    return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + Narrow::kCh - 1) / Narrow::kCh};
 }
+static bool scan_narrow(int64_t tokens, int64_t channels)
+{
+    return scan_blocks(tokens) * ((channels + Wide::kCh - 1) / Wide::kCh) <= kNarrowMost;
+}
+template <typename S>
 static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, void (*kernel)(ScanArgs))
 {
     const ScanSpace w = scan_space(p.tokens, p.channels);
     p.blocks = scan_blocks(p.tokens);
+    p.groups = (p.channels + S::kCh - 1) / S::kCh;
     p.pairs = (uint64_t *)workspace;
     p.supers = p.pairs + w.pairs;
     p.counters = (uint32_t *)(p.pairs + w.words());
@@ -883,6 +915,19 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, 
     }
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(kThreads), lds, s, p);
     return hip_check(hipGetLastError());
+}
+template <typename S>
+static int forward_launch(hipStream_t s, ScanArgs &p, void *workspace, int dtype)
+{
+    return scan_launch<S>(s, p, workspace, 0, dtype == ZIPML_F32 ? k_scan_forward<float, S> : k_scan_forward<__bf16, S>);
+}
+template <typename S>
+static int backward_launch(hipStream_t s, ScanArgs &p, void *workspace, int dtype)
+{
+    const auto k = dtype == ZIPML_F32 ? k_scan_backward<float, S> : k_scan_backward<__bf16, S>;
+    static std::atomic<uint64_t> done[2];
+    if (allow_lds((const void *)k, sizeof(BackwardShared<S>), done[dtype == ZIPML_F32])) return ZIPML_ELAUNCH;
+    return scan_launch<S>(s, p, workspace, sizeof(BackwardShared<S>), k);
 }
 
 }  // namespace zipml
@@ -922,9 +967,8 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.h_last = h_last_dev;
     p.seed = seed; p.epoch = epoch; p.stream = kActStream + tag;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
-    p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    return scan_launch(s, p, workspace_dev, 0, dtype == ZIPML_F32 ? k_scan_forward<float> : k_scan_forward<__bf16>);
+    return scan_narrow(tokens, channels) ? forward_launch<Narrow>(s, p, workspace_dev, dtype) : forward_launch<Wide>(s, p, workspace_dev, dtype);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -952,12 +996,8 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.lddy = lddy; p.lddx = lddx; p.lddz = lddz;
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.dh_last = dh_last_dev; p.dh0 = dh0_dev;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
-    p.groups = (channels + kCh - 1) / kCh;
     hipStream_t s = entry_stream(stream);
-    const auto k = dtype == ZIPML_F32 ? k_scan_backward<float> : k_scan_backward<__bf16>;
-    static std::atomic<uint64_t> done[2];
-    if (allow_lds((const void *)k, sizeof(BackwardShared), done[dtype == ZIPML_F32])) return ZIPML_ELAUNCH;
-    return scan_launch(s, p, workspace_dev, sizeof(BackwardShared), k);
+    return scan_narrow(tokens, channels) ? backward_launch<Narrow>(s, p, workspace_dev, dtype) : backward_launch<Wide>(s, p, workspace_dev, dtype);
 }
 
 template <typename T>
