@@ -358,8 +358,10 @@ __global__ __launch_bounds__(256) void k_wgrad_sum(const float *__restrict__ par
 // the machine where dW is small, two or more workgroups to a compute unit; two teams on a tile where there are not that many.
 template <typename T> struct Shapes {
     static constexpr int BK = sizeof(T) == 4 ? 32 : 64;
-    typedef WgradShape<T, 256, 256, BK, 2, 4> Large;
-    typedef WgradShape<T, 128, 128, BK, 2, 4> Middle;
+    // 2 x 4 waves or 4 x 2: the three terms of fp32 dY make its side the dearer one to read from LDS (1 to 2 % either way)
+    static constexpr int WM = sizeof(T) == 4 ? 4 : 2, WN = 8 / WM;
+    typedef WgradShape<T, 256, 256, BK, WM, WN> Large;
+    typedef WgradShape<T, 128, 128, BK, WM, WN> Middle;
     typedef WgradShape<T, 64, 64, BK, 2, 2> Small;
     typedef WgradShape<T, 64, 64, BK, 2, 2, 2> Teams;
 };
