@@ -60,8 +60,8 @@ struct ScanArgs {
     float *h_last, *dh0;
     uint64_t *pairs;                       // [blocks][channels], then
     uint64_t *supers;                      // [blocks / kSuper][channels], then
-    uint32_t *counters;                    // [groups], side by side: a line to each has blocks start more evenly, and phases of
-                                           // neighbours then coincide (2 % slower at 32,768 tokens x 2,048 channels)
+    uint32_t *counters;                    // [groups], `apart` words apart
+    uint32_t apart;
     uint64_t seed;
     uint32_t epoch, stream;
     int64_t tokens, channels, n_seq, blocks, groups;
@@ -425,7 +425,7 @@ __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
     const uint32_t n = (uint32_t)p.groups, b = blockIdx.x, even = (uint32_t)p.blocks / 8 * 8 * n;
     const uint32_t g = (b < even ? b >> 3 : b - even) % n;
     if (p.blocks == 1) return Place{0, g * (int64_t)S::kCh};
-    if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g * p.apart, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     return Place{sh.ticket, g * (int64_t)S::kCh};
 }
@@ -883,6 +883,13 @@ static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= col
 // gains 0 to 10 % and loses as much above.
 constexpr int64_t kNarrowMost = 128;
 
+// A line of memory to each counter where the blocks start together, so that they get their tickets at once: up to 512, or up to
+// 1,024 of few groups (forward alone and with the backward pass, of the time with counters side by side: 8,192 tokens x 1,024
+// channels 0.83 and 0.88, 12,345 x 1,024 0.93 and 0.98, 131,072 x 128 0.94 and 0.97, 4,096 x 2,048 0.95 and 0.97).  Side by side
+// else: blocks that start less evenly do not pass through the same phase at once (5,120 x 2,048 1.08 and 1.06, 32,768 x 2,048 1.02).
+constexpr uint32_t kApart = 16;
+static bool start_together(int64_t blocks, int64_t groups) { return blocks * groups <= (groups < 32 ? 1024 : 512); }
+
 // The chain's words behind one another in the workspace.
 struct ScanSpace {
     int64_t pairs, supers, groups;
@@ -893,7 +900,7 @@ static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
     const int64_t blocks = scan_blocks(tokens);
     if (blocks == 1) return ScanSpace{0, 0, 0};
-    return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + Narrow::kCh - 1) / Narrow::kCh};
+    return ScanSpace{blocks * channels, blocks / kSuper * channels, (channels + Narrow::kCh - 1) / Narrow::kCh * kApart};
 }
 static bool scan_narrow(int64_t tokens, int64_t channels)
 {
@@ -908,6 +915,7 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, 
     p.pairs = (uint64_t *)workspace;
     p.supers = p.pairs + w.pairs;
     p.counters = (uint32_t *)(p.pairs + w.words());
+    p.apart = start_together(p.blocks, p.groups) ? kApart : 1;
     if (p.blocks > 1) {
         const int64_t n = w.words(), blocks = (n + 511) / 512;
         hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
