@@ -71,19 +71,23 @@ __device__ __forceinline__ void load8(const T *p, int64_t left, float (&v)[8])
         for (int k = 0; k < 8; ++k) v[k] = k < left ? (float)p[k] : 0.0f;
     }
 }
-// (rounded to T once, to the nearest)
-template <typename T>
+// (rounded to T once, to the nearest; THROUGH: past the caches)
+template <bool THROUGH = false, typename T>
 __device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8])
 {
+    auto put = [](auto *to, auto w) {
+        if constexpr (THROUGH) __builtin_nontemporal_store(w, to);
+        else *to = w;
+    };
     if (left >= 8) {
         if constexpr (sizeof(T) == 2) {
             bf16x8 o;
 #pragma unroll
             for (int k = 0; k < 8; ++k) o[k] = (__bf16)v[k];
-            *reinterpret_cast<bf16x8_any *>(p) = o;
+            put(reinterpret_cast<bf16x8_any *>(p), (bf16x8_any)o);
         } else {
-            reinterpret_cast<f32x4_any *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-            reinterpret_cast<f32x4_any *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+            put(reinterpret_cast<f32x4_any *>(p), (f32x4_any)f32x4{v[0], v[1], v[2], v[3]});
+            put(reinterpret_cast<f32x4_any *>(p) + 1, (f32x4_any)f32x4{v[4], v[5], v[6], v[7]});
         }
     } else {
 #pragma unroll

@@ -872,7 +872,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *__restrict__ x, int6
             gates(zv[k], f, g);
             v[k] = __builtin_fmaf(f, v[k], g * xv[k]);
         }
-        store8<float>(s, left, v);
+        store8(s, left, v);
     }
     store8(y + row * ldy + c, left, v);
 }

@@ -92,3 +92,17 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(alone[k], y) for y in both[k])
+
+
+def test_large_results_are_those_of_small_ones():
+    """More than 96 MiB are written another way; the values are the same, and the rows' padding stays as it was."""
+    rows, cols = 6200, 4099
+    x = torch.randn(rows, cols, device=DEV)
+    stored = torch.empty(zipml.act_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    zipml.act_encode(x, rows, cols, cols, 1, 2, 3, stored)
+    small = torch.full((rows, cols + 3), 9.0, dtype=BF16, device=DEV)
+    large = torch.full((rows, cols + 3), 9.0, device=DEV)
+    assert rows * cols * 2 < 96 << 20 < rows * cols * 4
+    zipml.act_decode(stored, rows, cols, small, cols + 3)
+    zipml.act_decode(stored, rows, cols, large, cols + 3)
+    assert torch.equal(small.float(), large) and (large[:, cols:] == 9.0).all()
