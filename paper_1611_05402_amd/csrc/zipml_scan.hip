@@ -174,8 +174,9 @@ struct Part {
         for (int j = 0; j < kRun; ++j) v[j].move(s);
     }
 };
-// THROUGH: past the L2, which then keeps what is read a second time (32,768 tokens x 2,048 channels, forward and backward: bf16
-// 310 us against 322, fp32 417 against 453; an elementwise kernel that reads the result next takes as long).
+// THROUGH: past the caches, so that the L2 keeps what is read a second time (32,768 tokens x 2,048 channels, forward and backward:
+// bf16 310 us against 322, fp32 417 against 454; 131,072 x 256 forward 57 against 58.7).  An elementwise kernel that reads the result
+// next loses some of it: together with the forward pass 0.99 to 1.04 of the time, with the backward pass 0.98 to 1.01.
 template <bool THROUGH, typename T>
 __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn])
 {
@@ -517,8 +518,8 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 
 // ---- forward -----------------------------------------------------------------------------------
 // What bounds it: storing the inputs, vector instructions (59 a value, 36 of them for the two codes; two thirds of the cycles at
-// 32,768 tokens x 2,048 channels, 165 us, 3.3 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
-// pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 57 us, 3.5 TB/s; a copy reaches 4.9).  128 tokens to
+// 32,768 tokens x 2,048 channels, 160 us, 3.4 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
+// pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 55 us, 3.7 TB/s; a copy reaches 4.9).  128 tokens to
 // a workgroup in place of 256: 241 and 98 us against 229 and 85 (an earlier form), the chain being twice as long.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
@@ -657,10 +658,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // LDS, each thread's own in its place; x is decoded and dy read a second time behind the chain (kept in registers, dy costs 2 %
 // at 32,768 tokens x 2,048 channels of bf16 and, with 69 registers spilled, 18 % of fp32).
 // What bounds it: as in the forward direction, what a block does one after the other, at two blocks to a compute unit (128
-// registers a thread; 32,768 tokens x 2,048 channels: 170 us, 3.2 TB/s; 386 MB are read for 273, the two halves of a line of
-// codes often by different XCDs).  With one block of 232 registers to a compute unit it took 321 us against 230 in the same form.  A block in
-// which sequences begin or end takes a path of its own from the pairs on: it is the rarer one, and the registers of both together
-// would not fit (stores and loads are counted together, so a register fetched back after a store waits for that store).
+// registers a thread; 32,768 tokens x 2,048 channels: 155 us, 3.5 TB/s).  With one block of 232 registers to a compute unit it took
+// 321 us against 230 in the same form.  A block in which sequences begin or end takes a path of its own from the pairs on: it is the
+// rarer one, and the registers of both together would not fit (stores and loads are counted together, so a register fetched back
+// after a store waits for that store).
 template <typename S>
 struct BackwardShared {
     ScanShared s;
