@@ -3,8 +3,9 @@
 // Both directions are scans of pairs: a run of tokens takes a state h to A h + B, and two runs one after the other
 // to (A2 A1) h + (A2 B1 + B2).  A workgroup owns 64 channels and a block of 256 tokens: sixteen lanes side by side take four
 // channels each (128 bytes of a bf16 row), 32 such rows of lanes eight tokens each, which a thread walks through in
-// registers (with few blocks 32 channels: eight lanes side by side, four tokens each).  Everything is read and written once: the rows of lanes are joined by shuffles and LDS, the blocks by a chain in
-// global memory while their tokens stay in registers.
+// registers (with few blocks 32 channels: eight lanes side by side, four tokens each).  Everything is read and written once,
+// but for dy in the backward pass: the rows of lanes are joined by shuffles and LDS, the blocks by a chain in global memory
+// while their tokens stay in registers.
 //
 // The chain.  A block publishes its pair, takes the pairs of the blocks before it up to the last multiple of kSuper and the
 // state there, which the block before that multiple has published, and so has the state that enters it.  What is
@@ -984,7 +985,8 @@ extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, 
     p.seed = seed; p.epoch = epoch; p.stream = kActStream + tag;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     hipStream_t s = entry_stream(stream);
-    return scan_narrow(tokens, channels) ? forward_launch<Narrow>(s, p, workspace_dev, dtype) : forward_launch<Wide>(s, p, workspace_dev, dtype);
+    return scan_narrow(tokens, channels) ? forward_launch<Narrow>(s, p, workspace_dev, dtype)
+                                         : forward_launch<Wide>(s, p, workspace_dev, dtype);
 }
 
 extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
@@ -1013,7 +1015,8 @@ extern "C" int zipml_scan_backward(void *stream, const void *act_x_dev, const vo
     p.seq_start = seq_start_dev; p.h0 = h0_dev; p.dh_last = dh_last_dev; p.dh0 = dh0_dev;
     p.tokens = tokens; p.channels = channels; p.n_seq = n_seq;
     hipStream_t s = entry_stream(stream);
-    return scan_narrow(tokens, channels) ? backward_launch<Narrow>(s, p, workspace_dev, dtype) : backward_launch<Wide>(s, p, workspace_dev, dtype);
+    return scan_narrow(tokens, channels) ? backward_launch<Narrow>(s, p, workspace_dev, dtype)
+                                         : backward_launch<Wide>(s, p, workspace_dev, dtype);
 }
 
 template <typename T>

@@ -6,11 +6,11 @@
 // memory, [token][column], and are read through the transposing LDS read, which hands every lane four tokens of one
 // column.  Which tokens a lane gets does not matter as long as both operands agree.
 //
-// What bounds it: at 16,384 tokens, 4,096 x 4,096, the power that the matrix cores draw at this rate (455 us alone, 1,210 TFLOP/s; repeated,
-// 460 to 540; the matrix instructions fill 63 % of the cycles; a library product of the same form, both operands
-// transposed, 1,083 TFLOP/s).  Small dW: LDS reads and the steps between barriers (65,536 tokens, 512 x 256: 31 us and 4 for
-// the joining of 32 ranges; the bytes alone would be 17).  fp32 dY at the first of these sizes: 1.30 ms,
-// the same rate of matrix instructions.
+// What bounds it: at 16,384 tokens, 4,096 x 4,096, the power that the matrix cores draw at this rate (455 us, 1,210 TFLOP/s; 440 to
+// 540 with the clock; the matrix instructions fill 63 % of the cycles; a library product of the same form, both operands
+// transposed, 1,083 TFLOP/s).  Small dW: LDS reads and the steps between barriers (65,536 tokens, 512 x 256: 30 us and 5 for
+// the joining of 32 ranges; the bytes alone would be 17).  fp32 dY at the first of these sizes: 1.30 ms, the same rate of matrix
+// instructions.
 //
 // bf16 dY: the products are exact and the sums fp32.  fp32 dY is split into three bf16 terms of 8 bits each, which
 // together are the value exactly, and takes three matrix instructions in place of one.
