@@ -87,3 +87,33 @@ def test_nan_and_infinity_stay_in_their_sequence(kind):
     for v in (dx, dz):
         assert np.isfinite(v[900:]).all() and (v[:3] == 0).all() and (v[1990:] == 0).all()
     assert np.isfinite(host(p.dh0)[1:]).all() and np.isnan(dz[101:900, 5]).all()
+
+
+def test_more_blocks_than_start_together():
+    forward_is_right("bf16", 270000, 5, "empty ones")
+
+
+def test_same_bits_every_time_and_in_a_graph():
+    """Captured once, replayed with the program's own work in between; every replay and every eager pass gives the same bits."""
+    p = Problem(9000, 290, [0, 100, 8500, 9000], "bf16")
+    y, (dx, dz) = p.forward(train=True).clone(), (v.clone() for v in p.backward())
+    t, c = p.tokens, p.channels
+    out, g = p.new(t, c, dtype=torch.bfloat16), p.new(t, p.ld, dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        zipml.scan_forward(p.x, p.ld, p.z, p.ld, t, c, out, c, p.ws, seq_start=p.start_dev, n_seq=3, h0=p.h0, h_last=p.last,
+                           act_x=p.ax, act_z=p.az, states=p.states, seed=5, epoch=3, tag=7)
+        zipml.scan_backward(p.ax, p.az, p.states, p.dy, c, t, c, g, p.ld, g[:, p.zat:], p.ld, p.ws,
+                            seq_start=p.start_dev, n_seq=3, h0=p.h0, dh_last=p.dh_last, dh0=p.dh0)
+    for _ in range(4):
+        out.fill_(3.0)
+        g.fill_(3.0)
+        p.ws.fill_(0xAB)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, y) and torch.equal(g[:, :c], dx) and torch.equal(g[:, p.zat:p.zat + c], dz)
+        assert torch.equal(p.forward(train=True), y)
+        ex, ez = p.backward()
+        assert torch.equal(ex, dx) and torch.equal(ez, dz)
