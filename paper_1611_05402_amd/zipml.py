@@ -143,14 +143,21 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_current_stream = None
+
+
 def _stream(stream=None):
     """The stream's handle; without one, that of the current device's current stream (asked for without building a
     Stream object, which costs more than a kernel launch)."""
-    import torch
+    global _current_stream
     if stream is not None:
         return stream.cuda_stream
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+    if _current_stream is None:
+        import torch
+        torch.cuda.current_device()                        # raises where there is no GPU
+        raw, device = (getattr(torch._C, f, None) for f in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        _current_stream = (lambda: raw(device())) if raw and device else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _current_stream()
 
 
 (KNOB_TARGET_WORKGROUPS, KNOB_NO_MATRIX_CORES, KNOB_CHUNK_SAMPLES, KNOB_MAX_REPLICAS, KNOB_ROWS_MIN_BATCH,
