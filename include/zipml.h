@@ -326,6 +326,8 @@ int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int64_t lddy, c
  * outside the tokens give undefined results, but nothing outside the arrays is touched.  Outputs must not overlap inputs.
  * h0_dev [n_seq][channels]: the states before the sequences, NULL for zeros.  h_last_dev [n_seq][channels], optional:
  * the states after them (an empty sequence hands its h0 on).  A NaN or an infinity stays within its sequence and channel.
+ * Gates that are nearly open cost no accuracy: what a state forgets is held to a few units of 2^-24 of itself, and a state is
+ * rounded to fp32 a few times a block of ZIPML_SCAN_BLOCK tokens, not at every token.
  * For training, act_x_dev, act_z_dev (zipml_act_bytes(tokens, channels) bytes each) and states_dev
  * ([ceil(tokens / ZIPML_SCAN_BLOCK)][channels], the state before each block of so many tokens) are written for
  * zipml_scan_backward: x as zipml_act_encode stores it with `tag`, z clamped to [-16, 16] and stored with tag + 1
@@ -353,7 +355,8 @@ int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_d
 
 /* One token of each of `rows` requests (serving): row r takes the state in row slots[r] of h_dev [n_slots][channels]
  * (row r without slots_dev) one step on, in place, and y gets it.  A row whose slot is outside 0..n_slots - 1 belongs to no
- * request: y = 0, no state is touched.  No two rows may name the same slot.  Asynchronous. */
+ * request: y = 0, no state is touched.  No two rows may name the same slot.  The state is rounded to fp32 at every token, so what
+ * a token changes in it by less than 2^-25 of it (1 - f < 2^-25: z > 17.3) is lost.  Asynchronous. */
 int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,
                     int64_t rows, int64_t channels, float *h_dev, int64_t n_slots, const int32_t *slots_dev,
                     void *y_dev, int64_t ldy);
