@@ -315,15 +315,61 @@ def unpack_codes(packed, copy, n, d, bits, codes_out, stream=None):
                                     _ptr(codes_out)), "zipml_unpack_codes")
 
 
-_DTYPES: dict = {}
+class _Codes(dict):
+    """ZIPML_F32 or ZIPML_BF16 for a torch type, -1 for others; torch is not imported before the first is asked for."""
+
+    def __missing__(self, kind):
+        import torch
+        self.update({torch.float32: F32, torch.bfloat16: BF16})
+        return self.get(kind, -1)
+
+
+class _Kinds(dict):
+    def __missing__(self, name):
+        import torch
+        self[name] = getattr(torch, name)
+        return self[name]
+
+
+_CODES, _KINDS, _ONE = _Codes(), _Kinds(), (1,)
 
 
 def _dtype(t) -> int:
     """ZIPML_F32 or ZIPML_BF16 for a tensor (or a torch dtype); the library refuses -1."""
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16})
-    return _DTYPES.get(getattr(t, "dtype", t), -1)
+    return _CODES[getattr(t, "dtype", t)]
+
+
+def _same_dtype(a, b, c) -> int:
+    """The common type of x, z and y (or of the gradients); -1, which the library refuses, if they differ."""
+    return _dtype(a) if a.dtype == b.dtype == c.dtype else -1
+
+
+def _rows(where, a, b=None, c=None) -> int:
+    """The common type of one tensor or three whose rows lie a stride of the caller's apart (-1, which the library refuses, if they
+    differ).  The values of a row have to lie side by side: the library sees no stride between them."""
+    if a is None:
+        return -1
+    kind = a.dtype
+    if a.stride()[-1:] == _ONE and (b is None or (b.stride()[-1:] == _ONE and c.stride()[-1:] == _ONE and b.dtype is kind
+                                                  and c.dtype is kind)):
+        return _CODES[kind]
+    tensors = [t for t in (a, b, c) if t is not None]
+    for t in tensors:
+        s = t.stride()
+        if s and s[-1] != 1 and t.shape[-1] > 1:
+            raise ZipmlError(EINVAL, f"{where}: the values of a row lie {s[-1]} elements apart, not 1")
+    return _CODES[kind] if b is None else _same_dtype(a, b, c)
+
+
+def _array(where, name, t, kind=None):
+    """The address of an array that is read or written without strides, of one type (None: bytes, whatever they are called); None if
+    there is none.  Another type's values would be read past their end."""
+    if t is None:
+        return None
+    if not t.is_contiguous() or (kind is not None and t.dtype is not _KINDS[kind]):
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be contiguous{' ' + kind if kind else ''}, not {t.dtype} with "
+                                 f"strides {t.stride()}")
+    return t.data_ptr()
 
 
 def act_bytes(rows: int, cols: int) -> int:
@@ -332,13 +378,15 @@ def act_bytes(rows: int, cols: int) -> int:
 
 def act_encode(x, rows, cols, ldx, seed, epoch, tag, act, stream=None):
     """Stores x (fp32 or bf16) in 8 bits; `act`: act_bytes(rows, cols) bytes."""
-    _check(lib().zipml_act_encode(_stream(stream), _ptr(x), _dtype(x), rows, cols, ldx, seed, epoch, tag,
-                                  _ptr(act)), "zipml_act_encode")
+    w = "zipml_act_encode"
+    _check(lib().zipml_act_encode(_stream(stream), _ptr(x), _rows(w, x), rows, cols, ldx, seed, epoch, tag,
+                                  _array(w, "act", act)), w)
 
 
 def act_decode(act, rows, cols, out, ldo, stream=None):
-    _check(lib().zipml_act_decode(_stream(stream), _ptr(act), rows, cols, _ptr(out), _dtype(out), ldo),
-           "zipml_act_decode")
+    """The values that `act` stands for, in out (fp32 or bf16)."""
+    w = "zipml_act_decode"
+    _check(lib().zipml_act_decode(_stream(stream), _array(w, "act", act), rows, cols, _ptr(out), _rows(w, out), ldo), w)
 
 
 def act_wgrad_workspace_bytes(rows: int, d_out: int, d_in: int, dtype) -> int:
@@ -348,38 +396,42 @@ def act_wgrad_workspace_bytes(rows: int, d_out: int, d_in: int, dtype) -> int:
 
 def act_wgrad(dy, lddy, act, rows, d_out, d_in, dw, lddw, workspace, *, flags=0, stream=None):
     """dw = dy^T Q(X) (fp32) from the stored X; flags: WGRAD_ADD adds to dw."""
-    _check(lib().zipml_act_wgrad(_stream(stream), _ptr(dy), _dtype(dy), lddy, _ptr(act), rows, d_out, d_in, flags,
-                                 _ptr(dw), lddw, _ptr(workspace), workspace.numel() * workspace.element_size()),
-           "zipml_act_wgrad")
+    w = "zipml_act_wgrad"
+    if _rows(w, dw) != F32 and dw is not None:
+        raise ZipmlError(EINVAL, f"{w}: dw has to be float32, not {dw.dtype}")
+    _check(lib().zipml_act_wgrad(_stream(stream), _ptr(dy), _rows(w, dy), lddy, _array(w, "act", act), rows, d_out, d_in, flags,
+                                 _ptr(dw), lddw, workspace.data_ptr(), workspace.nbytes), w)
 
 
 def scan_workspace_bytes(tokens: int, channels: int) -> int:
     return int(lib().zipml_scan_workspace_bytes(tokens, channels))
 
 
-def _same_dtype(a, b, c) -> int:
-    """The common type of x, z and y (or of the gradients); -1, which the library refuses, if they differ."""
-    return _dtype(a) if a.dtype == b.dtype == c.dtype else -1
-
-
 def scan_forward(x, ldx, z, ldz, tokens, channels, y, ldy, workspace, *, seq_start=None, n_seq=1, h0=None, h_last=None,
                  act_x=None, act_z=None, states=None, seed=0, epoch=0, tag=0, stream=None):
-    """The recurrence over packed sequences; with act_x, act_z and states, its inputs are stored for scan_backward."""
-    _check(lib().zipml_scan_forward(_stream(stream), _ptr(x), ldx, _ptr(z), ldz, _same_dtype(x, z, y), tokens, channels,
-                                    _ptr(seq_start), n_seq, _ptr(h0), _ptr(y), ldy, _ptr(h_last), _ptr(act_x),
-                                    _ptr(act_z), _ptr(states), seed, epoch, tag, _ptr(workspace),
-                                    workspace.numel() * workspace.element_size()), "zipml_scan_forward")
+    """The recurrence over packed sequences; with act_x, act_z and states, its inputs are stored for scan_backward.
+    seq_start: n_seq + 1 int64 offsets; h0, h_last, states: fp32."""
+    w = "zipml_scan_forward"
+    _check(lib().zipml_scan_forward(_stream(stream), x.data_ptr(), ldx, z.data_ptr(), ldz, _rows(w, x, z, y), tokens, channels,
+                                    _array(w, "seq_start", seq_start, "int64"), n_seq, _array(w, "h0", h0, "float32"),
+                                    y.data_ptr(), ldy, _array(w, "h_last", h_last, "float32"), _array(w, "act_x", act_x),
+                                    _array(w, "act_z", act_z), _array(w, "states", states, "float32"), seed, epoch, tag,
+                                    workspace.data_ptr(), workspace.nbytes), w)
 
 
 def scan_backward(act_x, act_z, states, dy, lddy, tokens, channels, dx, lddx, dz, lddz, workspace, *, seq_start=None,
                   n_seq=1, h0=None, dh_last=None, dh0=None, stream=None):
-    _check(lib().zipml_scan_backward(_stream(stream), _ptr(act_x), _ptr(act_z), _ptr(states), _ptr(dy), lddy,
-                                     _same_dtype(dy, dx, dz), tokens, channels, _ptr(seq_start), n_seq, _ptr(h0),
-                                     _ptr(dh_last), _ptr(dx), lddx, _ptr(dz), lddz, _ptr(dh0), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size()), "zipml_scan_backward")
+    """Gradients dx, dz, dh0 from what scan_forward stored.  seq_start: n_seq + 1 int64 offsets; h0, dh_last, dh0, states: fp32."""
+    w = "zipml_scan_backward"
+    _check(lib().zipml_scan_backward(_stream(stream), _array(w, "act_x", act_x), _array(w, "act_z", act_z),
+                                     _array(w, "states", states, "float32"), dy.data_ptr(), lddy, _rows(w, dy, dx, dz), tokens,
+                                     channels, _array(w, "seq_start", seq_start, "int64"), n_seq, _array(w, "h0", h0, "float32"),
+                                     _array(w, "dh_last", dh_last, "float32"), dx.data_ptr(), lddx, dz.data_ptr(), lddz,
+                                     _array(w, "dh0", dh0, "float32"), workspace.data_ptr(), workspace.nbytes), w)
 
 
 def scan_step(x, ldx, z, ldz, rows, channels, h, n_slots, y, ldy, *, slots=None, stream=None):
-    """One token of each request; `slots`: int32 rows of the states h [n_slots][channels], which are updated."""
-    _check(lib().zipml_scan_step(_stream(stream), _ptr(x), ldx, _ptr(z), ldz, _same_dtype(x, z, y), rows, channels,
-                                 _ptr(h), n_slots, _ptr(slots), _ptr(y), ldy), "zipml_scan_step")
+    """One token of each request; `slots`: int32 rows of the states h [n_slots][channels] (fp32), which are updated."""
+    w = "zipml_scan_step"
+    _check(lib().zipml_scan_step(_stream(stream), x.data_ptr(), ldx, z.data_ptr(), ldz, _rows(w, x, z, y), rows, channels,
+                                 _array(w, "h", h, "float32"), n_slots, _array(w, "slots", slots, "int32"), y.data_ptr(), ldy), w)
