@@ -13,8 +13,8 @@
  *     (zipml_loss keeps some pinned host memory of its own, see there).  Pointers named
  *     *_host are host pointers.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All device work is
- *     enqueued on it.  Calls that return a host value (zipml_loss, zipml_sgd_status, the OPTIMAL
- *     mode of zipml_levels) synchronise that stream; every other call is asynchronous.
+ *     enqueued on it.  Calls that return a host value (zipml_loss, zipml_sgd_status, zipml_scan_status,
+ *     the OPTIMAL mode of zipml_levels) synchronise that stream; every other call is asynchronous.
  *   - Every call returns ZIPML_OK (0) or a negative error code; nothing aborts or throws across the
  *     boundary.  Argument errors are detected before any work is enqueued.
  *   - A is row-major fp32 with leading dimension lda >= d.  Level tables are [d][2^bits] fp32,
@@ -45,7 +45,7 @@ extern "C" {
 #define ZIPML_EWORKSPACE   -4   /* workspace missing or smaller than zipml_workspace_bytes()      */
 #define ZIPML_ELAUNCH      -5   /* the HIP runtime refused a launch or copy                       */
 #define ZIPML_EUNSUPPORTED -6   /* valid request that this build does not implement               */
-#define ZIPML_ETIMEOUT     -7   /* a grid-wide wait inside the epoch kernel gave up               */
+#define ZIPML_ETIMEOUT     -7   /* a wait inside an epoch kernel or a recurrence gave up          */
 
 /* ---- modes and flags ---------------------------------------------------------------------- */
 #define ZIPML_UNIFORM 0          /* 2^bits evenly spaced levels on [lo_j, hi_j]    (Sec. 2.1)     */
@@ -353,6 +353,11 @@ int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_d
                         const float *dh_last_dev, void *dx_dev, int64_t lddx, void *dz_dev, int64_t lddz,
                         float *dh0_dev, void *workspace_dev, size_t workspace_bytes);
 
+/* Waits for the stream and returns the status word that the last zipml_scan_forward or zipml_scan_backward left in this workspace:
+ * ZIPML_OK or ZIPML_ETIMEOUT.  Blocks of a call wait for the states that enter them; blocks that a block waits for always run, but
+ * no wait lasts longer than some seconds (ZIPML_KNOB_SPIN_LIMIT): past that what depends on it is NaN and the status says so. */
+int zipml_scan_status(void *stream, const void *workspace_dev, size_t workspace_bytes);
+
 /* One token of each of `rows` requests (serving): row r takes the state in row slots[r] of h_dev [n_slots][channels]
  * (row r without slots_dev) one step on, in place, and y gets it.  A row whose slot is outside 0..n_slots - 1 belongs to no
  * request: y = 0, no state is touched.  No two rows may name the same slot.  The state is rounded to fp32 at every token, so what
@@ -409,7 +414,8 @@ int zipml_debug_stream(void *stream, const void *src_dev, void *dst_dev, size_t 
                                             value keeps the integer kernel; 101, 102: the 4-bit floating-point
                                             dot pass with tiles of 64, 128 samples)                      */
 #define ZIPML_KNOB_ROWS_WORKGROUPS   6  /* its number of workgroups                                     */
-#define ZIPML_KNOB_SPIN_LIMIT        7  /* polls before a device-wide wait gives up (0: at once)        */
+#define ZIPML_KNOB_SPIN_LIMIT        7  /* polls before a device-wide wait or a recurrence's gives up
+                                            (0: at once)                                              */
 #define ZIPML_KNOB_HOST_DP           8  /* 1: the dynamic program of zipml_levels runs on the host     */
 #define ZIPML_KNOB_HIST_FEATURES     9  /* features per workgroup of the bin-moment kernel              */
 #define ZIPML_KNOB_STORE_EXCHANGE_MIN 10 /* smallest (workgroups x samples of one exchange) from which

@@ -67,6 +67,8 @@ struct ScanArgs {
     const int64_t *seq_start;              // n_seq + 1 offsets, or NULL: one sequence
     const float *h0, *dh_last;
     float *h_last, *dh0;
+    int *status;                           // ZIPML_OK, or ZIPML_ETIMEOUT where a wait gave up
+    uint32_t spin_limit;                   // polls before one does
     uint64_t *pairs;                       // [blocks][channels], then
     uint64_t *supers;                      // [blocks / kSuper][channels], then
     uint32_t *counters;                    // [groups], `apart` words apart
@@ -404,15 +406,18 @@ __device__ __forceinline__ void enter(const float (&A)[kOwn], const float (&B)[k
 
 constexpr uint64_t kAbsent = ~0ull;
 __device__ __forceinline__ uint64_t word(float a, float b) { return (uint64_t)as_u32(a) << 32 | as_u32(b); }
-// The word once it is there.  (The limit is never reached; a NaN would tell.)
-__device__ __forceinline__ uint64_t await(const uint64_t *p)
+// The word once it is there.  Blocks are handed out in the chain's order, so it comes; still no wait is without a limit (kSpinLimit polls,
+// some seconds): at it, the states that depend on the word are NaN, and the status word says so.
+constexpr uint32_t kSpinLimit = 1u << 22;
+__device__ __forceinline__ uint64_t await(const ScanArgs &p, const uint64_t *from)
 {
-    uint64_t w = load_dev(p);
-    for (int n = 0; w == kAbsent && n < (1 << 22); ++n) {
+    uint64_t w = load_dev(from);
+    for (uint32_t n = 0; w == kAbsent && n < p.spin_limit; ++n) {
         __builtin_amdgcn_s_sleep(1);
-        w = load_dev(p);
+        w = load_dev(from);
     }
-    return w == kAbsent ? word(0.0f, __builtin_nanf("")) : w;
+    if (__builtin_expect(w == kAbsent, 0)) store_dev(p.status, (int)ZIPML_ETIMEOUT);
+    return w;                              // (all ones is a pair of NaNs)
 }
 
 // From the waves' pairs to the state that enters block `k` of the chain (k counts in the direction of the scan), in sh.carry; the
@@ -441,7 +446,7 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
     float a = 1.0f, b = 0.0f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        if (w[i] == kAbsent) w[i] = await(p.pairs + at(from + i));
+        if (w[i] == kAbsent) w[i] = await(p, p.pairs + at(from + i));
         const float wa = as_f32((uint32_t)(w[i] >> 32)), wb = as_f32((uint32_t)w[i]);
         b = join<true>(wa, b, wb);
         a = times<true>(wa, a);
@@ -452,7 +457,7 @@ __device__ __forceinline__ void chain(const ScanArgs &p, int64_t k, int64_t c0, 
         float2 q[kWaves];
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) q[i] = sh.blocks[i][lane];
-        float h = base > 0 && live ? as_f32((uint32_t)await(p.supers + (base / kSuper - 1) * p.channels + c)) : 0.0f;
+        float h = base > 0 && live ? as_f32((uint32_t)await(p, p.supers + (base / kSuper - 1) * p.channels + c)) : 0.0f;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) h = join<true>(q[i].x, h, q[i].y);
         sh.carry[lane] = h;
@@ -471,15 +476,19 @@ __device__ __forceinline__ Place take(const ScanArgs &p, ScanShared &sh)
 {
     const uint32_t n = (uint32_t)p.groups, b = blockIdx.x, even = (uint32_t)p.blocks / 8 * 8 * n;
     const uint32_t g = (b < even ? b >> 3 : b - even) % n;
-    if (p.blocks == 1) return Place{0, g * (int64_t)S::kCh};
+    if (p.blocks == 1) {
+        if (b == 0 && threadIdx.x == 0) *p.status = ZIPML_OK;
+        return Place{0, g * (int64_t)S::kCh};
+    }
     if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(p.counters + g * p.apart, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     return Place{sh.ticket, g * (int64_t)S::kCh};
 }
 
-// The words (an even number of them) and counters of a chain before it starts: a launch, 2 to 5 us.
-__global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, uint32_t *counters, int64_t groups)
+// The words (an even number of them), counters and status of a chain before it starts: a launch, 2 to 5 us.
+__global__ __launch_bounds__(256) void k_scan_clear(uint64_t *words, int64_t n, uint32_t *counters, int64_t groups, int *status)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *status = ZIPML_OK;
     const int64_t step = (int64_t)gridDim.x * 256, i0 = blockIdx.x * 256ll + threadIdx.x;
     u32x4 *w = reinterpret_cast<u32x4 *>(words);
     for (int64_t i = i0; i < n / 2; i += step) w[i] = u32x4{~0u, ~0u, ~0u, ~0u};
@@ -941,11 +950,12 @@ constexpr int64_t kNarrowMost = 128;
 constexpr uint32_t kApart = 16;
 static bool start_together(int64_t blocks, int64_t groups) { return blocks * groups <= (groups < 32 ? 1024 : 512); }
 
-// The chain's words behind one another in the workspace.
+// The status word and the chain's words behind one another in the workspace.
 struct ScanSpace {
+    static constexpr size_t kStatusBytes = 256;
     int64_t pairs, supers, groups;
     int64_t words() const { return (pairs + supers + 1) / 2 * 2; }
-    size_t bytes() const { return (size_t)words() * 8 + (size_t)groups * 4; }
+    size_t bytes() const { return kStatusBytes + (size_t)words() * 8 + (size_t)groups * 4; }
 };
 static ScanSpace scan_space(int64_t tokens, int64_t channels)
 {
@@ -963,14 +973,17 @@ static int scan_launch(hipStream_t s, ScanArgs &p, void *workspace, size_t lds, 
     const ScanSpace w = scan_space(p.tokens, p.channels);
     p.blocks = scan_blocks(p.tokens);
     p.groups = (p.channels + S::kCh - 1) / S::kCh;
-    p.pairs = (uint64_t *)workspace;
+    p.status = (int *)workspace;
+    p.spin_limit = kSpinLimit;
+    if (const long long v = knob(ZIPML_KNOB_SPIN_LIMIT); v >= 0 && v <= (long long)kSpinLimit) p.spin_limit = (uint32_t)v;
+    p.pairs = (uint64_t *)((char *)workspace + ScanSpace::kStatusBytes);
     p.supers = p.pairs + w.pairs;
     p.counters = (uint32_t *)(p.pairs + w.words());
     p.apart = start_together(p.blocks, p.groups) ? kApart : 1;
     if (p.blocks > 1) {
         const int64_t n = w.words(), blocks = (n + 511) / 512;
         hipLaunchKernelGGL(k_scan_clear, dim3((uint32_t)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s, p.pairs, n, p.counters,
-                           w.groups);
+                           w.groups, p.status);
     }
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.blocks * p.groups)), dim3(kThreads), lds, s, p);
     return hip_check(hipGetLastError());
@@ -996,8 +1009,18 @@ using namespace zipml;
 extern "C" size_t zipml_scan_workspace_bytes(int64_t tokens, int64_t channels)
 {
     if (!scan_sizes_ok(tokens, channels)) return 0;
-    const size_t b = scan_space(tokens, channels).bytes();
-    return b < 256 ? 256 : b;
+    return scan_space(tokens, channels).bytes();
+}
+
+extern "C" int zipml_scan_status(void *stream, const void *workspace_dev, size_t workspace_bytes)
+{
+    if (!workspace_dev || workspace_bytes < ScanSpace::kStatusBytes) return ZIPML_EWORKSPACE;
+    if (!aligned16(workspace_dev)) return ZIPML_EALIGN;
+    int st = 0;
+    hipStream_t s = entry_stream(stream);
+    if (HIP_FAILED(hipMemcpyAsync(&st, workspace_dev, sizeof(int), hipMemcpyDeviceToHost, s))) return ZIPML_ELAUNCH;
+    if (HIP_FAILED(hipStreamSynchronize(s))) return ZIPML_ELAUNCH;
+    return st;
 }
 
 extern "C" int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,

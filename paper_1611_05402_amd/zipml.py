@@ -32,7 +32,8 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_loss", "zipml_debug_stream", "zipml_debug_set", "zipml_sgd_epoch_compact",
            "zipml_unpack_codes", "zipml_debug_step", "zipml_act_bytes", "zipml_act_encode",
            "zipml_act_decode", "zipml_act_wgrad_workspace_bytes", "zipml_act_wgrad",
-           "zipml_scan_workspace_bytes", "zipml_scan_forward", "zipml_scan_backward", "zipml_scan_step"]
+           "zipml_scan_workspace_bytes", "zipml_scan_forward", "zipml_scan_backward", "zipml_scan_status",
+           "zipml_scan_step"]
 
 
 class ZipmlError(RuntimeError):
@@ -124,6 +125,8 @@ def lib() -> C.CDLL:
         L.zipml_scan_backward.restype = i32
         L.zipml_scan_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp,
                                           vp, sz]
+        L.zipml_scan_status.restype = i32
+        L.zipml_scan_status.argtypes = [vp, vp, sz]
         L.zipml_scan_step.restype = i32
         L.zipml_scan_step.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, i64]
         _lib = L
@@ -428,6 +431,11 @@ def scan_backward(act_x, act_z, states, dy, lddy, tokens, channels, dx, lddx, dz
                                      channels, _array(w, "seq_start", seq_start, "int64"), n_seq, _array(w, "h0", h0, "float32"),
                                      _array(w, "dh_last", dh_last, "float32"), dx.data_ptr(), lddx, dz.data_ptr(), lddz,
                                      _array(w, "dh0", dh0, "float32"), workspace.data_ptr(), workspace.nbytes), w)
+
+
+def scan_status(workspace, stream=None) -> int:
+    """OK, or ETIMEOUT where a wait of the last scan call on this workspace gave up; waits for the stream."""
+    return int(lib().zipml_scan_status(_stream(stream), _ptr(workspace), workspace.nbytes))
 
 
 def scan_step(x, ldx, z, ldz, rows, channels, h, n_slots, y, ldy, *, slots=None, stream=None):
