@@ -308,7 +308,8 @@ int zipml_act_decode(void *stream, const void *act_dev, int64_t rows, int64_t co
  *   dW[o][i] = sum_t dY[t][o] Q(X)[t][i],   or dW += that with ZIPML_WGRAD_ADD,
  * the estimator of eq. (5) for a layer: unbiased, as Q's draws are independent of dY given X.  dY_dev: rows x d_out,
  * lddy >= d_out; act_dev: rows x d_in as zipml_act_encode wrote it; dw_dev: fp32, d_out rows of d_in values, lddw >=
- * d_in apart.  Products are exact (fp32 dY is taken as three bf16 terms), sums are in fp32, in an order that depends on
+ * d_in apart.  Products are exact (fp32 dY is taken as three bf16 terms, which hold values of 2^-110 and more exactly and smaller ones
+ * to 2^-133; a bf16 dY is taken as it is), sums are in fp32, in an order that depends on
  * the sizes alone: the same call gives the same bits.  A NaN group of X makes its columns of dW NaN.  d_out and d_in
  * up to 2^24.  Asynchronous. */
 #define ZIPML_WGRAD_ADD 1

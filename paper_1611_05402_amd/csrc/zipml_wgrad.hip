@@ -12,8 +12,9 @@
 // the joining of 32 ranges; the bytes alone would be 17).  fp32 dY at the first of these sizes: 1.30 ms, the same rate of matrix
 // instructions.
 //
-// bf16 dY: the products are exact and the sums fp32.  fp32 dY is split into three bf16 terms of 8 bits each, which
-// together are the value exactly, and takes three matrix instructions in place of one.
+// bf16 dY: the products are exact and the sums fp32.  fp32 dY is split into three bf16 terms of 8 bits each and takes three matrix
+// instructions in place of one.  Together the terms are the value exactly from 2^-110 on; below that its bits under 2^-133, where bf16
+// ends, are left out.
 #include "zipml_act.h"
 
 namespace zipml {
@@ -92,7 +93,8 @@ template <> struct Raw8<__bf16> { u32x4 w; };
 template <> struct Raw8<float> { u32x4 w, w2; };
 
 // Four fp32 values as three bf16 terms each; the first takes the upper 8 bits of the mantissa by truncation, so that it
-// never overflows, the second those of the rest, the third what is left (an infinity or a NaN has only the first).
+// never overflows, the second those of the rest, the third what is left down to 2^-133 (an infinity or a NaN has only the
+// first).
 __device__ __forceinline__ void split4(u32x4 v, uint32_t (&plane)[3][2])
 {
 #pragma unroll
