@@ -321,8 +321,9 @@ int zipml_act_wgrad(void *stream, const void *dy_dev, int dtype, int64_t lddy, c
 /* Gated linear recurrence over packed sequences:
  *   f_t = sigmoid(z_t),  h_t = f_t h_{t-1} + (1 - f_t) x_t,  y_t = h_t,  channel by channel, states in fp32.
  * x_dev, z_dev, y_dev: tokens x channels, dtype ZIPML_F32 or ZIPML_BF16, rows ld* >= channels apart (so x and z may be
- * two halves of one projection).  seq_start_dev: n_seq + 1 ascending offsets; sequence s holds the tokens from
- * seq_start[s] up to seq_start[s + 1], none if they are equal; NULL with n_seq = 1: all tokens are one sequence.
+ * two halves of one projection, the second of which begins at a multiple of 8 bf16 or 4 fp32 values: the first value of each
+ * tensor has to be 16-byte aligned, as everywhere, its rows need not be).  seq_start_dev: n_seq + 1 ascending offsets; sequence s
+ * holds the tokens from seq_start[s] up to seq_start[s + 1], none if they are equal; NULL with n_seq = 1: all tokens are one sequence.
  * Tokens in no sequence (before the first offset, from the last one on) give y = 0.  Offsets that do not ascend or lie
  * outside the tokens give undefined results, but nothing outside the arrays is touched.  Outputs must not overlap inputs.
  * h0_dev [n_seq][channels]: the states before the sequences, NULL for zeros.  h_last_dev [n_seq][channels], optional:
@@ -347,7 +348,10 @@ int zipml_scan_forward(void *stream, const void *x_dev, int64_t ldx, const void 
  * with f = sigmoid(Q(z)) and the states formed again from Q(x), Q(z): from h0 at a sequence's start and from states_dev
  * at the start of each block of ZIPML_SCAN_BLOCK tokens.  dy, dx, dz: dtype, any rows apart; dh_last_dev (NULL for zeros)
  * and dh0_dev (optional): [n_seq][channels].  Tokens in no sequence give dx = dz = 0; an empty sequence's dh0 is its
- * dh_last.  seq_start_dev, n_seq, h0_dev and the sizes as in the forward pass.  Asynchronous. */
+ * dh_last.  seq_start_dev, n_seq, h0_dev and the sizes as in the forward pass.  Outputs must not overlap inputs: dy is read twice.
+ * x and z are stored 32 channels to a step, so a NaN or an infinity of x (a NaN of z) in one channel reaches the 32 of its group: dz
+ * of that token and, through the states, of later ones up to the end of the block of ZIPML_SCAN_BLOCK (in its own channel up to the
+ * sequence's end); z's also dx and dz of that token and of all earlier ones of its sequence, and dh0.  Asynchronous. */
 int zipml_scan_backward(void *stream, const void *act_x_dev, const void *act_z_dev, const float *states_dev,
                         const void *dy_dev, int64_t lddy, int dtype, int64_t tokens, int64_t channels,
                         const int64_t *seq_start_dev, int64_t n_seq, const float *h0_dev,

@@ -4,7 +4,7 @@
 // floor(v * 2^-e + u), u uniform on the odd multiples of 2^-17 in (0, 1).  With a power of two as the step a
 // code times its step has at most 7 significant bits, so it is a bf16 (and fp32) number exactly: what reads the
 // codes may feed the bf16 matrix cores without rounding again.  Against a step of max / 127 this costs a step
-// up to twice as large, 1.5 bits of 255 levels at worst and about half a bit on average.
+// up to twice as large, one bit at worst and half a bit on average (over magnitudes spread evenly in the logarithm).
 #pragma once
 #include "zipml_device.h"
 #include "zipml_host.h"

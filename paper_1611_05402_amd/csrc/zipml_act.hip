@@ -8,8 +8,8 @@ namespace zipml {
 constexpr int kRows = 4;
 
 // Both kernels stream; every byte is moved once.  16,384 x 4,096 bf16: storing 203 MB in 36 to 41 us (4.9 to 5.6 TB/s; its generator, ten
-// rounds for eight values, keeps the vector units busy for more than half of that), restoring 203 MB in 31 us (the codes
-// come out of the cache that the storing left them in).  Small calls are bound by their launch: 2.5 and 1.6 us for 2,048 values.
+// rounds for eight values, keeps the vector units busy for more than half of that), restoring 203 MB in 30 us (the codes
+// come out of the cache that the storing left them in).  fp32: storing 336 MB in 61 us, restoring to fp32 110 (3.1 TB/s).  Small calls are bound by their launch: 2.5 and 1.6 us for 2,048 values.
 // Threads side by side in x take the units of eight columns of a row, those side by side in y rows; a workgroup takes tx * 8
 // columns of 256 / tx * kRows rows at a time.
 struct ActGrid {

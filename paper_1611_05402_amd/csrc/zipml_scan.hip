@@ -23,7 +23,7 @@
 // state at z = 12 is off by 0.3 to 0.6 % after 100,000 tokens, and at z = 17 nothing is ever forgotten.  So what a run forgets,
 // D = 1 - A, is summed beside A, each token's 1 - f times the A before it, from the tokens up to the block: all terms are positive, so D
 // keeps its relative accuracy, and A = 1 - D is rounded once where D is the smaller one.  A state is then off by 2^-25 of itself a
-// block, as from its own rounding.  This costs 0 to 5 % (131,072 x 256 forward 60 us against 57.6, 32,768 x 2,048 forward and
+// block, as from its own rounding.  This costs 0 to 6 % (131,072 x 256 forward 60 us against 57.6, 32,768 x 2,048 forward and
 // backward bf16 316 against 309, fp32 419 either way).
 #include "zipml_act.h"
 
@@ -36,7 +36,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kMostCh = 64;
 constexpr float kTiny = 1.17549435e-38f;
-constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1
+constexpr float kZMax = 16.0f;             // gates are stored clamped to +-kZMax: sigmoid(16) is 1 - 2^-23.1 (a group with one there has step 1/4)
 static_assert(kSuper % kWaves == 0, "the waves share the pairs of kSuper blocks");
 static_assert(kThreads == 2 * kBlock, "a thread for each token of x and z");
 
@@ -189,9 +189,10 @@ struct Part {
         for (int j = 0; j < kRun; ++j) v[j].move(s);
     }
 };
-// THROUGH: past the caches, so that the L2 keeps what is read a second time (32,768 tokens x 2,048 channels, forward and backward:
-// bf16 310 us against 322, fp32 417 against 454; 131,072 x 256 forward 57 against 58.7).  An elementwise kernel that reads the result
-// next loses some of it: together with the forward pass 0.99 to 1.04 of the time, with the backward pass 0.98 to 1.01.
+// THROUGH: past the caches, which leaves them more of what is read a second time: of dy in the backward pass half to three quarters,
+// by the bytes that leave the L2 (when this was measured, 32,768 tokens x 2,048 channels, forward and backward: bf16 310 us against
+// 322, fp32 417 against 454; 131,072 x 256 forward 57 against 58.7).  An elementwise kernel that reads the result next loses some of it:
+// together with the forward pass 0.99 to 1.04 of the time, with the backward pass 0.98 to 1.01.
 template <bool THROUGH, typename T>
 __device__ __forceinline__ void store4(T *p, int64_t left, const float (&v)[kOwn])
 {
@@ -565,9 +566,9 @@ __device__ __forceinline__ void decode4(uint32_t codes, float step, float (&v)[k
 }
 
 // ---- forward -----------------------------------------------------------------------------------
-// What bounds it: storing the inputs, vector instructions (59 a value, 36 of them for the two codes; two thirds of the cycles at
-// 32,768 tokens x 2,048 channels, 160 us, 3.4 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
-// pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 55 us, 3.7 TB/s; a copy reaches 4.9).  128 tokens to
+// What bounds it: storing the inputs, vector instructions (62 a value, 36 of them for the two codes; two thirds of the cycles at
+// 32,768 tokens x 2,048 channels, 163 us, 3.3 TB/s); without storing, what a block has to do one after the other -- ticket, loads,
+// pairs, state, stores: 8 us, two blocks to a compute unit -- (131,072 x 256: 58 us, 3.5 TB/s; a copy reaches 4.9).  128 tokens to
 // a workgroup in place of 256: 241 and 98 us against 229 and 85 (an earlier form), the chain being twice as long.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
@@ -705,10 +706,12 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_forward(ScanArgs p)
 // LDS, each thread's own in its place; x is decoded and dy read a second time behind the chain (kept in registers, dy costs 2 %
 // at 32,768 tokens x 2,048 channels of bf16 and, with 69 registers spilled, 18 % of fp32).
 // What bounds it: as in the forward direction, what a block does one after the other, at two blocks to a compute unit (128
-// registers a thread; 32,768 tokens x 2,048 channels: 155 us, 3.5 TB/s).  With one block of 232 registers to a compute unit it took
+// registers a thread; 32,768 tokens x 2,048 channels: 152 us, 3.6 TB/s).  With one block of 232 registers to a compute unit it took
 // 321 us against 230 in the same form.  A block in which sequences begin or end takes a path of its own from the pairs on: it is the
 // rarer one, and the registers of both together would not fit (stores and loads are counted together, so a register fetched back
-// after a store waits for that store).
+// after a store waits for that store).  The common path has no register in memory; the boundary path (fp32: 12 bytes a lane, 8 in the forward pass) and that of fewer
+// than four channels (bf16: 52 bytes) have.  Blocks with boundaries take longer, not only for that: 400 sequences in 32,768 x 1,024
+// 202 us forward and backward, 8 sequences 177 (fp32 262 and 239).
 template <typename S>
 struct BackwardShared {
     ScanShared s;
@@ -943,10 +946,11 @@ static bool stride_ok(int64_t ld, int64_t rows, int64_t cols) { return ld >= col
 // gains 0 to 10 % and loses as much above.
 constexpr int64_t kNarrowMost = 128;
 
-// A line of memory to each counter where the blocks start together, so that they get their tickets at once: up to 512, or up to
-// 1,024 of few groups (forward alone and with the backward pass, of the time with counters side by side: 8,192 tokens x 1,024
-// channels 0.83 and 0.88, 12,345 x 1,024 0.93 and 0.98, 131,072 x 128 0.94 and 0.97, 4,096 x 2,048 0.95 and 0.97).  Side by side
-// else: blocks that start less evenly do not pass through the same phase at once (5,120 x 2,048 1.08 and 1.06, 32,768 x 2,048 1.02).
+// A line of memory to each counter for up to 512 blocks, which all start at once, or up to 1,024 of few groups; side by side else.
+// Measured at 68 sizes, 2 to 128 groups, 160 to 2,560 blocks (bf16, of the time with counters side by side): up to 512 blocks forward 0.76 to
+// 1.01 and with the backward pass 0.87 to 1.03, least with 8 to 24 groups; 513 to 1,024 blocks of fewer than 32 groups 0.90 to 1.02 and 0.96 to
+// 1.01, of 32 groups 1.01 to 1.09 and 1.00 to 1.04, of 64 and 128 0.93 to 0.99 and 0.98 to 1.00; more blocks 0.98 to 1.09 and 0.99 to 1.07.
+// Why the larger calls lose was not found out.
 constexpr uint32_t kApart = 16;
 static bool start_together(int64_t blocks, int64_t groups) { return blocks * groups <= (groups < 32 ? 1024 : 512); }
 

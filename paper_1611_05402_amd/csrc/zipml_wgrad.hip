@@ -6,11 +6,12 @@
 // memory, [token][column], and are read through the transposing LDS read, which hands every lane four tokens of one
 // column.  Which tokens a lane gets does not matter as long as both operands agree.
 //
-// What bounds it: at 16,384 tokens, 4,096 x 4,096, the power that the matrix cores draw at this rate (455 us, 1,210 TFLOP/s; 440 to
-// 540 with the clock; the matrix instructions fill 63 % of the cycles; a library product of the same form, both operands
+// What bounds it: at 16,384 tokens, 4,096 x 4,096, the power that the matrix cores draw at this rate (458 us, 1,200 TFLOP/s in a long
+// run, 457 to 476; 465 to 550 in runs of a few calls, with the clock; the matrix instructions fill 63 % of the cycles; a library product of the same form, both operands
 // transposed, 1,083 TFLOP/s).  Small dW: LDS reads and the steps between barriers (65,536 tokens, 512 x 256: 30 us and 5 for
-// the joining of 32 ranges; the bytes alone would be 17).  fp32 dY at the first of these sizes: 1.30 ms, the same rate of matrix
-// instructions.
+// the joining of 32 ranges; the bytes alone would be 17).  fp32 dY at the first of these sizes: 1.29 to 1.34 ms, the same rate of matrix
+// instructions.  Adding to dW: 514 us at the first size, 13.9 in place of 10.2 at 1,000 tokens, 1,001 x 520 (the values of dW are read
+// one by one behind the last product), nothing where ranges are joined.
 //
 // bf16 dY: the products are exact and the sums fp32.  fp32 dY is split into three bf16 terms of 8 bits each and takes three matrix
 // instructions in place of one.  Together the terms are the value exactly from 2^-110 on; below that its bits under 2^-133, where bf16
@@ -373,8 +374,10 @@ template <typename T> struct Shapes {
 //   start + turns of a range * (one workgroup on a compute unit: lone, k of them: k * shared)
 //         + (ranges > 1: a launch, partial sums written and read),
 // a turn being 64 tokens of bf16 or 32 of fp32 dY, twice that with two teams.  The constants (us) are those that come nearest to 1,978
-// times measured over 55 sizes, both types, all shapes and numbers of ranges; the choice is then 1.4 % (bf16) and 0.3 % (fp32)
-// slower than the fastest on average, 15 % at most.  Without teams it was 4.4 and 3.8 %, 34 % at most: 1,000 tokens, 1,001 x 520 12.8 in
+// times measured over 55 sizes, both types, all shapes and numbers of ranges that are powers of two, the only ones tried here; of these
+// the choice is 1.4 % (bf16) and 0.3 % (fp32) slower than the fastest on average, 15 % at most.  The operands of those runs held one
+// value throughout, at which the matrix cores draw less power and clock higher: on random data large products take a third longer
+// than the sum says (16,384 tokens, 4,096 x 4,096: 458 us, 352 by the sum).  Without teams it was 4.4 and 3.8 %, 34 % at most: 1,000 tokens, 1,001 x 520 12.8 in
 // place of 9.6 us with bf16 and 19.9 in place of 16.7 with fp32; 4,096 tokens, 1,024 x 1,024 28 in place of 22.  A team alone
 // is faster up to some hundred tokens (128 tokens, 512 x 512: 4.8 us against 5.2).
 struct WgradPlan {
