@@ -25,7 +25,7 @@
  *   - Random numbers: Philox4x32-10, key = seed, counter = (row, feature / 4, epoch * 256 + stream),
  *     output word feature % 4, the top 24 bits as a uniform in [0,1).  Streams 1, 2 are the two
  *     sample quantisations (row = sample index), 3 and 4 the model and gradient quantisations
- *     (row = step index within the epoch), 16 and up the stored activations.  epoch must be < 2^24.
+ *     (row = step index within the epoch), 16 and up the stored activations and the rows of codes.  epoch must be < 2^24.
  */
 #ifndef ZIPML_H
 #define ZIPML_H
@@ -370,6 +370,78 @@ int zipml_scan_status(void *stream, const void *workspace_dev, size_t workspace_
 int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, const void *z_dev, int64_t ldz, int dtype,
                     int64_t rows, int64_t channels, float *h_dev, int64_t n_slots, const int32_t *slots_dev,
                     void *y_dev, int64_t ldy);
+
+/* ---- layers whose product runs on 8-bit codes -------------------------------------------------
+ * Rows (of tokens, or of a weight matrix, one for each output) as 8-bit codes with one scale a row, what makes such rows (an
+ * encoder, the norm in front of a layer), the product of two sets of them, and the norm's backward pass; and the norm of all
+ * gradients of a step.  All calls are asynchronous and may be captured in a graph.  Workspaces as above: no preparation, shared by
+ * calls that follow one another on a stream.  Scales and other vectors of one value a row need be aligned to their type only, so
+ * that calls may take part of the rows.
+ *
+ * Form of the codes (public): int8, rows ldc bytes apart, a multiple of 16 and at least cols; the bytes of a row from cols up to the
+ * next multiple of 16 are zeros (encoders write them).  value = code * scale of the row, fp32.
+ *   scale = max(max |v| / 127, 2^-126),  t = v * (1 / scale),  each a single fp32 operation;
+ *   ZIPML_NEAREST: code = t rounded to an integer, ties to even;
+ *   ZIPML_STOCHASTIC: code = floor(t + (k + 1/2) / 2^16), at most 127 in magnitude, k a 16-bit draw: v in expectation, to 2^-17 of
+ *   the scale.  Draws as those of zipml_act_encode, from (seed, epoch, tag, row, column).
+ * A row that holds an infinity or a NaN has a scale of NaN and codes of zero: all it is multiplied with becomes NaN. */
+#define ZIPML_NEAREST    0
+#define ZIPML_STOCHASTIC 1
+int zipml_row8_encode(void *stream, const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t ldx, int rounding,
+                      uint64_t seed, uint32_t epoch, int tag, void *codes_dev, int64_t ldc, float *scales_dev);
+
+/* The values that the codes stand for, rounded to dtype once. */
+int zipml_row8_decode(void *stream, const void *codes_dev, int64_t ldc, const float *scales_dev, int64_t rows, int64_t cols,
+                      void *out_dev, int dtype, int64_t ldo);
+
+/* Linear layer on codes: y[t][o] = ((sum_i x[t][i] w[o][i]) * x_scales[t]) * w_scales[o] + bias[o]: the sum is exact (32-bit
+ * integers), what follows is in fp32 and rounded to dtype once.  x_dev: codes of `rows` tokens, w_dev: of d_out rows of weights,
+ * both d_in wide, rows at most 4 MiB apart; bias_dev NULL: none.  d_in up to 131,071 (ZIPML_ERANGE beyond: the sum could leave 32
+ * bits), d_out up to 2^24.  A row with a scale of NaN gives NaN.  The same call with rows of a gradient, encoded by draws, and the
+ * codes of W^T gives the layer's input gradient, unbiased as those draws are independent of W's codes. */
+size_t zipml_row8_product_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in);
+int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, const float *x_scales_dev, const void *w_dev, int64_t ldw,
+                       const float *w_scales_dev, const float *bias_dev, int64_t rows, int64_t d_out, int64_t d_in, void *y_dev,
+                       int dtype, int64_t ldy, void *workspace_dev, size_t workspace_bytes);
+
+/* Root-mean-square norm of a residual stream:
+ *   r = x + add rounded to dtype (x alone without add_dev),  rstd = 1 / sqrt(mean r^2 + eps),  v = (r * rstd) * gain,
+ * row by row; mean and root in 64 bits, rstd rounded to fp32 once.  Outputs, each of them optional but one of the first two:
+ * y_dev, v rounded to dtype; codes_dev with scales_dev, v as 8-bit codes (ZIPML_NEAREST); sum_dev, r (for the next block's residual
+ * and the backward pass); rstd_dev, fp32 [rows] (for the backward pass).  x, add, sum, y: dtype, rows ld* >= cols apart, each one's
+ * leading dimension ignored where it is NULL; gain_dev: fp32 [cols], NULL for ones; eps finite and not negative.  sum_dev or y_dev
+ * may be x_dev or add_dev themselves (with the same leading dimension); otherwise outputs must not overlap inputs. */
+int zipml_norm_forward(void *stream, const void *x_dev, int64_t ldx, const void *add_dev, int64_t ldadd, int dtype, int64_t rows,
+                       int64_t cols, const float *gain_dev, float eps, void *sum_dev, int64_t ldsum, void *y_dev, int64_t ldy,
+                       void *codes_dev, int64_t ldc, float *scales_dev, float *rstd_dev);
+
+/* Its backward pass, from the r and rstd that it kept: with n = r * rstd and a = dy * gain,
+ *   dx = dsum + rstd (a - n mean(a n)),  the gradient of x and of add alike,    dgain = sum over the rows of dy n,
+ * dgain (fp32 [cols], NULL if it is not wanted) in an order of the sizes alone, or added to what is there with ZIPML_NORM_ADD.
+ * dsum_dev: the gradient that reaches r by the residual stream, NULL for none.  dx_dev may be dy_dev, sum_dev or dsum_dev itself.
+ * The workspace is for dgain: NULL will do without. */
+#define ZIPML_NORM_ADD 1
+size_t zipml_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+int zipml_norm_backward(void *stream, const void *dy_dev, int64_t lddy, const void *sum_dev, int64_t ldsum, int dtype, int64_t rows,
+                        int64_t cols, const float *gain_dev, const float *rstd_dev, const void *dsum_dev, int64_t lddsum,
+                        void *dx_dev, int64_t lddx, float *dgain_dev, int flags, void *workspace_dev, size_t workspace_bytes);
+
+/* Global norm of the gradients of a step, and the gradients scaled down to it:
+ *   norm = sqrt(sum of all g^2),  factor = 1 where norm <= max_norm, else max_norm / norm,  out = factor * g rounded to its type.
+ * tensors_host: n_tensors (1 .. 2^20) descriptions, read before the call returns (a captured graph keeps the addresses in them).
+ * Gradients and outputs are aligned to their types; out_dev may be grad_dev itself (of the same type) or NULL where only the norm
+ * is wanted; no output may overlap another output or another tensor's gradient.  norm_dev gets {norm, factor}.  Squares are summed
+ * in 64 bits in an order of the sizes alone.  A norm that is not finite leaves nothing hidden: an infinity gives factor 0 (and NaN
+ * where it stands), a NaN makes all outputs NaN. */
+typedef struct {
+    const void *grad_dev;
+    void *out_dev;
+    int64_t count;               /* values, 0 .. 2^34 */
+    int32_t grad_dtype, out_dtype;
+} zipml_clip_tensor;
+size_t zipml_clip_workspace_bytes(int64_t n_tensors);
+int zipml_clip(void *stream, const zipml_clip_tensor *tensors_host, int64_t n_tensors, float max_norm, float *norm_dev,
+               void *workspace_dev, size_t workspace_bytes);
 
 /* ---- parity / debug exports (not on the timed path) --------------------------------------- */
 

@@ -3,19 +3,9 @@
 
 namespace zipml {
 
-// A thread takes eight columns of kRows rows; the loads of all of them are issued before the first is used (2 rows measure the
-// same, 8 are 3 % slower).
-constexpr int kRows = 4;
-
 // Both kernels stream; every byte is moved once.  16,384 x 4,096 bf16: storing 203 MB in 36 to 41 us (4.9 to 5.6 TB/s; its generator, ten
 // rounds for eight values, keeps the vector units busy for more than half of that), restoring 203 MB in 30 us (the codes
 // come out of the cache that the storing left them in).  fp32: storing 336 MB in 61 us, restoring to fp32 110 (3.1 TB/s).  Small calls are bound by their launch: 2.5 and 1.6 us for 2,048 values.
-// Threads side by side in x take the units of eight columns of a row, those side by side in y rows; a workgroup takes tx * 8
-// columns of 256 / tx * kRows rows at a time.
-struct ActGrid {
-    int tx_log;       // log2 of the threads along a row
-    int64_t col_blocks, row_blocks;
-};
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, ActLayout lay, int64_t ldx, ActGrid g,
@@ -26,22 +16,22 @@ __global__ __launch_bounds__(256) void k_act_encode(const T *__restrict__ x, Act
     for (int64_t b = blockIdx.x; b < g.col_blocks * g.row_blocks; b += gridDim.x) {
         const int64_t rb = b / g.col_blocks, unit = ((b - rb * g.col_blocks) << g.tx_log) + tx;
         if (unit * 8 >= lay.pitch) continue;               // whole groups of four lanes
-        const int64_t row0 = rb * (ny * kRows) + ty;
-        float v[kRows][8];
+        const int64_t row0 = rb * (ny * kActRows) + ty;
+        float v[kActRows][8];
         // (where all is there the loads stand in no branch of their own, or each would wait for the one before)
-        const bool whole = (rb + 1) * (ny * kRows) <= lay.rows && (unit - tx + (1 << g.tx_log)) * 8 <= lay.cols;
+        const bool whole = (rb + 1) * (ny * kActRows) <= lay.rows && (unit - tx + (1 << g.tx_log)) * 8 <= lay.cols;
         if (__builtin_expect(whole, 1)) {
 #pragma unroll
-            for (int q = 0; q < kRows; ++q) load8(x + (row0 + q * ny) * ldx + unit * 8, 8, v[q]);
+            for (int q = 0; q < kActRows; ++q) load8(x + (row0 + q * ny) * ldx + unit * 8, 8, v[q]);
         } else {
 #pragma unroll
-            for (int q = 0; q < kRows; ++q) {
+            for (int q = 0; q < kActRows; ++q) {
                 const int64_t row = row0 + q * ny;
                 load8(x + row * ldx + unit * 8, row < lay.rows ? lay.cols - unit * 8 : 0, v[q]);
             }
         }
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
+        for (int q = 0; q < kActRows; ++q) {
             const int64_t row = row0 + q * ny;
             if (!whole && row >= lay.rows) break;
             const ActCodes8 c = act_encode8<T>(v[q], seed, epoch, row, (uint32_t)unit, stream);
@@ -60,18 +50,18 @@ __global__ __launch_bounds__(256) void k_act_decode(const uint8_t *__restrict__ 
     for (int64_t b = blockIdx.x; b < g.col_blocks * g.row_blocks; b += gridDim.x) {
         const int64_t rb = b / g.col_blocks, unit = ((b - rb * g.col_blocks) << g.tx_log) + tx;
         if (unit * 8 >= lay.cols) continue;
-        const int64_t row0 = rb * (ny * kRows) + ty;
-        u32x2 c[kRows];
-        uint32_t byte[kRows];
+        const int64_t row0 = rb * (ny * kActRows) + ty;
+        u32x2 c[kActRows];
+        uint32_t byte[kActRows];
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
+        for (int q = 0; q < kActRows; ++q) {
             const int64_t row = row0 + q * ny;
             const bool there = row < lay.rows;
             c[q] = there ? *reinterpret_cast<const u32x2 *>(act + row * lay.pitch + unit * 8) : u32x2{0, 0};
             byte[q] = there ? act[lay.steps + row * lay.groups + (unit >> 2)] : 0;
         }
 #pragma unroll
-        for (int q = 0; q < kRows; ++q) {
+        for (int q = 0; q < kActRows; ++q) {
             const int64_t row = row0 + q * ny;
             if (row >= lay.rows) break;
             float v[8];
@@ -79,23 +69,6 @@ __global__ __launch_bounds__(256) void k_act_decode(const uint8_t *__restrict__ 
             store8<THROUGH>(out + row * ldo + unit * 8, lay.cols - unit * 8, v);
         }
     }
-}
-
-static ActGrid act_grid(int64_t rows, int64_t units)
-{
-    ActGrid g;
-    g.tx_log = 2;
-    while (g.tx_log < 8 && (1ll << g.tx_log) < units) ++g.tx_log;
-    g.col_blocks = (units + (1 << g.tx_log) - 1) >> g.tx_log;
-    const int64_t rows_block = (256 >> g.tx_log) * kRows;
-    g.row_blocks = (rows + rows_block - 1) / rows_block;
-    return g;
-}
-// Workgroups of a grid-stride launch.
-static int act_blocks(const ActGrid &g)
-{
-    const int64_t all = g.col_blocks * g.row_blocks;
-    return (int)(all < (1 << 20) ? all : 1 << 20);
 }
 
 template <typename T>

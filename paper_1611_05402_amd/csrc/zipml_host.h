@@ -12,6 +12,7 @@ namespace zipml {
 
 inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool valid_bits(int bits) { return bits >= 1 && bits <= 8; }
 
 // Packed layout (private).  A unit is 32 codes of `bits` bits: a little-endian bit string of

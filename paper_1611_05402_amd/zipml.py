@@ -22,6 +22,8 @@ PROX_NONE, PROX_L1, PROX_L2SQ, PROX_BOX = 0, 1, 2, 3
 F32, BF16 = 0, 1
 WGRAD_ADD = 1
 SCAN_BLOCK = 256
+NEAREST, STOCHASTIC = 0, 1
+NORM_ADD = 1
 
 OK, EINVAL, EALIGN, ERANGE, EWORKSPACE, ELAUNCH, EUNSUPPORTED, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6, -7
 
@@ -33,7 +35,9 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_unpack_codes", "zipml_debug_step", "zipml_act_bytes", "zipml_act_encode",
            "zipml_act_decode", "zipml_act_wgrad_workspace_bytes", "zipml_act_wgrad",
            "zipml_scan_workspace_bytes", "zipml_scan_forward", "zipml_scan_backward", "zipml_scan_status",
-           "zipml_scan_step"]
+           "zipml_scan_step", "zipml_row8_encode", "zipml_row8_decode", "zipml_row8_product_workspace_bytes",
+           "zipml_row8_product", "zipml_norm_forward", "zipml_norm_backward_workspace_bytes", "zipml_norm_backward",
+           "zipml_clip_workspace_bytes", "zipml_clip"]
 
 
 class ZipmlError(RuntimeError):
@@ -129,6 +133,24 @@ def lib() -> C.CDLL:
         L.zipml_scan_status.argtypes = [vp, vp, sz]
         L.zipml_scan_step.restype = i32
         L.zipml_scan_step.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, vp, i64]
+        L.zipml_row8_encode.restype = i32
+        L.zipml_row8_encode.argtypes = [vp, vp, i32, i64, i64, i64, i32, u64, u32, i32, vp, i64, vp]
+        L.zipml_row8_decode.restype = i32
+        L.zipml_row8_decode.argtypes = [vp, vp, i64, vp, i64, i64, vp, i32, i64]
+        L.zipml_row8_product_workspace_bytes.restype = sz
+        L.zipml_row8_product_workspace_bytes.argtypes = [i64, i64, i64]
+        L.zipml_row8_product.restype = i32
+        L.zipml_row8_product.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, sz]
+        L.zipml_norm_forward.restype = i32
+        L.zipml_norm_forward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.zipml_norm_backward_workspace_bytes.restype = sz
+        L.zipml_norm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.zipml_norm_backward.restype = i32
+        L.zipml_norm_backward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, vp, vp, i64, vp, i64, vp, i32, vp, sz]
+        L.zipml_clip_workspace_bytes.restype = sz
+        L.zipml_clip_workspace_bytes.argtypes = [i64]
+        L.zipml_clip.restype = i32
+        L.zipml_clip.argtypes = [vp, vp, i64, f32, vp, vp, sz]
         _lib = L
     return _lib
 
@@ -443,3 +465,128 @@ def scan_step(x, ldx, z, ldz, rows, channels, h, n_slots, y, ldy, *, slots=None,
     w = "zipml_scan_step"
     _check(lib().zipml_scan_step(_stream(stream), x.data_ptr(), ldx, z.data_ptr(), ldz, _rows(w, x, z, y), rows, channels,
                                  _array(w, "h", h, "float32"), n_slots, _array(w, "slots", slots, "int32"), y.data_ptr(), ldy), w)
+
+
+def _codes(where, name, t):
+    """The address of rows of codes, which lie a leading dimension of the caller's apart."""
+    if t is None:
+        return None
+    s = t.stride()
+    if t.dtype is not _KINDS["int8"] or (s and s[-1] != 1 and t.shape[-1] > 1):
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be int8 rows of codes side by side, not {t.dtype} with strides {s}")
+    return t.data_ptr()
+
+
+def _same_rows(where, kind, *named):
+    """Whether the rows of further tensors (name, tensor or None) are of type `kind` with their values side by side."""
+    for name, t in named:
+        if t is not None and (t.dtype is not kind or (t.stride()[-1:] != _ONE and _rows(where, t) < 0)):
+            raise ZipmlError(EINVAL, f"{where}: {name} is {t.dtype}, the other rows are {kind}")
+
+
+def row8_encode(x, rows, cols, ldx, codes, ldc, scales, *, rounding=NEAREST, seed=0, epoch=0, tag=0, stream=None):
+    """Rows of x (fp32 or bf16) as 8-bit codes (int8, rows ldc bytes apart) with a scale each (fp32)."""
+    w = "zipml_row8_encode"
+    _check(lib().zipml_row8_encode(_stream(stream), _ptr(x), _rows(w, x), rows, cols, ldx, rounding, seed, epoch, tag,
+                                   _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32")), w)
+
+
+def row8_decode(codes, ldc, scales, rows, cols, out, ldo, stream=None):
+    """The values that rows of codes stand for, in out (fp32 or bf16)."""
+    w = "zipml_row8_decode"
+    _check(lib().zipml_row8_decode(_stream(stream), _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32"), rows,
+                                   cols, _ptr(out), _rows(w, out), ldo), w)
+
+
+def row8_product_workspace_bytes(rows: int, d_out: int, d_in: int) -> int:
+    return int(lib().zipml_row8_product_workspace_bytes(rows, d_out, d_in))
+
+
+def row8_product(x, ldx, x_scales, w, ldw, w_scales, rows, d_out, d_in, y, ldy, workspace, *, bias=None, stream=None):
+    """y (fp32 or bf16) = x w^T from codes of tokens and of weights, with their scales (fp32) and a bias (fp32)."""
+    f = "zipml_row8_product"
+    _check(lib().zipml_row8_product(_stream(stream), _codes(f, "x", x), ldx, _array(f, "x_scales", x_scales, "float32"),
+                                    _codes(f, "w", w), ldw, _array(f, "w_scales", w_scales, "float32"),
+                                    _array(f, "bias", bias, "float32"), rows, d_out, d_in, _ptr(y), _rows(f, y), ldy,
+                                    workspace.data_ptr(), workspace.nbytes), f)
+
+
+def norm_forward(x, ldx, rows, cols, eps, *, gain=None, add=None, ldadd=0, sum=None, ldsum=0, y=None, ldy=0, codes=None, ldc=0,
+                 scales=None, rstd=None, stream=None):
+    """Root-mean-square norm of x + add: its result in y (x's type) or in codes with scales; sum gets x + add, rstd (fp32) what
+    the backward pass needs.  gain, scales, rstd: fp32."""
+    w = "zipml_norm_forward"
+    kind = _rows(w, x)
+    if kind >= 0:
+        _same_rows(w, x.dtype, ("add", add), ("sum", sum), ("y", y))
+    _check(lib().zipml_norm_forward(_stream(stream), _ptr(x), ldx, _ptr(add), ldadd, kind, rows, cols,
+                                    _array(w, "gain", gain, "float32"), eps, _ptr(sum), ldsum, _ptr(y), ldy,
+                                    _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32"),
+                                    _array(w, "rstd", rstd, "float32")), w)
+
+
+def norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().zipml_norm_backward_workspace_bytes(rows, cols))
+
+
+def norm_backward(dy, lddy, sum, ldsum, rows, cols, rstd, dx, lddx, workspace=None, *, gain=None, dsum=None, lddsum=0, dgain=None,
+                  flags=0, stream=None):
+    """Gradients dx and dgain of norm_forward from the sum and rstd that it kept; dsum: the gradient that reaches the sum by the
+    residual stream; flags: NORM_ADD adds to dgain.  The workspace is needed for dgain only."""
+    w = "zipml_norm_backward"
+    kind = _rows(w, dy)
+    if kind >= 0:
+        _same_rows(w, dy.dtype, ("sum", sum), ("dsum", dsum), ("dx", dx))
+    _check(lib().zipml_norm_backward(_stream(stream), _ptr(dy), lddy, _ptr(sum), ldsum, kind, rows, cols,
+                                     _array(w, "gain", gain, "float32"), _array(w, "rstd", rstd, "float32"), _ptr(dsum), lddsum,
+                                     _ptr(dx), lddx, _array(w, "dgain", dgain, "float32"), flags, _ptr(workspace),
+                                     0 if workspace is None else workspace.nbytes), w)
+
+
+class _ClipTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("grad_dtype", C.c_int32), ("out_dtype", C.c_int32)]
+
+
+class ClipList:
+    """Gradients (contiguous, fp32 or bf16) and where they go once they are clipped: outs, one for each of the same number of
+    values, None for an entry whose norm alone counts; without outs they stay in their places.  Made once for tensors that stay
+    where they are; it keeps them alive."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        w = "ClipList"
+        if len(self.outs) != len(self.grads) or not self.grads:
+            raise ZipmlError(EINVAL, f"{w}: {len(self.grads)} gradients and {len(self.outs)} outputs")
+        spans = []
+        self.table = (_ClipTensor * len(self.grads))()
+        for k, (g, o) in enumerate(zip(self.grads, self.outs)):
+            for name, t in (("gradient", g), ("output", o)):
+                if t is not None and (not t.is_contiguous() or _dtype(t) < 0):
+                    raise ZipmlError(EINVAL, f"{w}: {name} {k} has to be contiguous fp32 or bf16, not {t.dtype} with strides {t.stride()}")
+            if o is not None and o.numel() != g.numel():
+                raise ZipmlError(EINVAL, f"{w}: output {k} has {o.numel()} values, its gradient {g.numel()}")
+            same = o is not None and o.data_ptr() == g.data_ptr() and o.dtype is g.dtype
+            spans += [(t.data_ptr(), t.data_ptr() + t.nbytes, written) for t, written in
+                      ([(o, True)] if same else [(g, False), (o, True)]) if t is not None and t.numel()]
+            self.table[k] = _ClipTensor(_ptr(g), _ptr(o), g.numel(), _dtype(g), _dtype(g if o is None else o))
+        # no output overlaps another one or another tensor's gradient
+        end, written = 0, False
+        for start, stop, writes in sorted(spans):
+            if start < end and (writes or written):
+                raise ZipmlError(EINVAL, f"{w}: an output overlaps another tensor")
+            written = writes or (written and start < end)
+            end = max(end, stop)
+
+
+def clip_workspace_bytes(n_tensors: int) -> int:
+    return int(lib().zipml_clip_workspace_bytes(n_tensors))
+
+
+def clip(tensors, max_norm, norm, workspace, stream=None):
+    """Global norm over a ClipList's gradients, which are scaled down to max_norm; norm: fp32 [2], gets the norm and the factor."""
+    w = "zipml_clip"
+    if norm is not None and norm.numel() < 2:
+        raise ZipmlError(EINVAL, f"{w}: norm has to hold two values")
+    _check(lib().zipml_clip(_stream(stream), tensors.table, len(tensors.table), max_norm, _array(w, "norm", norm, "float32"),
+                            workspace.data_ptr(), workspace.nbytes), w)
