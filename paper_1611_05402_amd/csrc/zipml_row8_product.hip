@@ -17,6 +17,8 @@ struct ProductArgs {
     int64_t ldx, ldw, ldy, rows;
     int d_out, bytes;           // bytes: of a row, padding included
     int tiles_t, tiles_o;
+    int range;                  // bytes of a row that a workgroup takes, a multiple of kStep
+    int64_t part;               // sums of a range, [rows][ldy], behind those of the one before
 };
 
 constexpr int kStep = 128;      // codes of a row that are in LDS at a time
@@ -36,116 +38,443 @@ struct CodeRows {
     }
 };
 
-// MO x MT outputs x tokens of a workgroup, WO x WT waves.
-template <int MO_, int MT_, int WO_, int WT_>
-struct ProductShape {
-    static constexpr int MO = MO_, MT = MT_, WO = WO_, WT = WT_, kThreads = 64 * WO * WT;
-    static constexpr int TO = MO / WO / 32, TT = MT / WT / 32;
-    static constexpr int kLoadsW = MO * kStep / 16 / kThreads, kLoadsX = MT * kStep / 16 / kThreads;
-    static constexpr int kStage = (MO + MT) * kStep, kLds = 2 * kStage;
-    static_assert(kLoadsW * 16 * kThreads == MO * kStep && kLoadsX * 16 * kThreads == MT * kStep, "whole loads");
-};
-
 // Where the 16 bytes `chunk` of a row lie in an LDS tile: turned by the row's number, so that 16 rows' same chunk, which 16 lanes
 // read at once, fall on all banks.
 __device__ __forceinline__ int lds_at(int row, int chunk) { return row * kStep + ((chunk ^ (row >> 1 & 7)) << 4); }
+
+// Orders a wave's own LDS accesses, of all its lanes.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// Scales (and bias) of four neighbouring outputs, and four results of a token from them.
+struct Out4 {
+    float sw[4], bias[4];
+    int n;                      // how many of them there are
+    __device__ __forceinline__ Out4(const ProductArgs &a, int o) : n(a.d_out - o)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sw[k] = k < n ? a.sw[o + k] : 0.0f;
+            bias[k] = a.bias && k < n ? a.bias[o + k] : 0.0f;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void put(const ProductArgs &a, T *y, float sx, i32x4 sum) const
+    {
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = (float)sum[k] * sx * sw[k];
+            if (a.bias) v[k] += bias[k];
+        }
+        if (n >= 4) {
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            typedef T4 T4_any __attribute__((aligned(sizeof(T))));
+            *reinterpret_cast<T4_any *>(y) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < n) y[k] = (T)v[k];
+        }
+    }
+};
+
+// Workgroups go to the eight XCDs in turn; each XCD gets a run of neighbouring tiles, in bands four outputs deep, so that its L2
+// serves rows of both operands to several of them.
+__device__ __forceinline__ void tile_of(const ProductArgs &a, uint32_t n, uint32_t at, int &o, int &t)
+{
+    const uint32_t xcd = at & 7, per = n >> 3, more = n & 7;
+    const uint32_t id = xcd * per + (xcd < more ? xcd : more) + (at >> 3), band = id / (4 * a.tiles_t), in = id - band * 4 * a.tiles_t;
+    const uint32_t deep = a.tiles_o - band * 4 < 4 ? a.tiles_o - band * 4 : 4;
+    o = band * 4 + in % deep;
+    t = in / deep;
+}
+
+// ---- many tokens: tiles whose waves share the rows ----------------------------------------------
+// MO x MT outputs x tokens of a workgroup, WO x WT waves.
+template <typename T, int MO_, int MT_, int WO_, int WT_>
+struct ProductShape {
+    static constexpr int MO = MO_, MT = MT_, WO = WO_, WT = WT_, kThreads = 64 * WO * WT;
+    static constexpr int TO = MO / WO / 32, TT = MT / WT / 32;
+    static constexpr int kLoadsW = MO * kStep / 16 / kThreads, kLoadsX = MT * kStep / 16 / kThreads, kLoads = kLoadsW + kLoadsX;
+    static constexpr int kStage = (MO + MT) * kStep;
+    static constexpr bool kParts = std::is_same<T, int>::value;     // sums of a range of the contraction, not results
+    static constexpr int HO = 4 / (int)sizeof(T);                   // 32 x 32 tiles side by side in a line of 128 bytes of results
+    static constexpr int kOut = 32 * 128;                           // LDS of a wave's results on their way out: 32 tokens
+    static constexpr int kLds = 2 * kStage > kOut * WO * WT ? 2 * kStage : kOut * WO * WT;
+    static_assert(kLoadsW * 16 * kThreads == MO * kStep && kLoadsX * 16 * kThreads == MT * kStep && TO % HO == 0, "whole loads");
+    static_assert(kLds <= 160 * 1024, "LDS");
+};
 
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int tile_o = blockIdx.x % a.tiles_o, tile_t = blockIdx.x / a.tiles_o;
+    const int wo = wave / S::WT, wt = wave % S::WT;
+    int tile_o, tile_t;
+    const uint32_t tiles = (uint32_t)a.tiles_o * a.tiles_t, split = blockIdx.x / tiles;
+    tile_of(a, tiles, blockIdx.x - split * tiles, tile_o, tile_t);
+    const int k_begin = (int)split * a.range, k_end = k_begin + a.range < a.bytes ? k_begin + a.range : a.bytes;
     const int o0 = tile_o * S::MO;
     const int64_t t0 = (int64_t)tile_t * S::MT;
     const CodeRows w(a.w + o0 * a.ldw, a.d_out - o0, a.ldw, a.bytes), x(a.x + t0 * a.ldx, a.rows - t0, a.ldx, a.bytes);
 
-    u32x4 vw[S::kLoadsW], vx[S::kLoadsX];
-    auto load = [&](int k0) {
+    // The loads and the stores of a round are dealt over its steps but the last.
+    constexpr int kSteps = kStep / 32, kDeals = kSteps - 1;
+    u32x4 v[S::kLoads];
+    auto load = [&](int k0, int deal) {
 #pragma unroll
-        for (int q = 0; q < S::kLoadsW; ++q) {
-            const int c = tid + q * S::kThreads;
-            vw[q] = w.load16(c >> 3, k0 + (c & 7) * 16);
-        }
-#pragma unroll
-        for (int q = 0; q < S::kLoadsX; ++q) {
-            const int c = tid + q * S::kThreads;
-            vx[q] = x.load16(c >> 3, k0 + (c & 7) * 16);
+        for (int q = 0; q < S::kLoads; ++q) {
+            if (q * kDeals / S::kLoads != deal) continue;
+            const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
+            v[q] = (q < S::kLoadsW ? w : x).load16(c >> 3, k0 + (c & 7) * 16);
         }
     };
-    auto store = [&](char *stage) {
+    auto store = [&](char *stage, int deal) {
 #pragma unroll
-        for (int q = 0; q < S::kLoadsW; ++q) {
-            const int c = tid + q * S::kThreads;
-            *reinterpret_cast<u32x4 *>(stage + lds_at(c >> 3, c & 7)) = vw[q];
-        }
-#pragma unroll
-        for (int q = 0; q < S::kLoadsX; ++q) {
-            const int c = tid + q * S::kThreads;
-            *reinterpret_cast<u32x4 *>(stage + S::MO * kStep + lds_at(c >> 3, c & 7)) = vx[q];
+        for (int q = 0; q < S::kLoads; ++q) {
+            if (q * kDeals / S::kLoads != deal) continue;
+            const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
+            *reinterpret_cast<u32x4 *>(stage + (q < S::kLoadsW ? 0 : S::MO * kStep) + lds_at(c >> 3, c & 7)) = v[q];
         }
     };
 
-    const int wo = wave / S::WT, wt = wave % S::WT;
-    i32x16 acc[S::TO][S::TT] = {};
-    load(0);
-    store(lds);
+    i32x4 fw[2][S::TO], fx[2][S::TT];
+    auto read = [&](const char *stage, int s) {
+        const int chunk = 2 * s + (lane >> 5);
+#pragma unroll
+        for (int m = 0; m < S::TO; ++m)
+            fw[s & 1][m] = *reinterpret_cast<const i32x4 *>(stage + lds_at((wo * S::TO + m) * 32 + (lane & 31), chunk));
+#pragma unroll
+        for (int n = 0; n < S::TT; ++n)
+            fx[s & 1][n] = *reinterpret_cast<const i32x4 *>(stage + S::MO * kStep + lds_at((wt * S::TT + n) * 32 + (lane & 31), chunk));
+    };
     char *here = lds, *next = lds + S::kStage;
-    for (int k0 = 0; k0 < a.bytes; k0 += kStep) {
-        load(k0 + kStep);
-        lds_barrier();
+    i32x16 acc[S::TO][S::TT] = {};
 #pragma unroll
-        for (int s = 0; s < kStep / 32; ++s) {
-            const int chunk = 2 * s + (lane >> 5);
-            i32x4 fw[S::TO], fx[S::TT];
+    for (int d = 0; d < kDeals; ++d) load(k_begin, d);
+#pragma unroll
+    for (int d = 0; d < kDeals; ++d) {
+        store(here, d);
+        load(k_begin + kStep, d);
+    }
+    lds_barrier();
+    read(here, 0);
+    for (int k0 = k_begin; k0 < k_end; k0 += kStep) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s < kDeals) {
+                read(here, s + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                store(next, s);
+                load(k0 + 2 * kStep, s);
+            } else {
+                lds_barrier();
+                read(next, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int m = 0; m < S::TO; ++m)
-                fw[m] = *reinterpret_cast<const i32x4 *>(here + lds_at((wo * S::TO + m) * 32 + (lane & 31), chunk));
 #pragma unroll
-            for (int n = 0; n < S::TT; ++n)
-                fx[n] = *reinterpret_cast<const i32x4 *>(here + S::MO * kStep + lds_at((wt * S::TT + n) * 32 + (lane & 31), chunk));
-#pragma unroll
-            for (int m = 0; m < S::TO; ++m)
-#pragma unroll
-                for (int n = 0; n < S::TT; ++n) acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[m], fx[n], acc[m][n], 0, 0, 0);
+                for (int n = 0; n < S::TT; ++n)
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[s & 1][m], fx[s & 1][n], acc[m][n], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        store(next);
         char *const t = here;
         here = next;
         next = t;
     }
 
-    // a lane holds four neighbouring outputs of one token at a time
-    T *const y = (T *)a.y;
+    // A lane holds four neighbouring outputs of one token at a time.  Through LDS of its own, a wave turns 32 tokens' lines of 128
+    // bytes around and writes them 16 bytes a lane.
+    char *const out = lds + wave * S::kOut;
+    const int o_wave = o0 + wo * S::TO * 32;
+    const int64_t t_wave = t0 + wt * S::TT * 32;
+    lds_barrier();                         // (whose results may lie where another wave still reads)
+    const auto scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.sw), 0, a.d_out * 4, 0x00020000);
+    const auto biases = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.bias), 0, a.bias ? a.d_out * 4 : 0, 0x00020000);
+    float sx[S::TT];
 #pragma unroll
-    for (int n = 0; n < S::TT; ++n) {
-        const int64_t t = t0 + (wt * S::TT + n) * 32 + (lane & 31);
-        if (t >= a.rows) continue;
-        const float sx = a.sx[t];
+    for (int n = 0; n < S::TT && !S::kParts; ++n) {
+        const int64_t t = t_wave + n * 32 + (lane & 31);
+        sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
+    }
 #pragma unroll
-        for (int m = 0; m < S::TO; ++m)
+    for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
+        constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
+        const int o = o_wave + m0 * 32 + (lane & 7) * V, left = a.d_out - o;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const int o = o0 + (wo * S::TO + m) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
-                if (o >= a.d_out) continue;
-                const float v = (float)acc[m][n][q] * sx * a.sw[o];
-                y[t * a.ldy + o] = (T)(a.bias ? v + a.bias[o] : v);
+        for (int n = 0; n < S::TT; ++n) {
+            const int t32 = lane & 31;
+#pragma unroll
+            for (int m = 0; m < S::HO; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    T4 r;
+                    if constexpr (S::kParts) {
+                        r = T4{acc[m0 + m][n][4 * q], acc[m0 + m][n][4 * q + 1], acc[m0 + m][n][4 * q + 2], acc[m0 + m][n][4 * q + 3]};
+                    } else {
+                        const int at = (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4;
+                        const f32x4 sw = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at, 0, 0));
+                        f32x4 f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) f[k] = (float)acc[m0 + m][n][4 * q + k] * sx[n] * sw[k];
+                        if (a.bias) f += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at, 0, 0));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) r[k] = (T)f[k];
+                    }
+                    const int byte = (m * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
+                    *reinterpret_cast<T4 *>(out + t32 * 128 + (((byte >> 4) ^ (t32 >> 1 & 7)) << 4) + (byte & 15)) = r;
+                }
+            wave_fence();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 8 * i + (lane >> 3);
+                const u32x4 line = *reinterpret_cast<const u32x4 *>(out + lds_at(r, lane & 7));
+                const int64_t t = t_wave + n * 32 + r;
+                if (t >= a.rows) continue;
+                T *const y = (T *)a.y + split * a.part + t * a.ldy + o;
+                if (left >= V) {
+                    *reinterpret_cast<u32x4_any *>(y) = line;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k < left) {
+                            const uint32_t word = line[k * (int)sizeof(T) / 4];   // (a cast of the vector's element itself takes its first)
+                            if constexpr (sizeof(T) == 4) y[k] = __builtin_bit_cast(T, word);
+                            else y[k] = __builtin_bit_cast(__bf16, (uint16_t)(word >> (16 * (k & 1))));
+                        }
+                }
             }
+            wave_fence();
+        }
     }
 }
 
+// ---- few tokens, few outputs: the waves of a workgroup share the contraction -------------------
+// Where a tile has few products for its bytes, nothing is gained by sharing rows between waves; what counts is that all of a
+// compute unit's waves have loads under way.  So the waves of a workgroup take steps of KS codes of the same MO x MT tile by turns,
+// each through LDS of its own and without a barrier, and add up their sums at the end.
+template <int MO_, int MT_, int KS_, int WAVES_>
+struct SplitShape {
+    static constexpr int MO = MO_, MT = MT_, KS = KS_, WAVES = WAVES_, kThreads = 64 * WAVES;
+    static constexpr bool kSmall = MO == 16;                      // 16 x 16 x 64 instructions, otherwise 32 x 32 x 32
+    static constexpr int kPlanes = KS / 128;                      // 128 codes of all rows lie together
+    static constexpr int kLoadsW = MO / 8 * kPlanes, kLoadsX = MT / 8 * kPlanes;
+    static constexpr int TO = kSmall ? 1 : MO / 32, TT = kSmall ? 1 : MT / 32;
+    static constexpr int kStage = (MO + MT) * KS;
+    static constexpr int kRow = MO + 4;                           // a token's sums in LDS, with room against bank conflicts
+    static constexpr int kSums = MT * kRow * 4;
+    static constexpr int kWave = kStage > kSums ? kStage : kSums; // LDS of a wave
+    static constexpr int kLds = kWave * WAVES;
+    static_assert(kSmall ? MT == 16 : MO % 32 == 0 && MT % 32 == 0, "tile");
+    static_assert(kLds <= 160 * 1024, "LDS");
+};
+
 template <typename T, typename S>
-static int launch_product(hipStream_t s, ProductArgs a)
+__global__ __launch_bounds__(S::kThreads) void k_row8_product_split(ProductArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tile_o = blockIdx.x % a.tiles_o, tile_t = blockIdx.x / a.tiles_o;
+    const int o0 = tile_o * S::MO;
+    const int64_t t0 = (int64_t)tile_t * S::MT;
+    const CodeRows w(a.w + o0 * a.ldw, a.d_out - o0, a.ldw, a.bytes), x(a.x + t0 * a.ldx, a.rows - t0, a.ldx, a.bytes);
+    char *const mine = lds + wave * S::kWave;
+
+    u32x4 vw[S::kLoadsW], vx[S::kLoadsX];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int q = 0; q < S::kLoadsW; ++q)
+            vw[q] = w.load16(q / S::kPlanes * 8 + (lane >> 3), k0 + q % S::kPlanes * 128 + (lane & 7) * 16);
+#pragma unroll
+        for (int q = 0; q < S::kLoadsX; ++q)
+            vx[q] = x.load16(q / S::kPlanes * 8 + (lane >> 3), k0 + q % S::kPlanes * 128 + (lane & 7) * 16);
+    };
+    i32x16 acc[S::TO][S::TT] = {};
+    i32x4 small = {};
+    load(wave * S::KS);
+    for (int k0 = wave * S::KS; k0 < a.bytes; k0 += S::WAVES * S::KS) {
+#pragma unroll
+        for (int q = 0; q < S::kLoadsW; ++q)
+            *reinterpret_cast<u32x4 *>(mine + q % S::kPlanes * S::MO * 128 + lds_at(q / S::kPlanes * 8 + (lane >> 3), lane & 7)) = vw[q];
+#pragma unroll
+        for (int q = 0; q < S::kLoadsX; ++q)
+            *reinterpret_cast<u32x4 *>(mine + S::MO * S::KS + q % S::kPlanes * S::MT * 128 +
+                                       lds_at(q / S::kPlanes * 8 + (lane >> 3), lane & 7)) = vx[q];
+        wave_fence();
+        load(k0 + S::WAVES * S::KS);
+#pragma unroll
+        for (int p = 0; p < S::kPlanes; ++p) {
+            const char *const pw = mine + p * S::MO * 128, *const px = mine + S::MO * S::KS + p * S::MT * 128;
+            if constexpr (S::kSmall) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int at = lds_at(lane & 15, 4 * s + (lane >> 4));
+                    small = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(pw + at),
+                                                                  *reinterpret_cast<const i32x4 *>(px + at), small, 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    i32x4 fw[S::TO], fx[S::TT];
+#pragma unroll
+                    for (int m = 0; m < S::TO; ++m)
+                        fw[m] = *reinterpret_cast<const i32x4 *>(pw + lds_at(m * 32 + (lane & 31), 2 * s + (lane >> 5)));
+#pragma unroll
+                    for (int n = 0; n < S::TT; ++n)
+                        fx[n] = *reinterpret_cast<const i32x4 *>(px + lds_at(n * 32 + (lane & 31), 2 * s + (lane >> 5)));
+#pragma unroll
+                    for (int m = 0; m < S::TO; ++m)
+#pragma unroll
+                        for (int n = 0; n < S::TT; ++n) acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[m], fx[n], acc[m][n], 0, 0, 0);
+                }
+            }
+        }
+        wave_fence();
+    }
+
+    // [token][output] of each wave, then the waves' sums
+    int *const sums = reinterpret_cast<int *>(mine);
+    if constexpr (S::kSmall) {
+        *reinterpret_cast<i32x4 *>(sums + (lane & 15) * S::kRow + 4 * (lane >> 4)) = small;
+    } else {
+#pragma unroll
+        for (int m = 0; m < S::TO; ++m)
+#pragma unroll
+            for (int n = 0; n < S::TT; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<i32x4 *>(sums + (n * 32 + (lane & 31)) * S::kRow + m * 32 + 8 * q + 4 * (lane >> 5)) =
+                        i32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
+    }
+    lds_barrier();
+    for (int i = threadIdx.x; i < S::MT * S::MO / 4; i += S::kThreads) {
+        const int t = i / (S::MO / 4), o = i % (S::MO / 4) * 4;
+        if (t0 + t >= a.rows || o0 + o >= a.d_out) continue;
+        i32x4 sum = {};
+#pragma unroll
+        for (int v = 0; v < S::WAVES; ++v) sum += *reinterpret_cast<const i32x4 *>(lds + v * S::kWave + (t * S::kRow + o) * 4);
+        Out4(a, o0 + o).put(a, (T *)a.y + (t0 + t) * a.ldy + o0 + o, a.sx[t0 + t], sum);
+    }
+}
+
+// Results from the sums of the ranges: four neighbouring outputs of a token a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const int *part, int64_t ld_part, int ranges)
+{
+    const uint32_t units = (uint32_t)(ld_part / 4);
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x, t = i / units;
+    const int o = (int)(i - t * units) * 4;
+    if (t >= a.rows) return;
+    const int *p = part + t * ld_part + o;
+    i32x4 sum = *reinterpret_cast<const i32x4 *>(p);
+#pragma unroll 4
+    for (int r = 1; r < ranges; ++r) sum += *reinterpret_cast<const i32x4 *>(p + r * a.part);
+    Out4(a, o).put(a, (T *)a.y + t * a.ldy + o, a.sx[t], sum);
+}
+
+// The shapes: tiles whose waves share the contraction (outputs, tokens, waves), tiles whose waves share the rows (outputs, tokens, waves
+// along each).
+#define ZIPML_PRODUCT_SPLIT(F)                                                                                                  \
+    F(0, 16, 16, 4) F(1, 16, 16, 8) F(2, 16, 16, 16) F(3, 32, 32, 4) F(4, 32, 32, 8) F(5, 32, 32, 16) F(6, 64, 32, 8) F(7, 64, 64, 8)
+#define ZIPML_PRODUCT_TILE(F) F(8, 128, 64, 2, 2) F(9, 128, 128, 2, 4) F(10, 256, 256, 2, 4)
+
+// Which shape, and (of the second kind) in how many ranges the contraction is taken, whose sums a second launch joins: the least of
+//   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
+//   them: k * shared) + (ranges > 1: a launch, sums written and read).
+// The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
+// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 2 % slower than the fastest on average, 26 % at most.
+struct ProductPlan {
+    int shape, ranges, range;              // range: bytes of a row
+    size_t workspace;
+};
+static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
+{
+    struct Cost { int outs, tokens, waves; double start, turn, lone, shared; };
+    static const Cost costs[] = {
+        {16, 16, 4, 2.70, 0.00, 0.28, 0.25}, {16, 16, 8, 2.64, 0.00, 0.47, 0.51},
+        {16, 16, 16, 2.39, 0.00, 0.89, 1.12}, {32, 32, 4, 2.74, 0.04, 0.57, 0.51},
+        {32, 32, 8, 2.66, 0.12, 0.93, 1.05}, {32, 32, 16, 1.84, 0.00, 1.90, 2.36},
+        {64, 32, 8, 2.71, 2.24, 1.44, 1.37}, {64, 64, 8, 3.11, 3.03, 1.98, 2.00},
+        {128, 64, 1, 4.30, 1.36, 0.45, 0.42}, {128, 128, 1, 4.49, 2.73, 0.57, 0.60},
+        {256, 256, 1, 10.10, 8.00, 1.27, 1.73},
+    };
+    const int64_t bytes = round_up(d_in, kRow8Unit), sums = rows * round_up(d_out, 4) * 4;
+    ProductPlan best{-1, 1, 0, 0};
+    double least = 0;
+    for (int shape = 0; shape < (int)(sizeof(costs) / sizeof(costs[0])); ++shape) {
+        const Cost &c = costs[shape];
+        const int64_t tiles = ((d_out + c.outs - 1) / c.outs) * ((rows + c.tokens - 1) / c.tokens);
+        if (tiles > 0x3FFFFFFF) continue;
+        const double k1 = (double)((tiles + 255) / 256);
+        if (best.shape >= 0 && c.start + (k1 - 1) * c.turn >= least) continue;
+        for (const int wanted : {1, 2, 3, 4, 8, 16}) {
+            // (ranges of two rounds at least, whose sums stay in the caches)
+            if (wanted > 1 && (c.waves > 1 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;
+            const int64_t range = round_up((bytes + wanted - 1) / wanted, kStep), ranges = (bytes + range - 1) / range;
+            const double k = (double)((tiles * ranges + 255) / 256), step = (double)kStep * c.waves;
+            const double rounds = (double)(int64_t)(((double)(range < bytes ? range : bytes) + step - 1) / step);
+            const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && k * c.shared > c.lone ? k * c.shared : c.lone) +
+                              (ranges > 1 ? 2.2 + (double)(ranges * sums) * 2 / 6.3e6 : 0.0);
+            if (best.shape < 0 || us < least) {
+                least = us;
+                best = ProductPlan{shape, (int)ranges, (int)range, ranges > 1 ? (size_t)(ranges * sums) : 0};
+            }
+        }
+    }
+    return best;
+}
+
+template <typename S, typename K>
+static int launch_tiles(hipStream_t s, ProductArgs a, K k, int ranges)
 {
     a.tiles_o = (a.d_out + S::MO - 1) / S::MO;
-    const int64_t tiles = (a.rows + S::MT - 1) / S::MT;
-    if (tiles * a.tiles_o > 0x7FFFFFFF) return ZIPML_EINVAL;
+    const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * ranges;
+    if (all > 0x3FFFFFFF) return ZIPML_EINVAL;
     a.tiles_t = (int)tiles;
     static std::atomic<uint64_t> done;
-    const auto k = k_row8_product<T, S>;
     if (allow_lds((const void *)k, S::kLds, done)) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3((uint32_t)(tiles * a.tiles_o)), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL(k, dim3((uint32_t)all), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
+}
+
+template <typename T>
+static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, void *workspace)
+{
+    a.range = p.range;
+    a.part = 0;
+    if (p.ranges > 1) {
+        ProductArgs parts = a;
+        parts.y = workspace;
+        parts.ldy = round_up(a.d_out, 4);
+        a.part = parts.part = a.rows * parts.ldy;
+        int rc = ZIPML_EINVAL;
+        switch (p.shape) {
+#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<S>(s, parts, k_row8_product<int, S>, p.ranges); break; }
+            ZIPML_PRODUCT_TILE(TILE)
+#undef TILE
+        }
+        if (rc) return rc;
+        const int64_t blocks = (a.rows * (parts.ldy / 4) + 255) / 256;
+        hipLaunchKernelGGL(k_row8_product_join<T>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (const int *)workspace, parts.ldy, p.ranges);
+        return hip_check(hipGetLastError());
+    }
+    switch (p.shape) {
+#define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, kStep, waves> S; return launch_tiles<S>(s, a, k_row8_product_split<T, S>, 1); }
+#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<S>(s, a, k_row8_product<T, S>, 1); }
+        ZIPML_PRODUCT_SPLIT(SPLIT)
+        ZIPML_PRODUCT_TILE(TILE)
+#undef SPLIT
+#undef TILE
+    }
+    return ZIPML_EINVAL;
 }
 
 }  // namespace zipml
@@ -158,9 +487,12 @@ static bool product_sizes_ok(int64_t rows, int64_t d_out, int64_t d_in)
 }
 constexpr int64_t kProductMaxIn = 131071;      // 128 * 128 * d_in < 2^31
 
+static size_t product_workspace(const ProductPlan &p) { return p.workspace < 256 ? 256 : p.workspace; }
+
 extern "C" size_t zipml_row8_product_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in)
 {
-    return product_sizes_ok(rows, d_out, d_in) && d_in <= kProductMaxIn ? 256 : 0;
+    if (!product_sizes_ok(rows, d_out, d_in) || d_in > kProductMaxIn) return 0;
+    return product_workspace(product_plan(rows, d_out, d_in));
 }
 
 extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, const float *x_scales_dev, const void *w_dev,
@@ -173,13 +505,13 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
         ldy < d_out || ldy > (1ll << 60) / rows)
         return ZIPML_EINVAL;
     if (d_in > kProductMaxIn) return ZIPML_ERANGE;
-    if (!workspace_dev || workspace_bytes < zipml_row8_product_workspace_bytes(rows, d_out, d_in)) return ZIPML_EWORKSPACE;
+    const ProductPlan p = product_plan(rows, d_out, d_in);
+    if (!workspace_dev || workspace_bytes < product_workspace(p)) return ZIPML_EWORKSPACE;
     if (!aligned16(x_dev) || !aligned16(w_dev) || !aligned16(y_dev) || !aligned16(workspace_dev) || !aligned4(x_scales_dev) ||
         !aligned4(w_scales_dev) || !aligned4(bias_dev))
         return ZIPML_EALIGN;
     ProductArgs a{(const uint8_t *)x_dev, (const uint8_t *)w_dev, x_scales_dev, w_scales_dev, bias_dev, y_dev, ldx, ldw, ldy, rows,
-                  (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0};
+                  (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0, 0, 0};
     hipStream_t s = entry_stream(stream);
-    typedef ProductShape<128, 128, 2, 2> S;
-    return dtype == ZIPML_F32 ? launch_product<float, S>(s, a) : launch_product<__bf16, S>(s, a);
+    return dtype == ZIPML_F32 ? launch_product<float>(s, a, p, workspace_dev) : launch_product<__bf16>(s, a, p, workspace_dev);
 }
