@@ -31,15 +31,17 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
 {
     __shared__ double scratch_sum[2][S::kThreads / kWave];
     __shared__ uint32_t scratch_max[2][S::kThreads / kWave];
-    const int lane = threadIdx.x % S::TPR, team = threadIdx.x / S::TPR;
+    const int lane = S::lane(), team = S::team();
     constexpr int NV = S::NV ? S::NV : 1;
     float gain[NV][8];
     auto load_gain = [&](int64_t u, float (&g)[8]) {
-        if (a.gain) {
-            load8(a.gain + u * 8, a.cols - u * 8, g);
-        } else {
+        if (!a.gain) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) g[k] = 1.0f;
+        } else if constexpr (S::NV > 0) {
+            Row<float>(a.gain, 0, a.cols).load8((int)u, g);
+        } else {
+            load8(a.gain + u * 8, a.cols - u * 8, g);
         }
     };
     if constexpr (S::NV > 0)
@@ -49,25 +51,46 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + team; row < a.rows; row += (int64_t)gridDim.x * S::kRows, turn ^= 1) {
         float v[NV][8];
         double square = 0;
-        // r of unit u, written to the sum's row where there is one
+        // eight values of a tensor's row
+        auto get = [&](const void *tensor, int64_t ld, int64_t u, float (&w)[8]) {
+            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
+            else load8((const T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
+        };
+        auto set = [&](void *tensor, int64_t ld, int64_t u, const float (&w)[8]) {
+            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).store8((int)u, w);
+            else store8((T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
+        };
+        auto added = [&](float (&w)[8], const float (&o)[8]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = rounded<T>(w[k] + o[k]);
+        };
         auto take = [&](int64_t u, float (&w)[8]) {
-            const int64_t left = a.cols - u * 8;
-            load8((const T *)a.x + row * a.ldx + u * 8, left, w);
+            get(a.x, a.ldx, u, w);
             if (a.add) {
                 float o[8];
-                load8((const T *)a.add + row * a.ldadd + u * 8, left, o);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = rounded<T>(w[k] + o[k]);
+                get(a.add, a.ldadd, u, o);
+                added(w, o);
             }
         };
         auto squares = [&](int64_t u, const float (&w)[8]) {
-            if (a.sum) store8((T *)a.sum + row * a.ldsum + u * 8, a.cols - u * 8, w);
+            if (a.sum) set(a.sum, a.ldsum, u, w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) square = __builtin_fma((double)w[k], (double)w[k], square);
         };
         if constexpr (S::NV > 0) {
+            if (a.add) {                   // (all loads before the first is used)
+                float o[NV][8];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) take(lane + k * S::TPR, v[k]);
+                for (int k = 0; k < NV; ++k) {
+                    get(a.x, a.ldx, lane + k * S::TPR, v[k]);
+                    get(a.add, a.ldadd, lane + k * S::TPR, o[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < NV; ++k) added(v[k], o[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) get(a.x, a.ldx, lane + k * S::TPR, v[k]);
+            }
 #pragma unroll
             for (int k = 0; k < NV; ++k) squares(lane + k * S::TPR, v[k]);
         } else {
@@ -81,7 +104,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
         if (a.rstd && lane == 0) a.rstd[row] = rstd;
         // a row too long for the registers is read again: from the sum, which may stand in the place of x
         auto again = [&](int64_t u, float (&w)[8]) {
-            if (a.sum) load8((const T *)a.sum + row * a.ldsum + u * 8, a.cols - u * 8, w);
+            if (a.sum) get(a.sum, a.ldsum, u, w);
             else take(u, w);
             load_gain(u, gain[0]);
         };
@@ -110,7 +133,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
         }
         auto put = [&](int64_t u, const float (&w)[8]) {
             if (a.codes && u < a.units) *reinterpret_cast<u32x2 *>(a.codes + row * a.ldc + u * 8) = row8_nearest8(w, s);
-            if (a.y) store8((T *)a.y + row * a.ldy + u * 8, a.cols - u * 8, w);
+            if (a.y) set(a.y, a.ldy, u, w);
         };
         if constexpr (S::NV > 0) {
 #pragma unroll
@@ -138,15 +161,17 @@ template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
 {
     __shared__ float scratch[2][S::kThreads / kWave];
-    const int lane = threadIdx.x % S::TPR, team = threadIdx.x / S::TPR;
+    const int lane = S::lane(), team = S::team();
     constexpr int NV = S::NV ? S::NV : 1;
     float gain[NV][8], dgain[NV][8] = {};
     auto load_gain = [&](int64_t u, float (&g)[8]) {
-        if (a.gain) {
-            load8(a.gain + u * 8, a.cols - u * 8, g);
-        } else {
+        if (!a.gain) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) g[k] = 1.0f;
+        } else if constexpr (S::NV > 0) {
+            Row<float>(a.gain, 0, a.cols).load8((int)u, g);
+        } else {
+            load8(a.gain + u * 8, a.cols - u * 8, g);
         }
     };
     float *part = a.part ? a.part + blockIdx.x * a.pitch : nullptr;
@@ -159,14 +184,19 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + team; row < a.rows; row += (int64_t)gridDim.x * S::kRows, turn ^= 1) {
         const float rstd = a.rstd[row];
-        float g[NV][8], n[NV][8], along = 0.0f;
+        float g[NV][8], n[NV][8], o[NV][8] = {}, along = 0.0f;
+        auto get = [&](const void *tensor, int64_t ld, int64_t u, float (&w)[8]) {
+            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
+            else load8((const T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
+        };
         // g = dy, n = r rstd of unit u
-        auto take = [&](int64_t u, float (&p)[8], float (&q)[8]) {
-            const int64_t left = a.cols - u * 8;
-            load8((const T *)a.dy + row * a.lddy + u * 8, left, p);
-            load8((const T *)a.sum + row * a.ldsum + u * 8, left, q);
+        auto scaled = [&](float (&q)[8]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) q[k] *= rstd;
+        };
+        auto take = [&](int64_t u, float (&p)[8], float (&q)[8]) {
+            get(a.dy, a.lddy, u, p);
+            get(a.sum, a.ldsum, u, q);
         };
         // dy n into dgain's sums, g = dy gain
         auto weigh = [&](float (&p)[8], const float (&q)[8], const float (&w)[8], float (&sums)[8]) {
@@ -180,11 +210,18 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
         if constexpr (S::NV > 0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) take(lane + k * S::TPR, g[k], n[k]);
+            if (a.dsum)
 #pragma unroll
-            for (int k = 0; k < NV; ++k) weigh(g[k], n[k], gain[k], dgain[k]);
+                for (int k = 0; k < NV; ++k) get(a.dsum, a.lddsum, lane + k * S::TPR, o[k]);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                scaled(n[k]);
+                weigh(g[k], n[k], gain[k], dgain[k]);
+            }
         } else {
             for (int64_t u = lane; u < a.units; u += S::TPR) {
                 take(u, g[0], n[0]);
+                scaled(n[0]);
                 load_gain(u, gain[0]);
                 if (part) load8(part + u * 8, 8, dgain[0]);
                 weigh(g[0], n[0], gain[0], dgain[0]);
@@ -192,29 +229,27 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
             }
         }
         along = team_sum<S::TPR>(along, scratch[turn]) / (float)a.cols;
-        auto put = [&](int64_t u, const float (&p)[8], const float (&q)[8]) {
-            const int64_t left = a.cols - u * 8;
-            float o[8];
-            if (a.dsum) {
-                load8((const T *)a.dsum + row * a.lddsum + u * 8, left, o);
-            } else {
+        auto put = [&](int64_t u, const float (&p)[8], const float (&q)[8], float (&d)[8]) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(rstd, __builtin_fmaf(-along, q[k], p[k]), o[k]);
-            store8((T *)a.dx + row * a.lddx + u * 8, left, o);
+            for (int k = 0; k < 8; ++k) d[k] = __builtin_fmaf(rstd, __builtin_fmaf(-along, q[k], p[k]), d[k]);
+            if constexpr (S::NV > 0) Row<T>(a.dx, row * a.lddx, a.cols).store8((int)u, d);
+            else store8((T *)a.dx + row * a.lddx + u * 8, a.cols - u * 8, d);
         };
         if constexpr (S::NV > 0) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) put(lane + k * S::TPR, g[k], n[k]);
+            for (int k = 0; k < NV; ++k) put(lane + k * S::TPR, g[k], n[k], o[k]);
         } else {
             for (int64_t u = lane; u < a.units; u += S::TPR) {
                 take(u, g[0], n[0]);
+                scaled(n[0]);
                 load_gain(u, gain[0]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) g[0][k] *= gain[0][k];
-                put(u, g[0], n[0]);
+                for (int k = 0; k < 8; ++k) {
+                    g[0][k] *= gain[0][k];
+                    o[0][k] = 0.0f;
+                }
+                if (a.dsum) get(a.dsum, a.lddsum, u, o[0]);
+                put(u, g[0], n[0], o[0]);
             }
         }
     }
@@ -244,22 +279,25 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
     }
 }
 
-// dgain from the workgroups' sums, in an order of their number alone: a lane takes one column, each of the sixteen waves every sixteenth row.
+// dgain from the workgroups' sums, in an order of their number alone: sixteen lanes take sixteen columns, each of a workgroup's 64 such
+// sets every 64th row of sums.
 __global__ __launch_bounds__(1024) void k_norm_dgain(const float *part, int parts, int64_t pitch, int64_t cols, float *dgain, int add)
 {
-    __shared__ float sums[16][kWave];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+    __shared__ float sums[64][17];
+    const int lane = threadIdx.x & 15, set = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + lane;     // (the rows of sums are padded to sixteen)
     float s = 0.0f;
-    if (c < cols)
-#pragma unroll 8
-        for (int p = wave; p < parts; p += 16) s += part[p * pitch + c];
-    sums[wave][lane] = s;
+#pragma unroll 4
+    for (int p = set; p < parts; p += 64) s += part[p * pitch + c];
+    sums[set][lane] = s;
     __syncthreads();
-    if (wave > 0 || c >= cols) return;
+    if (set >= 4) return;
+    s = 0.0f;
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += sums[w][lane];
-    dgain[c] = add ? dgain[c] + s : s;
+    for (int w = 0; w < 16; ++w) s += sums[set * 16 + w][lane];
+    s += __shfl_xor(s, 16, kWave);
+    s += __shfl_xor(s, 32, kWave);
+    if (set == 0 && c < cols) dgain[c] = add ? dgain[c] + s : s;
 }
 
 // Workgroups of the backward pass: each one writes a row of sums, 256 MiB of them at most.
@@ -291,7 +329,7 @@ extern "C" int zipml_norm_forward(void *stream, const void *x_dev, int64_t ldx, 
     const NormArgs a{x_dev, add_dev, gain_dev, sum_dev, y_dev, (uint8_t *)codes_dev, scales_dev, rstd_dev, ldx, ldadd, ldsum, ldy,
                      ldc, rows, cols, round_up(cols, kRow8Unit) / 8, eps};
     hipStream_t s = entry_stream(stream);
-    return with_row_shape(a.units, [&](auto shape) {
+    return with_row_shape(rows, a.units, kRowUnits, [&](auto shape) {
         using S = decltype(shape);
         const int64_t blocks = (rows + S::kRows - 1) / S::kRows;
         const auto k = dtype == ZIPML_F32 ? k_norm_forward<float, S> : k_norm_forward<__bf16, S>;
@@ -324,13 +362,13 @@ extern "C" int zipml_norm_backward(void *stream, const void *dy_dev, int64_t ldd
     NormGradArgs a{dy_dev, sum_dev, dsum_dev, gain_dev, rstd_dev, dx_dev, dgain_dev ? (float *)workspace_dev : nullptr, lddy, ldsum,
                    lddsum, lddx, rows, cols, round_up(cols, kRow8Unit) / 8, round_up(cols, kRow8Unit)};
     hipStream_t s = entry_stream(stream);
-    return with_row_shape(a.units, [&](auto shape) {
+    return with_row_shape(rows, a.units, kRowUnits / 2, [&](auto shape) {
         using S = decltype(shape);
         const int64_t groups = norm_groups(rows, cols, S::kRows);
         const auto k = dtype == ZIPML_F32 ? k_norm_backward<float, S> : k_norm_backward<__bf16, S>;
         hipLaunchKernelGGL(k, dim3((uint32_t)groups), dim3(S::kThreads), 0, s, a);
         if (const int rc = hip_check(hipGetLastError()); rc || !dgain_dev) return rc;
-        hipLaunchKernelGGL(k_norm_dgain, dim3((uint32_t)((cols + kWave - 1) / kWave)), dim3(1024), 0, s, a.part, (int)groups, a.pitch,
+        hipLaunchKernelGGL(k_norm_dgain, dim3((uint32_t)(a.pitch / 16)), dim3(1024), 0, s, a.part, (int)groups, a.pitch,
                            cols, dgain_dev, flags & ZIPML_NORM_ADD ? 1 : 0);
         return hip_check(hipGetLastError());
     });

@@ -8,6 +8,8 @@
 
 namespace zipml {
 
+constexpr int64_t kFewRows = 512;                  // fewer rows than these are given more threads each
+constexpr int64_t kRowUnits = 4096;                // longest rows (in units of eight values) that wait in registers
 constexpr int kRow8Unit = 16;                       // bytes that a row of codes is padded to
 constexpr int64_t kRow8MaxPitch = 1ll << 22;        // so that the offsets within a tile of rows stay below 2^31
 
@@ -105,23 +107,84 @@ __device__ __forceinline__ F team_sum(F v, F *scratch)
     return v;
 }
 
+// ---- rows as buffers --------------------------------------------------------------------------
+// A row of at most 2^28 values, read and written eight neighbouring values at a time without a branch: what lies behind its end reads
+// as zeros and is not written.  (With a branch each load would wait for the one before.)  The end is exact to a dword: the last of an odd
+// number of bf16 values goes by itself.  Rows may start at any element.
+template <typename T>
+struct Row {
+    T *base;
+    __amdgpu_buffer_rsrc_t r;
+    int cols;
+    __device__ __forceinline__ Row(const void *tensor, int64_t at, int64_t cols_) : base((T *)tensor + at), cols((int)cols_)
+    {
+        r = __builtin_amdgcn_make_buffer_rsrc(base, 0, cols * (int)sizeof(T), 0x00020000);
+    }
+    __device__ __forceinline__ bool odd() const { return sizeof(T) == 2 && (cols & 1); }
+    __device__ __forceinline__ void load8(int u, float (&v)[8]) const
+    {
+        const u32x4 a = __builtin_amdgcn_raw_buffer_load_b128(r, u * 8 * (int)sizeof(T), 0, 0);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[2 * k] = as_f32(a[k] << 16);
+                v[2 * k + 1] = as_f32(a[k] & 0xFFFF0000u);
+            }
+        } else {
+            const u32x4 b = __builtin_amdgcn_raw_buffer_load_b128(r, u * 32 + 16, 0, 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t x = a[k], y = b[k];
+                v[k] = as_f32(x);
+                v[4 + k] = as_f32(y);
+            }
+        }
+        if (odd()) {                       // (cols - 1 is even, so the value is one of v[0], v[2], v[4], v[6])
+            const float last = u == (cols >> 3) ? (float)base[cols - 1] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) v[k] = u * 8 + k == cols - 1 ? last : v[k];
+        }
+    }
+    __device__ __forceinline__ void store8(int u, const float (&v)[8]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 o;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = (__bf16)v[k];
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), r, u * 16, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])}, r, u * 32, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])}, r, u * 32 + 16, 0, 0);
+        }
+        if (odd())
+#pragma unroll
+            for (int k = 0; k < 8; k += 2)
+                if (u * 8 + k == cols - 1) base[cols - 1] = (T)v[k];
+    }
+};
+
 // How a row of `units` units of eight values is dealt: TPR threads, up to NV units each; NV = 0: as many as there are.
 template <int TPR_, int NV_>
 struct RowShape {
     static constexpr int TPR = TPR_, NV = NV_, kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
+    // the team's number in the workgroup, the same for a whole wave
+    static __device__ __forceinline__ int team() { return TPR == kThreads ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); }
+    static __device__ __forceinline__ int lane() { return threadIdx.x % TPR; }
 };
-// Calls f with the shape for rows of so many units.
+// Calls f with the shape for `rows` rows of so many units, of which registers are to hold `most` at most.
 template <typename F>
-inline int with_row_shape(int64_t units, F f)
+inline int with_row_shape(int64_t rows, int64_t units, int64_t most, F f)
 {
+    if (units > most) return f(RowShape<1024, 0>());
     if (units <= 64) return f(RowShape<64, 1>());
+    if (rows < kFewRows && units <= 256) return f(RowShape<256, 1>());
+    if (rows < kFewRows && units <= 1024) return f(RowShape<1024, 1>());
     if (units <= 128) return f(RowShape<64, 2>());
     if (units <= 256) return f(RowShape<64, 4>());
     if (units <= 512) return f(RowShape<256, 2>());
     if (units <= 1024) return f(RowShape<256, 4>());
     if (units <= 2048) return f(RowShape<1024, 2>());
-    if (units <= 4096) return f(RowShape<1024, 4>());
-    return f(RowShape<1024, 0>());
+    return f(RowShape<1024, 4>());
 }
 
 }  // namespace zipml

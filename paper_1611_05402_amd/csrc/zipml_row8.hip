@@ -17,10 +17,11 @@ template <typename T, typename S, bool DRAWS>
 __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
 {
     __shared__ uint32_t scratch[2][S::kThreads / kWave];
-    const int lane = threadIdx.x % S::TPR, team = threadIdx.x / S::TPR;
+    const int lane = S::lane(), team = S::team();
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + team; row < a.rows; row += (int64_t)gridDim.x * S::kRows, turn ^= 1) {
         const T *x = (const T *)a.x + row * a.ldx;
+        const Row<T> in(a.x, row * a.ldx, a.cols);
         uint8_t *codes = a.codes + row * a.ldc;
         float v[S::NV ? S::NV : 1][8];
         uint32_t top = 0;
@@ -32,10 +33,7 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
         };
         if constexpr (S::NV > 0) {
 #pragma unroll
-            for (int k = 0; k < S::NV; ++k) {
-                const int64_t u = lane + k * S::TPR;
-                load8(x + u * 8, a.cols - u * 8, v[k]);
-            }
+            for (int k = 0; k < S::NV; ++k) in.load8(lane + k * S::TPR, v[k]);
 #pragma unroll
             for (int k = 0; k < S::NV; ++k) top = top_of(v[k], top);
         } else {
@@ -114,7 +112,7 @@ extern "C" int zipml_row8_encode(void *stream, const void *x_dev, int dtype, int
     const Row8Args a{x_dev, (uint8_t *)codes_dev, scales_dev, ldx, ldc, rows, cols, round_up(cols, kRow8Unit) / 8, seed, epoch,
                      (uint32_t)(kActStream + tag)};
     hipStream_t s = entry_stream(stream);
-    return with_row_shape(a.units, [&](auto shape) {
+    return with_row_shape(rows, a.units, kRowUnits, [&](auto shape) {
         using S = decltype(shape);
         const bool draws = rounding == ZIPML_STOCHASTIC;
         return dtype == ZIPML_F32 ? launch_encode<float, S>(s, a, draws) : launch_encode<__bf16, S>(s, a, draws);

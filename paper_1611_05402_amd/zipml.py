@@ -471,17 +471,19 @@ def _codes(where, name, t):
     """The address of rows of codes, which lie a leading dimension of the caller's apart."""
     if t is None:
         return None
-    s = t.stride()
-    if t.dtype is not _KINDS["int8"] or (s and s[-1] != 1 and t.shape[-1] > 1):
-        raise ZipmlError(EINVAL, f"{where}: {name} has to be int8 rows of codes side by side, not {t.dtype} with strides {s}")
+    if t.dtype is not _KINDS["int8"] or not (t.is_contiguous() or t.shape[-1:] == _ONE or t.stride()[-1:] == _ONE):
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be int8 rows of codes side by side, not {t.dtype} with strides {t.stride()}")
     return t.data_ptr()
 
 
-def _same_rows(where, kind, *named):
-    """Whether the rows of further tensors (name, tensor or None) are of type `kind` with their values side by side."""
-    for name, t in named:
-        if t is not None and (t.dtype is not kind or (t.stride()[-1:] != _ONE and _rows(where, t) < 0)):
-            raise ZipmlError(EINVAL, f"{where}: {name} is {t.dtype}, the other rows are {kind}")
+def _row(where, name, t, kind):
+    """The address of rows of type `kind`; None if there are none."""
+    if t is None:
+        return None
+    if t.dtype is not kind or not (t.is_contiguous() or t.shape[-1:] == _ONE or t.stride()[-1:] == _ONE):
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be rows of {kind} side by side as the others, not {t.dtype} with strides "
+                                 f"{t.stride()}")
+    return t.data_ptr()
 
 
 def row8_encode(x, rows, cols, ldx, codes, ldc, scales, *, rounding=NEAREST, seed=0, epoch=0, tag=0, stream=None):
@@ -516,11 +518,9 @@ def norm_forward(x, ldx, rows, cols, eps, *, gain=None, add=None, ldadd=0, sum=N
     """Root-mean-square norm of x + add: its result in y (x's type) or in codes with scales; sum gets x + add, rstd (fp32) what
     the backward pass needs.  gain, scales, rstd: fp32."""
     w = "zipml_norm_forward"
-    kind = _rows(w, x)
-    if kind >= 0:
-        _same_rows(w, x.dtype, ("add", add), ("sum", sum), ("y", y))
-    _check(lib().zipml_norm_forward(_stream(stream), _ptr(x), ldx, _ptr(add), ldadd, kind, rows, cols,
-                                    _array(w, "gain", gain, "float32"), eps, _ptr(sum), ldsum, _ptr(y), ldy,
+    k = x.dtype
+    _check(lib().zipml_norm_forward(_stream(stream), _row(w, "x", x, k), ldx, _row(w, "add", add, k), ldadd, _CODES[k], rows, cols,
+                                    _array(w, "gain", gain, "float32"), eps, _row(w, "sum", sum, k), ldsum, _row(w, "y", y, k), ldy,
                                     _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32"),
                                     _array(w, "rstd", rstd, "float32")), w)
 
@@ -534,12 +534,10 @@ def norm_backward(dy, lddy, sum, ldsum, rows, cols, rstd, dx, lddx, workspace=No
     """Gradients dx and dgain of norm_forward from the sum and rstd that it kept; dsum: the gradient that reaches the sum by the
     residual stream; flags: NORM_ADD adds to dgain.  The workspace is needed for dgain only."""
     w = "zipml_norm_backward"
-    kind = _rows(w, dy)
-    if kind >= 0:
-        _same_rows(w, dy.dtype, ("sum", sum), ("dsum", dsum), ("dx", dx))
-    _check(lib().zipml_norm_backward(_stream(stream), _ptr(dy), lddy, _ptr(sum), ldsum, kind, rows, cols,
-                                     _array(w, "gain", gain, "float32"), _array(w, "rstd", rstd, "float32"), _ptr(dsum), lddsum,
-                                     _ptr(dx), lddx, _array(w, "dgain", dgain, "float32"), flags, _ptr(workspace),
+    k = dy.dtype
+    _check(lib().zipml_norm_backward(_stream(stream), _row(w, "dy", dy, k), lddy, _row(w, "sum", sum, k), ldsum, _CODES[k], rows, cols,
+                                     _array(w, "gain", gain, "float32"), _array(w, "rstd", rstd, "float32"), _row(w, "dsum", dsum, k),
+                                     lddsum, _row(w, "dx", dx, k), lddx, _array(w, "dgain", dgain, "float32"), flags, _ptr(workspace),
                                      0 if workspace is None else workspace.nbytes), w)
 
 
