@@ -6,21 +6,23 @@
 // these up (every workgroup for itself, in the same order) and scales.  Squares are summed in 64 bits, so that no gradient that
 // fp32 holds overflows and the norm does not depend on the order.  The second pass goes from the last chunk to the first: what the
 // first pass has read last is still in the caches.
-#include "zipml_act.h"
+#include "zipml_row8.h"
 
 namespace zipml {
 
 constexpr int kClipTensors = 96;          // of a launch: what its arguments hold
 constexpr int kClipGroups = 1024;         // workgroups of a launch
-constexpr int kClipUnits = 4;             // units of eight values that a thread has under way
-constexpr int64_t kClipChunk = 256 * 8 * kClipUnits;
+// Units of eight values that a thread has under way: four, or one where chunks of four would leave compute units idle (1.6 million
+// values: XXX).
+constexpr int kClipMany = 4, kClipFew = 1;
+constexpr int64_t clip_chunk(int units) { return 256 * 8 * units; }
 
 struct ClipTensor {
     const void *grad;
     void *out;
     int64_t count;
     uint32_t first;                       // chunks of the tensors before it
-    uint8_t grad_bf16, out_bf16;
+    uint32_t types;                       // 1: bf16 gradient, 2: bf16 output
 };
 struct ClipArgs {
     ClipTensor t[kClipTensors];
@@ -29,80 +31,114 @@ struct ClipArgs {
 };
 static_assert(sizeof(ClipArgs) + 64 <= 4096, "kernel arguments");
 
-// The tensor that a chunk belongs to.
-__device__ __forceinline__ int clip_tensor(const ClipArgs &a, uint32_t chunk)
-{
-    int lo = 0, hi = a.n;                 // t[lo].first <= chunk < t[hi].first
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.t[mid].first <= chunk) lo = mid;
-        else hi = mid;
+// The launch's tensors, in the registers of each wave: a lane keeps those of its number and of 64 more.  Read all at once: kernel
+// arguments lie far away, and a search among them would wait for each step.
+struct ClipTable {
+    ClipTensor own[2];
+    int n;
+    __device__ __forceinline__ explicit ClipTable(const ClipArgs &a) : n(a.n)
+    {
+        const int lane = threadIdx.x & 63;
+        own[0] = a.t[lane < n ? lane : 0];
+        own[1] = a.t[lane + 64 < n ? lane + 64 : 0];
     }
-    return lo;
-}
+    static __device__ __forceinline__ uint64_t lane_of(uint64_t v, int l)
+    {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), l);
+        return (uint64_t)hi << 32 | lo;
+    }
+    // The tensor that a chunk belongs to: the last of those that begin at it or before.
+    __device__ __forceinline__ ClipTensor at(uint32_t chunk) const
+    {
+        const int lane = threadIdx.x & 63;
+        const int k = __builtin_popcountll(__ballot(lane < n && own[0].first <= chunk)) +
+                      __builtin_popcountll(__ballot(lane + 64 < n && own[1].first <= chunk)) - 1;
+        const ClipTensor &t = k < 64 ? own[0] : own[1];
+        const int l = k & 63;
+        ClipTensor r;
+        r.grad = (const void *)lane_of((uint64_t)t.grad, l);
+        r.out = (void *)lane_of((uint64_t)t.out, l);
+        r.count = (int64_t)lane_of((uint64_t)t.count, l);
+        r.first = (uint32_t)__builtin_amdgcn_readlane((int)t.first, l);
+        r.types = (uint32_t)__builtin_amdgcn_readlane((int)t.types, l);
+        return r;
+    }
+};
 
-template <typename T>
-__device__ __forceinline__ void clip_load(const void *p, int64_t at, int64_t count, float (&v)[kClipUnits][8])
+template <typename T, int U>
+__device__ __forceinline__ void clip_load(const void *p, int64_t at, int64_t count, float (&v)[U][8])
 {
     const T *x = (const T *)p + at;
-    if (at - threadIdx.x * 8 + kClipChunk <= count) {
+    if (at - threadIdx.x * 8 + clip_chunk(U) <= count) {
 #pragma unroll
-        for (int q = 0; q < kClipUnits; ++q) load8(x + q * 2048, 8, v[q]);
+        for (int q = 0; q < U; ++q) load8(x + q * 2048, 8, v[q]);
     } else {
 #pragma unroll
-        for (int q = 0; q < kClipUnits; ++q) load8(x + q * 2048, count - at - q * 2048, v[q]);
+        for (int q = 0; q < U; ++q) load8(x + q * 2048, count - at - q * 2048, v[q]);
     }
 }
-__device__ __forceinline__ void clip_values(const ClipTensor &t, int64_t at, float (&v)[kClipUnits][8])
+template <int U>
+__device__ __forceinline__ void clip_values(const ClipTensor &t, int64_t at, float (&v)[U][8])
 {
-    if (t.grad_bf16) clip_load<__bf16>(t.grad, at, t.count, v);
+    if (t.types & 1) clip_load<__bf16>(t.grad, at, t.count, v);
     else clip_load<float>(t.grad, at, t.count, v);
 }
 
+template <int U>
 __global__ __launch_bounds__(256) void k_clip_norm(ClipArgs a, double *part)
 {
-    __shared__ double scratch[8];
+    __shared__ double scratch[4];
+    const ClipTable table(a);
     double sum = 0;
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const ClipTensor &t = a.t[clip_tensor(a, c)];
-        float v[kClipUnits][8];
-        clip_values(t, (int64_t)(c - t.first) * kClipChunk + threadIdx.x * 8, v);
+        const ClipTensor t = table.at(c);
+        float v[U][8];
+        clip_values(t, (int64_t)(c - t.first) * clip_chunk(U) + threadIdx.x * 8, v);
 #pragma unroll
-        for (int q = 0; q < kClipUnits; ++q)
+        for (int q = 0; q < U; ++q)
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum = __builtin_fma((double)v[q][k], (double)v[q][k], sum);
     }
-    sum = block_sum(sum, scratch);
+    sum = team_sum<256>(sum, scratch);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
+template <int U>
 __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, const double *part, int parts, float max_norm, float *norm_out)
 {
-    __shared__ double scratch[8];
+    __shared__ double scratch[4];
     double sum = 0;
     for (int p = threadIdx.x; p < parts; p += 256) sum += part[p];
-    const double norm = __builtin_sqrt(block_sum(sum, scratch));
+    // (the first chunk is on its way while the norm is formed)
+    const ClipTable table(a);
+    float v[U][8];
+    uint32_t i = blockIdx.x;
+    ClipTensor t{};
+    auto fetch = [&]() {
+        t = table.at(a.chunks - 1 - i);
+        if (t.out) clip_values(t, (int64_t)(a.chunks - 1 - i - t.first) * clip_chunk(U) + threadIdx.x * 8, v);
+    };
+    if (i < a.chunks) fetch();
+    const double norm = __builtin_sqrt(team_sum<256>(sum, scratch));
     const float factor = norm <= (double)max_norm ? 1.0f : (float)((double)max_norm / norm);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) {
         norm_out[0] = (float)norm;
         norm_out[1] = factor;
     }
-    for (uint32_t i = blockIdx.x; i < a.chunks; i += gridDim.x) {
-        const uint32_t c = a.chunks - 1 - i;
-        const ClipTensor &t = a.t[clip_tensor(a, c)];
-        // (a tensor in place needs no second pass where nothing is scaled)
-        if (!t.out || (t.out == t.grad && factor == 1.0f)) continue;
-        const int64_t at = (int64_t)(c - t.first) * kClipChunk + threadIdx.x * 8;
-        float v[kClipUnits][8];
-        clip_values(t, at, v);
+    while (i < a.chunks) {
+        const int64_t at = (int64_t)(a.chunks - 1 - i - t.first) * clip_chunk(U) + threadIdx.x * 8;
+        // (a tensor in place stays as it is where nothing is scaled)
+        if (t.out && (t.out != t.grad || factor != 1.0f))
 #pragma unroll
-        for (int q = 0; q < kClipUnits; ++q) {
+            for (int q = 0; q < U; ++q) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[q][k] *= factor;
-            const int64_t to = at + q * 2048, left = t.count - to;
-            if (t.out_bf16) store8((__bf16 *)t.out + to, left, v[q]);
-            else store8((float *)t.out + to, left, v[q]);
-        }
+                for (int j = 0; j < 8; ++j) v[q][j] *= factor;
+                const int64_t to = at + q * 2048, left = t.count - to;
+                if (t.types & 2) store8<true>((__bf16 *)t.out + to, left, v[q]);
+                else store8<true>((float *)t.out + to, left, v[q]);
+            }
+        i += gridDim.x;
+        if (i < a.chunks) fetch();
     }
 }
 
@@ -135,6 +171,13 @@ extern "C" int zipml_clip(void *stream, const zipml_clip_tensor *tensors_host, i
         const zipml_clip_tensor &t = tensors_host[i];
         if (!aligned_as(t.grad_dev, t.grad_dtype) || !aligned_as(t.out_dev, t.out_dtype)) return ZIPML_EALIGN;
     }
+    int64_t most = 0;                      // chunks of four units of the launch with most of them
+    for (int64_t i0 = 0, n = 0; i0 < n_tensors; ++i0) {
+        n = (i0 % kClipTensors ? n : 0) + (tensors_host[i0].count + clip_chunk(kClipMany) - 1) / clip_chunk(kClipMany);
+        most = n > most ? n : most;
+    }
+    const bool few = most < kClipGroups;
+    const int64_t chunk = clip_chunk(few ? kClipFew : kClipMany);
     hipStream_t s = entry_stream(stream);
     double *part = (double *)workspace_dev;
     int parts = 0;
@@ -146,16 +189,16 @@ extern "C" int zipml_clip(void *stream, const zipml_clip_tensor *tensors_host, i
             bool writes = i0 == 0;         // (the first launch of the second pass hands the norm on)
             for (int k = 0; k < a.n; ++k) {
                 const zipml_clip_tensor &t = tensors_host[i0 + k];
-                a.t[k] = ClipTensor{t.grad_dev, t.out_dev, t.count, a.chunks, t.grad_dtype == ZIPML_BF16, t.out_dtype == ZIPML_BF16};
-                a.chunks += (uint32_t)((t.count + kClipChunk - 1) / kClipChunk);
+                a.t[k] = ClipTensor{t.grad_dev, t.out_dev, t.count, a.chunks, (t.grad_dtype == ZIPML_BF16 ? 1u : 0u) | (t.out_dtype == ZIPML_BF16 ? 2u : 0u)};
+                a.chunks += (uint32_t)((t.count + chunk - 1) / chunk);
                 writes |= t.out_dev != nullptr;
             }
             const int groups = a.chunks < 1 ? 1 : a.chunks < (uint32_t)kClipGroups ? (int)a.chunks : kClipGroups;
             if (pass == 0) {
-                hipLaunchKernelGGL(k_clip_norm, dim3(groups), dim3(256), 0, s, a, part + parts);
+                hipLaunchKernelGGL(few ? k_clip_norm<kClipFew> : k_clip_norm<kClipMany>, dim3(groups), dim3(256), 0, s, a, part + parts);
                 parts += groups;
             } else if (writes) {
-                hipLaunchKernelGGL(k_clip_scale, dim3(groups), dim3(256), 0, s, a, part, parts, max_norm, i0 == 0 ? norm_dev : nullptr);
+                hipLaunchKernelGGL(few ? k_clip_scale<kClipFew> : k_clip_scale<kClipMany>, dim3(groups), dim3(256), 0, s, a, part, parts, max_norm, i0 == 0 ? norm_dev : nullptr);
             }
             if (const int rc = hip_check(hipGetLastError())) return rc;
         }
