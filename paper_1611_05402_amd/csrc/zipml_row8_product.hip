@@ -17,10 +17,14 @@ struct ProductArgs {
     int64_t ldx, ldw, ldy, rows;
     int d_out, bytes;           // bytes: of a row, padding included
     int tiles_t, tiles_o;
-    int range;                  // bytes of a row that a workgroup takes, a multiple of kStep
+    int range, ranges;          // bytes of a row that a workgroup takes, a multiple of kStep; how many such ranges there are
+    int through;                // results go past the caches
     int64_t part;               // sums of a range, [rows][ldy], behind those of the one before
 };
 
+// Results that the caches would not hold until they are read: written past them (16,384 x 4,096 bf16 and 4,096 inputs: 237 us against 246,
+// 520 inputs: 67 against 78).
+constexpr int64_t kThroughLeast = 96ll << 20;
 constexpr int kStep = 128;      // codes of a row that are in LDS at a time
 
 // Rows of codes as a buffer: rows behind the last one, and what lies behind a row's padding, read as zeros.
@@ -30,11 +34,12 @@ struct CodeRows {
     __device__ __forceinline__ CodeRows(const uint8_t *base, int64_t left, int64_t ld_, int bytes_) : ld((int)ld_), bytes(bytes_)
     {
         const int64_t n = (left - 1) * ld_ + bytes_;
-        r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, left < 1 ? 0 : n > 0x7FFFFF00 ? 0x7FFFFF00 : (int)n, 0x00020000);
+        r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, left < 1 ? 0 : n > 0x7FFE0000 ? 0x7FFE0000 : (int)n, 0x00020000);
     }
-    __device__ __forceinline__ u32x4 load16(int row, int at) const
+    // 16 codes at an offset, `rows` rows further down; zeros where there are none
+    __device__ __forceinline__ u32x4 load16(bool there, int at, int rows) const
     {
-        return __builtin_amdgcn_raw_buffer_load_b128(r, at < bytes ? row * ld + at : 0x7FFFFFF0, 0, 0);
+        return __builtin_amdgcn_raw_buffer_load_b128(r, there ? at + rows * ld : 0x7FFFFFF0, 0, 0);
     }
 };
 
@@ -83,14 +88,14 @@ struct Out4 {
     }
 };
 
-// Workgroups go to the eight XCDs in turn; each XCD gets a run of neighbouring tiles, in bands four outputs deep, so that its L2
-// serves rows of both operands to several of them.
+// Workgroups go to the eight XCDs in turn; each XCD gets a run of neighbouring tiles, in bands eight outputs deep, so that its L2
+// serves rows of both operands to several of them (16,384 tokens, 4,096 x 4,096: 237 us, with four or sixteen 240).
 __device__ __forceinline__ void tile_of(const ProductArgs &a, uint32_t n, uint32_t at, int &o, int &t)
 {
     const uint32_t xcd = at & 7, per = n >> 3, more = n & 7;
-    const uint32_t id = xcd * per + (xcd < more ? xcd : more) + (at >> 3), band = id / (4 * a.tiles_t), in = id - band * 4 * a.tiles_t;
-    const uint32_t deep = a.tiles_o - band * 4 < 4 ? a.tiles_o - band * 4 : 4;
-    o = band * 4 + in % deep;
+    const uint32_t id = xcd * per + (xcd < more ? xcd : more) + (at >> 3), band = id / (8 * a.tiles_t), in = id - band * 8 * a.tiles_t;
+    const uint32_t deep = a.tiles_o - band * 8 < 8 ? a.tiles_o - band * 8 : 8;
+    o = band * 8 + in % deep;
     t = in / deep;
 }
 
@@ -110,6 +115,87 @@ struct ProductShape {
     static_assert(kLds <= 160 * 1024, "LDS");
 };
 
+// What a wave has summed, on its way out.  A lane holds four neighbouring outputs of one token at a time.  Through LDS of its own (`out`), a
+// wave turns 32 tokens' lines of 128 bytes around and writes them 16 bytes a lane.
+template <typename T, typename S>
+__device__ __forceinline__ void write_out(const ProductArgs &a, const i32x16 (&acc)[S::TO][S::TT], char *out, int o_wave, int64_t t_wave,
+                                          uint32_t split)
+{
+    const int lane = threadIdx.x & 63;
+    const auto scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.sw), 0, a.d_out * 4, 0x00020000);
+    const auto biases = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.bias), 0, a.bias ? a.d_out * 4 : 0, 0x00020000);
+    float sx[S::TT];
+#pragma unroll
+    for (int n = 0; n < S::TT && !S::kParts; ++n) {
+        const int64_t t = t_wave + n * 32 + (lane & 31);
+        sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
+    }
+#pragma unroll
+    for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
+        constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
+        const int o = o_wave + m0 * 32 + (lane & 7) * V, left = a.d_out - o;
+        // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256; -0 leaves every value as it is)
+        f32x4 sw[S::HO][4], bias[S::HO][4];
+#pragma unroll
+        for (int m = 0; m < S::HO && !S::kParts; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4;
+                sw[m][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at, 0, 0));
+                bias[m][q] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
+            }
+        if (a.bias)
+#pragma unroll
+            for (int m = 0; m < S::HO && !S::kParts; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    bias[m][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                               biases, (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4, 0, 0));
+#pragma unroll
+        for (int n = 0; n < S::TT; ++n) {
+            const int t32 = lane & 31;
+#pragma unroll
+            for (int m = 0; m < S::HO; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    T4 r;
+                    if constexpr (S::kParts) {
+                        r = T4{acc[m0 + m][n][4 * q], acc[m0 + m][n][4 * q + 1], acc[m0 + m][n][4 * q + 2], acc[m0 + m][n][4 * q + 3]};
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            r[k] = (T)((float)acc[m0 + m][n][4 * q + k] * sx[n] * sw[m][q][k] + bias[m][q][k]);
+                    }
+                    const int byte = (m * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
+                    *reinterpret_cast<T4 *>(out + t32 * 128 + (((byte >> 4) ^ (t32 >> 1 & 7)) << 4) + (byte & 15)) = r;
+                }
+            wave_fence();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 8 * i + (lane >> 3);
+                const u32x4 line = *reinterpret_cast<const u32x4 *>(out + lds_at(r, lane & 7));
+                const int64_t t = t_wave + n * 32 + r;
+                if (t >= a.rows) continue;
+                T *const y = (T *)a.y + split * a.part + t * a.ldy + o;
+                if (left >= V) {
+                    if (a.through) __builtin_nontemporal_store((u32x4_any)line, reinterpret_cast<u32x4_any *>(y));
+                    else *reinterpret_cast<u32x4_any *>(y) = line;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k < left) {
+                            const uint32_t word = line[k * (int)sizeof(T) / 4];   // (a cast of the vector's element itself takes its first)
+                            if constexpr (sizeof(T) == 4) y[k] = __builtin_bit_cast(T, word);
+                            else y[k] = __builtin_bit_cast(__bf16, (uint16_t)(word >> (16 * (k & 1))));
+                        }
+                }
+            }
+            wave_fence();
+        }
+    }
+}
+
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 {
@@ -127,20 +213,22 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
     // The loads and the stores of a round are dealt over its steps but the last.
     constexpr int kSteps = kStep / 32, kDeals = kSteps - 1;
     u32x4 v[S::kLoads];
-    auto load = [&](int k0, int deal) {
+    constexpr int kRowsLoad = S::kThreads / 8;                      // rows that one load of all threads takes
+    const int at_w = (tid >> 3) * (int)a.ldw + (tid & 7) * 16, at_x = (tid >> 3) * (int)a.ldx + (tid & 7) * 16;
+    auto load = [&](u32x4 (&to)[S::kLoads], int k0, int deal) {
+        const bool there = k0 + (tid & 7) * 16 < a.bytes;
 #pragma unroll
         for (int q = 0; q < S::kLoads; ++q) {
             if (q * kDeals / S::kLoads != deal) continue;
-            const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
-            v[q] = (q < S::kLoadsW ? w : x).load16(c >> 3, k0 + (c & 7) * 16);
+            to[q] = q < S::kLoadsW ? w.load16(there, at_w + k0, q * kRowsLoad) : x.load16(there, at_x + k0, (q - S::kLoadsW) * kRowsLoad);
         }
     };
-    auto store = [&](char *stage, int deal) {
+    auto store = [&](const u32x4 (&from)[S::kLoads], char *stage, int deal) {
 #pragma unroll
         for (int q = 0; q < S::kLoads; ++q) {
             if (q * kDeals / S::kLoads != deal) continue;
             const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
-            *reinterpret_cast<u32x4 *>(stage + (q < S::kLoadsW ? 0 : S::MO * kStep) + lds_at(c >> 3, c & 7)) = v[q];
+            *reinterpret_cast<u32x4 *>(stage + (q < S::kLoadsW ? 0 : S::MO * kStep) + lds_at(c >> 3, c & 7)) = from[q];
         }
     };
 
@@ -155,14 +243,16 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
             fx[s & 1][n] = *reinterpret_cast<const i32x4 *>(stage + S::MO * kStep + lds_at((wt * S::TT + n) * 32 + (lane & 31), chunk));
     };
     char *here = lds, *next = lds + S::kStage;
-    i32x16 acc[S::TO][S::TT] = {};
+    {                                      // both first rounds asked for at once: the memory's latency once, not twice
+        u32x4 first[S::kLoads];
 #pragma unroll
-    for (int d = 0; d < kDeals; ++d) load(k_begin, d);
+        for (int d = 0; d < kDeals; ++d) load(first, k_begin, d);
 #pragma unroll
-    for (int d = 0; d < kDeals; ++d) {
-        store(here, d);
-        load(k_begin + kStep, d);
+        for (int d = 0; d < kDeals; ++d) load(v, k_begin + kStep, d);
+#pragma unroll
+        for (int d = 0; d < kDeals; ++d) store(first, here, d);
     }
+    i32x16 acc[S::TO][S::TT] = {};
     lds_barrier();
     read(here, 0);
     for (int k0 = k_begin; k0 < k_end; k0 += kStep) {
@@ -171,8 +261,8 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
             if (s < kDeals) {
                 read(here, s + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                store(next, s);
-                load(k0 + 2 * kStep, s);
+                store(v, next, s);
+                load(v, k0 + 2 * kStep, s);
             } else {
                 lds_barrier();
                 read(next, 0);
@@ -190,85 +280,21 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
         next = t;
     }
 
-    // A lane holds four neighbouring outputs of one token at a time.  Through LDS of its own, a wave turns 32 tokens' lines of 128
-    // bytes around and writes them 16 bytes a lane.
-    char *const out = lds + wave * S::kOut;
-    const int o_wave = o0 + wo * S::TO * 32;
-    const int64_t t_wave = t0 + wt * S::TT * 32;
-    lds_barrier();                         // (whose results may lie where another wave still reads)
-    const auto scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.sw), 0, a.d_out * 4, 0x00020000);
-    const auto biases = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.bias), 0, a.bias ? a.d_out * 4 : 0, 0x00020000);
-    float sx[S::TT];
-#pragma unroll
-    for (int n = 0; n < S::TT && !S::kParts; ++n) {
-        const int64_t t = t_wave + n * 32 + (lane & 31);
-        sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
-    }
-#pragma unroll
-    for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
-        constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
-        const int o = o_wave + m0 * 32 + (lane & 7) * V, left = a.d_out - o;
-#pragma unroll
-        for (int n = 0; n < S::TT; ++n) {
-            const int t32 = lane & 31;
-#pragma unroll
-            for (int m = 0; m < S::HO; ++m)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    typedef T T4 __attribute__((ext_vector_type(4)));
-                    T4 r;
-                    if constexpr (S::kParts) {
-                        r = T4{acc[m0 + m][n][4 * q], acc[m0 + m][n][4 * q + 1], acc[m0 + m][n][4 * q + 2], acc[m0 + m][n][4 * q + 3]};
-                    } else {
-                        const int at = (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4;
-                        const f32x4 sw = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at, 0, 0));
-                        f32x4 f;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) f[k] = (float)acc[m0 + m][n][4 * q + k] * sx[n] * sw[k];
-                        if (a.bias) f += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at, 0, 0));
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) r[k] = (T)f[k];
-                    }
-                    const int byte = (m * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
-                    *reinterpret_cast<T4 *>(out + t32 * 128 + (((byte >> 4) ^ (t32 >> 1 & 7)) << 4) + (byte & 15)) = r;
-                }
-            wave_fence();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 8 * i + (lane >> 3);
-                const u32x4 line = *reinterpret_cast<const u32x4 *>(out + lds_at(r, lane & 7));
-                const int64_t t = t_wave + n * 32 + r;
-                if (t >= a.rows) continue;
-                T *const y = (T *)a.y + split * a.part + t * a.ldy + o;
-                if (left >= V) {
-                    *reinterpret_cast<u32x4_any *>(y) = line;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < V; ++k)
-                        if (k < left) {
-                            const uint32_t word = line[k * (int)sizeof(T) / 4];   // (a cast of the vector's element itself takes its first)
-                            if constexpr (sizeof(T) == 4) y[k] = __builtin_bit_cast(T, word);
-                            else y[k] = __builtin_bit_cast(__bf16, (uint16_t)(word >> (16 * (k & 1))));
-                        }
-                }
-            }
-            wave_fence();
-        }
-    }
+    lds_barrier();                         // (the results may lie where another wave still reads)
+    write_out<T, S>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 32, t0 + wt * S::TT * 32, split);
 }
 
 // ---- few tokens, few outputs: the waves of a workgroup share the contraction -------------------
 // Where a tile has few products for its bytes, nothing is gained by sharing rows between waves; what counts is that all of a
-// compute unit's waves have loads under way.  So the waves of a workgroup take steps of KS codes of the same MO x MT tile by turns,
+// compute unit's waves have loads under way.  So the waves of a workgroup take steps of 128 codes of the same MO x MT tile by turns,
 // each through LDS of its own and without a barrier, and add up their sums at the end.
-template <int MO_, int MT_, int KS_, int WAVES_>
+template <int MO_, int MT_, int WAVES_>
 struct SplitShape {
-    static constexpr int MO = MO_, MT = MT_, KS = KS_, WAVES = WAVES_, kThreads = 64 * WAVES;
+    static constexpr int MO = MO_, MT = MT_, WAVES = WAVES_, kThreads = 64 * WAVES;
     static constexpr bool kSmall = MO == 16;                      // 16 x 16 x 64 instructions, otherwise 32 x 32 x 32
-    static constexpr int kPlanes = KS / 128;                      // 128 codes of all rows lie together
-    static constexpr int kLoadsW = MO / 8 * kPlanes, kLoadsX = MT / 8 * kPlanes;
+    static constexpr int kLoadsW = MO / 8, kLoadsX = MT / 8;
     static constexpr int TO = kSmall ? 1 : MO / 32, TT = kSmall ? 1 : MT / 32;
-    static constexpr int kStage = (MO + MT) * KS;
+    static constexpr int kStage = (MO + MT) * kStep;
     static constexpr int kRow = MO + 4;                           // a token's sums in LDS, with room against bank conflicts
     static constexpr int kSums = MT * kRow * 4;
     static constexpr int kWave = kStage > kSums ? kStage : kSums; // LDS of a wave
@@ -289,52 +315,48 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product_split(ProductArgs 
     char *const mine = lds + wave * S::kWave;
 
     u32x4 vw[S::kLoadsW], vx[S::kLoadsX];
+    const int at_w = (lane >> 3) * (int)a.ldw + (lane & 7) * 16, at_x = (lane >> 3) * (int)a.ldx + (lane & 7) * 16;
     auto load = [&](int k0) {
+        const bool there = k0 + (lane & 7) * 16 < a.bytes;
 #pragma unroll
-        for (int q = 0; q < S::kLoadsW; ++q)
-            vw[q] = w.load16(q / S::kPlanes * 8 + (lane >> 3), k0 + q % S::kPlanes * 128 + (lane & 7) * 16);
+        for (int q = 0; q < S::kLoadsW; ++q) vw[q] = w.load16(there, at_w + k0, q * 8);
 #pragma unroll
-        for (int q = 0; q < S::kLoadsX; ++q)
-            vx[q] = x.load16(q / S::kPlanes * 8 + (lane >> 3), k0 + q % S::kPlanes * 128 + (lane & 7) * 16);
+        for (int q = 0; q < S::kLoadsX; ++q) vx[q] = x.load16(there, at_x + k0, q * 8);
     };
     i32x16 acc[S::TO][S::TT] = {};
     i32x4 small = {};
-    load(wave * S::KS);
-    for (int k0 = wave * S::KS; k0 < a.bytes; k0 += S::WAVES * S::KS) {
+    load(wave * kStep);
+    for (int k0 = wave * kStep; k0 < a.bytes; k0 += S::WAVES * kStep) {
 #pragma unroll
         for (int q = 0; q < S::kLoadsW; ++q)
-            *reinterpret_cast<u32x4 *>(mine + q % S::kPlanes * S::MO * 128 + lds_at(q / S::kPlanes * 8 + (lane >> 3), lane & 7)) = vw[q];
+            *reinterpret_cast<u32x4 *>(mine + lds_at(q * 8 + (lane >> 3), lane & 7)) = vw[q];
 #pragma unroll
         for (int q = 0; q < S::kLoadsX; ++q)
-            *reinterpret_cast<u32x4 *>(mine + S::MO * S::KS + q % S::kPlanes * S::MT * 128 +
-                                       lds_at(q / S::kPlanes * 8 + (lane >> 3), lane & 7)) = vx[q];
+            *reinterpret_cast<u32x4 *>(mine + S::MO * kStep + lds_at(q * 8 + (lane >> 3), lane & 7)) = vx[q];
         wave_fence();
-        load(k0 + S::WAVES * S::KS);
+        load(k0 + S::WAVES * kStep);
+        const char *const pw = mine, *const px = mine + S::MO * kStep;
+        if constexpr (S::kSmall) {
 #pragma unroll
-        for (int p = 0; p < S::kPlanes; ++p) {
-            const char *const pw = mine + p * S::MO * 128, *const px = mine + S::MO * S::KS + p * S::MT * 128;
-            if constexpr (S::kSmall) {
+            for (int s = 0; s < 2; ++s) {
+                const int at = lds_at(lane & 15, 4 * s + (lane >> 4));
+                small = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(pw + at),
+                                                              *reinterpret_cast<const i32x4 *>(px + at), small, 0, 0, 0);
+            }
+        } else {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int at = lds_at(lane & 15, 4 * s + (lane >> 4));
-                    small = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(pw + at),
-                                                                  *reinterpret_cast<const i32x4 *>(px + at), small, 0, 0, 0);
-                }
-            } else {
+            for (int s = 0; s < 4; ++s) {
+                i32x4 fw[S::TO], fx[S::TT];
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    i32x4 fw[S::TO], fx[S::TT];
+                for (int m = 0; m < S::TO; ++m)
+                    fw[m] = *reinterpret_cast<const i32x4 *>(pw + lds_at(m * 32 + (lane & 31), 2 * s + (lane >> 5)));
 #pragma unroll
-                    for (int m = 0; m < S::TO; ++m)
-                        fw[m] = *reinterpret_cast<const i32x4 *>(pw + lds_at(m * 32 + (lane & 31), 2 * s + (lane >> 5)));
+                for (int n = 0; n < S::TT; ++n)
+                    fx[n] = *reinterpret_cast<const i32x4 *>(px + lds_at(n * 32 + (lane & 31), 2 * s + (lane >> 5)));
 #pragma unroll
-                    for (int n = 0; n < S::TT; ++n)
-                        fx[n] = *reinterpret_cast<const i32x4 *>(px + lds_at(n * 32 + (lane & 31), 2 * s + (lane >> 5)));
+                for (int m = 0; m < S::TO; ++m)
 #pragma unroll
-                    for (int m = 0; m < S::TO; ++m)
-#pragma unroll
-                        for (int n = 0; n < S::TT; ++n) acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[m], fx[n], acc[m][n], 0, 0, 0);
-                }
+                    for (int n = 0; n < S::TT; ++n) acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[m], fx[n], acc[m][n], 0, 0, 0);
             }
         }
         wave_fence();
@@ -384,13 +406,13 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 // along each).
 #define ZIPML_PRODUCT_SPLIT(F)                                                                                                  \
     F(0, 16, 16, 4) F(1, 16, 16, 8) F(2, 16, 16, 16) F(3, 32, 32, 4) F(4, 32, 32, 8) F(5, 32, 32, 16) F(6, 64, 32, 8) F(7, 64, 64, 8)
-#define ZIPML_PRODUCT_TILE(F) F(8, 128, 64, 2, 2) F(9, 128, 128, 2, 4) F(10, 256, 256, 2, 4)
+#define ZIPML_PRODUCT_TILE(F) F(8, 128, 64, 2, 2) F(9, 128, 128, 2, 4) F(10, 256, 256, 2, 4) 
 
 // Which shape, and (of the second kind) in how many ranges the contraction is taken, whose sums a second launch joins: the least of
 //   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
 //   them: k * shared) + (ranges > 1: a launch, sums written and read).
 // The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
-// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 2 % slower than the fastest on average, 26 % at most.
+// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 29 % at most.
 struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
@@ -399,12 +421,12 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
 {
     struct Cost { int outs, tokens, waves; double start, turn, lone, shared; };
     static const Cost costs[] = {
-        {16, 16, 4, 2.70, 0.00, 0.28, 0.25}, {16, 16, 8, 2.64, 0.00, 0.47, 0.51},
-        {16, 16, 16, 2.39, 0.00, 0.89, 1.12}, {32, 32, 4, 2.74, 0.04, 0.57, 0.51},
-        {32, 32, 8, 2.66, 0.12, 0.93, 1.05}, {32, 32, 16, 1.84, 0.00, 1.90, 2.36},
-        {64, 32, 8, 2.71, 2.24, 1.44, 1.37}, {64, 64, 8, 3.11, 3.03, 1.98, 2.00},
-        {128, 64, 1, 4.30, 1.36, 0.45, 0.42}, {128, 128, 1, 4.49, 2.73, 0.57, 0.60},
-        {256, 256, 1, 10.10, 8.00, 1.27, 1.73},
+        {16, 16, 4, 2.19, 0.00, 0.28, 0.25}, {16, 16, 8, 2.15, 0.00, 0.47, 0.50},
+        {16, 16, 16, 1.88, 0.00, 0.90, 1.12}, {32, 32, 4, 2.24, 0.06, 0.56, 0.51},
+        {32, 32, 8, 2.15, 0.13, 0.95, 1.03}, {32, 32, 16, 1.22, 0.00, 2.09, 2.41},
+        {64, 32, 8, 2.18, 2.36, 1.51, 1.38}, {64, 64, 8, 3.06, 2.93, 1.98, 2.06},
+        {128, 64, 1, 3.80, 1.39, 0.51, 0.43}, {128, 128, 1, 4.36, 2.70, 0.59, 0.61},
+        {256, 256, 1, 9.68, 8.00, 1.30, 1.78},
     };
     const int64_t bytes = round_up(d_in, kRow8Unit), sums = rows * round_up(d_out, 4) * 4;
     ProductPlan best{-1, 1, 0, 0};
@@ -422,7 +444,7 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
             const double k = (double)((tiles * ranges + 255) / 256), step = (double)kStep * c.waves;
             const double rounds = (double)(int64_t)(((double)(range < bytes ? range : bytes) + step - 1) / step);
             const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && k * c.shared > c.lone ? k * c.shared : c.lone) +
-                              (ranges > 1 ? 2.2 + (double)(ranges * sums) * 2 / 6.3e6 : 0.0);
+                              (ranges > 1 ? 2.1 + (double)(ranges * sums) * 2 / 5.8e6 : 0.0);
             if (best.shape < 0 || us < least) {
                 least = us;
                 best = ProductPlan{shape, (int)ranges, (int)range, ranges > 1 ? (size_t)(ranges * sums) : 0};
@@ -433,15 +455,15 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
 }
 
 template <typename S, typename K>
-static int launch_tiles(hipStream_t s, ProductArgs a, K k, int ranges)
+static int launch_tiles(hipStream_t s, ProductArgs a, K k, int64_t most = 1ll << 30)
 {
     a.tiles_o = (a.d_out + S::MO - 1) / S::MO;
-    const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * ranges;
+    const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * a.ranges;
     if (all > 0x3FFFFFFF) return ZIPML_EINVAL;
     a.tiles_t = (int)tiles;
     static std::atomic<uint64_t> done;
     if (allow_lds((const void *)k, S::kLds, done)) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3((uint32_t)all), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL(k, dim3((uint32_t)(all < most ? all : most)), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
 
@@ -449,15 +471,17 @@ template <typename T>
 static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, void *workspace)
 {
     a.range = p.range;
+    a.ranges = p.ranges;
     a.part = 0;
     if (p.ranges > 1) {
         ProductArgs parts = a;
+        parts.through = 0;
         parts.y = workspace;
         parts.ldy = round_up(a.d_out, 4);
         a.part = parts.part = a.rows * parts.ldy;
         int rc = ZIPML_EINVAL;
         switch (p.shape) {
-#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<S>(s, parts, k_row8_product<int, S>, p.ranges); break; }
+#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<S>(s, parts, k_row8_product<int, S>); break; }
             ZIPML_PRODUCT_TILE(TILE)
 #undef TILE
         }
@@ -467,8 +491,8 @@ static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, vo
         return hip_check(hipGetLastError());
     }
     switch (p.shape) {
-#define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, kStep, waves> S; return launch_tiles<S>(s, a, k_row8_product_split<T, S>, 1); }
-#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<S>(s, a, k_row8_product<T, S>, 1); }
+#define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, waves> S; return launch_tiles<S>(s, a, k_row8_product_split<T, S>); }
+#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<S>(s, a, k_row8_product<T, S>); }
         ZIPML_PRODUCT_SPLIT(SPLIT)
         ZIPML_PRODUCT_TILE(TILE)
 #undef SPLIT
@@ -511,7 +535,8 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
         !aligned4(w_scales_dev) || !aligned4(bias_dev))
         return ZIPML_EALIGN;
     ProductArgs a{(const uint8_t *)x_dev, (const uint8_t *)w_dev, x_scales_dev, w_scales_dev, bias_dev, y_dev, ldx, ldw, ldy, rows,
-                  (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0, 0, 0};
+                  (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0, 0, 0,
+                  rows * d_out * (int64_t)dtype_bytes(dtype) > kThroughLeast, 0};
     hipStream_t s = entry_stream(stream);
     return dtype == ZIPML_F32 ? launch_product<float>(s, a, p, workspace_dev) : launch_product<__bf16>(s, a, p, workspace_dev);
 }
