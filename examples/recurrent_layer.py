@@ -41,7 +41,8 @@ class RecurrentLayer:
         self.dw_in, self.dw_out = torch.empty_like(self.w_in), torch.empty_like(self.w_out)
         self.ws = new(max(zipml.scan_workspace_bytes(tokens, channels),
                           zipml.act_wgrad_workspace_bytes(tokens, 2 * channels, d_in, BF16),
-                          zipml.act_wgrad_workspace_bytes(tokens, d_out, channels, BF16)), dtype=torch.uint8)
+                          zipml.act_wgrad_workspace_bytes(tokens, d_out, channels, BF16), zipml.clip_workspace_bytes(2)), dtype=torch.uint8)
+        self.norm = new(2, dtype=torch.float32)
         self.copy_weights()
 
     def copy_weights(self):
@@ -74,7 +75,10 @@ class RecurrentLayer:
         zipml.act_wgrad(self.dxz, 2 * c, self.act_u, t, 2 * c, self.d_in, self.dw_in, self.d_in, self.ws)
         return self.dxz @ self.b_in
 
-    def sgd(self, lr):
+    def sgd(self, lr, max_norm=None):
+        """One step, with max_norm along the gradients scaled down to that norm."""
+        if max_norm is not None:
+            zipml.clip(zipml.ClipList([self.dw_in, self.dw_out]), max_norm, self.norm, self.ws)
         self.w_in -= lr * self.dw_in
         self.w_out -= lr * self.dw_out
         self.copy_weights()
@@ -86,6 +90,32 @@ class RecurrentLayer:
         xz, y = u @ self.b_in.t(), torch.empty(u.shape[0], c, dtype=BF16, device=DEV)
         zipml.scan_step(xz[:, :c], 2 * c, xz[:, c:], 2 * c, rows, c, pool, pool.shape[0], y, c, slots=slots)
         return y @ self.b_out.t()
+
+    def encode_weights(self):
+        """Lays the weights out for decode8: codes with a scale for each output."""
+        self.codes = []
+        for w in (self.w_in, self.w_out):
+            q = torch.empty(w.shape[0], -(-w.shape[1] // 16) * 16, dtype=torch.int8, device=DEV)
+            scales = torch.empty(w.shape[0], device=DEV)
+            zipml.row8_encode(w, w.shape[0], w.shape[1], w.shape[1], q, q.stride(0), scales)
+            self.codes.append((q, scales))
+
+    def product8(self, x, weights):
+        """x (bf16 rows) times weights in codes: x becomes codes row by row."""
+        (w, w_scales), (rows, d_in) = weights, x.shape
+        q = torch.empty(rows, w.stride(0), dtype=torch.int8, device=DEV)
+        scales, y = torch.empty(rows, device=DEV), torch.empty(rows, w.shape[0], dtype=BF16, device=DEV)
+        zipml.row8_encode(x, rows, d_in, x.stride(0), q, q.stride(0), scales)
+        room = torch.empty(zipml.row8_product_workspace_bytes(rows, w.shape[0], d_in), dtype=torch.uint8, device=DEV)
+        zipml.row8_product(q, q.stride(0), scales, w, w.stride(0), w_scales, rows, w.shape[0], d_in, y, w.shape[0], room)
+        return y
+
+    def decode8(self, u, pool, slots):
+        """decode with weights and activations in 8 bits (after encode_weights): half the bytes a token."""
+        rows, c = u.shape[0], self.c
+        xz, y = self.product8(u, self.codes[0]), torch.empty(rows, c, dtype=BF16, device=DEV)
+        zipml.scan_step(xz[:, :c], 2 * c, xz[:, c:], 2 * c, rows, c, pool, pool.shape[0], y, c, slots=slots)
+        return self.product8(y, self.codes[1])
 
 
 def documents(tokens, n_seq, seed):

@@ -467,37 +467,64 @@ def scan_step(x, ldx, z, ldz, rows, channels, h, n_slots, y, ldy, *, slots=None,
                                  _array(w, "h", h, "float32"), n_slots, _array(w, "slots", slots, "int32"), y.data_ptr(), ldy), w)
 
 
-def _codes(where, name, t):
-    """The address of rows of codes, which lie a leading dimension of the caller's apart."""
-    if t is None:
-        return None
-    if t.dtype is not _KINDS["int8"] or not (t.is_contiguous() or t.shape[-1:] == _ONE or t.stride()[-1:] == _ONE):
-        raise ZipmlError(EINVAL, f"{where}: {name} has to be int8 rows of codes side by side, not {t.dtype} with strides {t.stride()}")
-    return t.data_ptr()
+_device = None
 
 
-def _row(where, name, t, kind):
-    """The address of rows of type `kind`; None if there are none."""
+def _here() -> int:
+    """The current device's number, on which the tensors of a call have to be: a kernel may not reach another's memory."""
+    global _device
+    if _device is None:
+        import torch
+        torch.cuda.current_device()                        # raises where there is no GPU
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
+
+
+def _row(where, name, t, kind, device):
+    """The address of rows of type `kind` whose values lie side by side and that lie a leading dimension of the caller's apart; None if
+    there are none."""
     if t is None:
         return None
     if t.dtype is not kind or not (t.is_contiguous() or t.shape[-1:] == _ONE or t.stride()[-1:] == _ONE):
-        raise ZipmlError(EINVAL, f"{where}: {name} has to be rows of {kind} side by side as the others, not {t.dtype} with strides "
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be rows of {kind} with their values side by side, not {t.dtype} with strides "
                                  f"{t.stride()}")
+    if t.get_device() != device:
+        raise ZipmlError(EINVAL, f"{where}: {name} is on {t.device}, the current device is {device}")
     return t.data_ptr()
+
+
+def _floats(where, name, t, device):
+    """The address of a contiguous fp32 array; None if there is none."""
+    if t is None:
+        return None
+    if t.dtype is not _KINDS["float32"] or not t.is_contiguous():
+        raise ZipmlError(EINVAL, f"{where}: {name} has to be contiguous float32, not {t.dtype} with strides {t.stride()}")
+    if t.get_device() != device:
+        raise ZipmlError(EINVAL, f"{where}: {name} is on {t.device}, the current device is {device}")
+    return t.data_ptr()
+
+
+def _room(where, workspace, device):
+    """Address and size of a workspace; none of them where there is none."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        raise ZipmlError(EINVAL, f"{where}: the workspace is on {workspace.device}, the current device is {device}")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def row8_encode(x, rows, cols, ldx, codes, ldc, scales, *, rounding=NEAREST, seed=0, epoch=0, tag=0, stream=None):
     """Rows of x (fp32 or bf16) as 8-bit codes (int8, rows ldc bytes apart) with a scale each (fp32)."""
-    w = "zipml_row8_encode"
-    _check(lib().zipml_row8_encode(_stream(stream), _ptr(x), _rows(w, x), rows, cols, ldx, rounding, seed, epoch, tag,
-                                   _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32")), w)
+    w, d, k = "zipml_row8_encode", _here(), x.dtype
+    _check(lib().zipml_row8_encode(_stream(stream), _row(w, "x", x, k, d), _CODES[k], rows, cols, ldx, rounding, seed, epoch, tag,
+                                   _row(w, "codes", codes, _KINDS["int8"], d), ldc, _floats(w, "scales", scales, d)), w)
 
 
 def row8_decode(codes, ldc, scales, rows, cols, out, ldo, stream=None):
     """The values that rows of codes stand for, in out (fp32 or bf16)."""
-    w = "zipml_row8_decode"
-    _check(lib().zipml_row8_decode(_stream(stream), _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32"), rows,
-                                   cols, _ptr(out), _rows(w, out), ldo), w)
+    w, d, k = "zipml_row8_decode", _here(), out.dtype
+    _check(lib().zipml_row8_decode(_stream(stream), _row(w, "codes", codes, _KINDS["int8"], d), ldc, _floats(w, "scales", scales, d),
+                                   rows, cols, _row(w, "out", out, k, d), _CODES[k], ldo), w)
 
 
 def row8_product_workspace_bytes(rows: int, d_out: int, d_in: int) -> int:
@@ -506,23 +533,22 @@ def row8_product_workspace_bytes(rows: int, d_out: int, d_in: int) -> int:
 
 def row8_product(x, ldx, x_scales, w, ldw, w_scales, rows, d_out, d_in, y, ldy, workspace, *, bias=None, stream=None):
     """y (fp32 or bf16) = x w^T from codes of tokens and of weights, with their scales (fp32) and a bias (fp32)."""
-    f = "zipml_row8_product"
-    _check(lib().zipml_row8_product(_stream(stream), _codes(f, "x", x), ldx, _array(f, "x_scales", x_scales, "float32"),
-                                    _codes(f, "w", w), ldw, _array(f, "w_scales", w_scales, "float32"),
-                                    _array(f, "bias", bias, "float32"), rows, d_out, d_in, _ptr(y), _rows(f, y), ldy,
-                                    workspace.data_ptr(), workspace.nbytes), f)
+    f, d, k, codes = "zipml_row8_product", _here(), y.dtype, _KINDS["int8"]
+    room, size = _room(f, workspace, d)
+    _check(lib().zipml_row8_product(_stream(stream), _row(f, "x", x, codes, d), ldx, _floats(f, "x_scales", x_scales, d),
+                                    _row(f, "w", w, codes, d), ldw, _floats(f, "w_scales", w_scales, d), _floats(f, "bias", bias, d),
+                                    rows, d_out, d_in, _row(f, "y", y, k, d), _CODES[k], ldy, room, size), f)
 
 
 def norm_forward(x, ldx, rows, cols, eps, *, gain=None, add=None, ldadd=0, sum=None, ldsum=0, y=None, ldy=0, codes=None, ldc=0,
                  scales=None, rstd=None, stream=None):
     """Root-mean-square norm of x + add: its result in y (x's type) or in codes with scales; sum gets x + add, rstd (fp32) what
     the backward pass needs.  gain, scales, rstd: fp32."""
-    w = "zipml_norm_forward"
-    k = x.dtype
-    _check(lib().zipml_norm_forward(_stream(stream), _row(w, "x", x, k), ldx, _row(w, "add", add, k), ldadd, _CODES[k], rows, cols,
-                                    _array(w, "gain", gain, "float32"), eps, _row(w, "sum", sum, k), ldsum, _row(w, "y", y, k), ldy,
-                                    _codes(w, "codes", codes), ldc, _array(w, "scales", scales, "float32"),
-                                    _array(w, "rstd", rstd, "float32")), w)
+    w, d, k = "zipml_norm_forward", _here(), x.dtype
+    _check(lib().zipml_norm_forward(_stream(stream), _row(w, "x", x, k, d), ldx, _row(w, "add", add, k, d), ldadd, _CODES[k], rows,
+                                    cols, _floats(w, "gain", gain, d), eps, _row(w, "sum", sum, k, d), ldsum, _row(w, "y", y, k, d),
+                                    ldy, _row(w, "codes", codes, _KINDS["int8"], d), ldc, _floats(w, "scales", scales, d),
+                                    _floats(w, "rstd", rstd, d)), w)
 
 
 def norm_backward_workspace_bytes(rows: int, cols: int) -> int:
@@ -533,12 +559,11 @@ def norm_backward(dy, lddy, sum, ldsum, rows, cols, rstd, dx, lddx, workspace=No
                   flags=0, stream=None):
     """Gradients dx and dgain of norm_forward from the sum and rstd that it kept; dsum: the gradient that reaches the sum by the
     residual stream; flags: NORM_ADD adds to dgain.  The workspace is needed for dgain only."""
-    w = "zipml_norm_backward"
-    k = dy.dtype
-    _check(lib().zipml_norm_backward(_stream(stream), _row(w, "dy", dy, k), lddy, _row(w, "sum", sum, k), ldsum, _CODES[k], rows, cols,
-                                     _array(w, "gain", gain, "float32"), _array(w, "rstd", rstd, "float32"), _row(w, "dsum", dsum, k),
-                                     lddsum, _row(w, "dx", dx, k), lddx, _array(w, "dgain", dgain, "float32"), flags, _ptr(workspace),
-                                     0 if workspace is None else workspace.nbytes), w)
+    w, d, k = "zipml_norm_backward", _here(), dy.dtype
+    room, size = _room(w, workspace, d)
+    _check(lib().zipml_norm_backward(_stream(stream), _row(w, "dy", dy, k, d), lddy, _row(w, "sum", sum, k, d), ldsum, _CODES[k], rows,
+                                     cols, _floats(w, "gain", gain, d), _floats(w, "rstd", rstd, d), _row(w, "dsum", dsum, k, d),
+                                     lddsum, _row(w, "dx", dx, k, d), lddx, _floats(w, "dgain", dgain, d), flags, room, size), w)
 
 
 class _ClipTensor(C.Structure):
@@ -556,12 +581,15 @@ class ClipList:
         w = "ClipList"
         if len(self.outs) != len(self.grads) or not self.grads:
             raise ZipmlError(EINVAL, f"{w}: {len(self.grads)} gradients and {len(self.outs)} outputs")
+        self.device = self.grads[0].get_device()
         spans = []
         self.table = (_ClipTensor * len(self.grads))()
         for k, (g, o) in enumerate(zip(self.grads, self.outs)):
             for name, t in (("gradient", g), ("output", o)):
                 if t is not None and (not t.is_contiguous() or _dtype(t) < 0):
                     raise ZipmlError(EINVAL, f"{w}: {name} {k} has to be contiguous fp32 or bf16, not {t.dtype} with strides {t.stride()}")
+                if t is not None and t.get_device() != self.device:
+                    raise ZipmlError(EINVAL, f"{w}: {name} {k} is on {t.device}, not where the first gradient is")
             if o is not None and o.numel() != g.numel():
                 raise ZipmlError(EINVAL, f"{w}: output {k} has {o.numel()} values, its gradient {g.numel()}")
             same = o is not None and o.data_ptr() == g.data_ptr() and o.dtype is g.dtype
@@ -583,8 +611,10 @@ def clip_workspace_bytes(n_tensors: int) -> int:
 
 def clip(tensors, max_norm, norm, workspace, stream=None):
     """Global norm over a ClipList's gradients, which are scaled down to max_norm; norm: fp32 [2], gets the norm and the factor."""
-    w = "zipml_clip"
+    w, d = "zipml_clip", _here()
+    if tensors.device != d:
+        raise ZipmlError(EINVAL, f"{w}: the gradients are on device {tensors.device}, the current device is {d}")
     if norm is not None and norm.numel() < 2:
         raise ZipmlError(EINVAL, f"{w}: norm has to hold two values")
-    _check(lib().zipml_clip(_stream(stream), tensors.table, len(tensors.table), max_norm, _array(w, "norm", norm, "float32"),
-                            workspace.data_ptr(), workspace.nbytes), w)
+    room, size = _room(w, workspace, d)
+    _check(lib().zipml_clip(_stream(stream), tensors.table, len(tensors.table), max_norm, _floats(w, "norm", norm, d), room, size), w)

@@ -118,14 +118,23 @@ def test_rows_far_apart(rows, d_out):
 
 
 @pytest.mark.gpu
-def test_part_of_the_rows():
-    """Codes and scales from any row on (scales are aligned to their type only)."""
-    (x, sx), (w, sw) = codes(20, 300, 1), codes(50, 300, 2)
-    xd, wd, sxd, swd = on_gpu(x), on_gpu(w), torch.from_numpy(sx).to(DEV), torch.from_numpy(sw).to(DEV)
-    y = torch.empty(3, 9, device=DEV)
-    ws = torch.empty(zipml.row8_product_workspace_bytes(3, 9, 300), dtype=torch.uint8, device=DEV)
-    zipml.row8_product(xd[17:], 304, sxd[17:], wd[41:], 304, swd[41:], 3, 9, 300, y, 9, ws)
-    np.testing.assert_array_equal(y.cpu().numpy(), ref.product(x[17:], w[41:], sx[17:], sw[41:], None, torch.float32).numpy())
+@pytest.mark.parametrize("rows,d_out", [(3, 9), (700, 520), (2000, 2049)])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_part_of_the_rows(rows, d_out, kind):
+    """Codes and scales from any row on (scales and bias are aligned to their type only)."""
+    (x, sx), (w, sw) = codes(rows + 17, 300, 1), codes(d_out + 41, 300, 2)
+    b = np.random.default_rng(3).standard_normal(d_out + 3).astype(np.float32)
+    xd, wd, sxd, swd, bd = on_gpu(x), on_gpu(w), *(torch.from_numpy(v).to(DEV) for v in (sx, sw, b))
+    y = torch.empty(rows, d_out, dtype=TYPES[kind], device=DEV)
+    ws = torch.empty(zipml.row8_product_workspace_bytes(rows, d_out, 300), dtype=torch.uint8, device=DEV)
+    zipml.row8_product(xd[17:], 304, sxd[17:], wd[41:], 304, swd[41:], rows, d_out, 300, y, d_out, ws, bias=bd[3:])
+    assert torch.equal(y.cpu(), ref.product(x[17:], w[41:], sx[17:], sw[41:], b[3:], TYPES[kind]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,d_out,d_in,kind", [(8300, 6107, 40, "bf16"), (5000, 5121, 130, "f32"), (4096, 12290, 16, "bf16")])
+def test_results_larger_than_the_caches(rows, d_out, d_in, kind):
+    same(rows, d_out, d_in, kind, True)
 
 
 @pytest.mark.gpu
