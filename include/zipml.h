@@ -375,8 +375,8 @@ int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, const void *z_
  * Rows (of tokens, or of a weight matrix, one for each output) as 8-bit codes with one scale a row, what makes such rows (an
  * encoder, the norm in front of a layer), the product of two sets of them, and the norm's backward pass; and the norm of all
  * gradients of a step.  All calls are asynchronous and may be captured in a graph.  Workspaces as above: no preparation, shared by
- * calls that follow one another on a stream.  Scales and other vectors of one value a row need be aligned to their type only, so
- * that calls may take part of the rows.
+ * calls that follow one another on a stream.  Vectors (scales, gain, bias, rstd, dgain) need be aligned to their type only, so that
+ * calls may take part of the rows, and parameters lie side by side.  Outputs must not overlap inputs except where it is said.
  *
  * Form of the codes (public): int8, rows ldc bytes apart, a multiple of 16 and at least cols; the bytes of a row from cols up to the
  * next multiple of 16 are zeros (encoders write them).  value = code * scale of the row, fp32.

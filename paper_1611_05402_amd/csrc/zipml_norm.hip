@@ -314,6 +314,12 @@ using namespace zipml;
 
 static bool norm_rows_ok(const void *p, int64_t ld, int64_t rows, int64_t cols) { return !p || (ld >= cols && ld <= (1ll << 60) / rows); }
 
+// An output may stand in an input's place row by row, not at another pitch.
+static bool in_place_ok(const void *out, int64_t ldo, const void *in, int64_t ldi, int64_t rows)
+{
+    return out != in || !out || ldo == ldi || rows == 1;
+}
+
 extern "C" int zipml_norm_forward(void *stream, const void *x_dev, int64_t ldx, const void *add_dev, int64_t ldadd, int dtype,
                                   int64_t rows, int64_t cols, const float *gain_dev, float eps, void *sum_dev, int64_t ldsum,
                                   void *y_dev, int64_t ldy, void *codes_dev, int64_t ldc, float *scales_dev, float *rstd_dev)
@@ -322,8 +328,11 @@ extern "C" int zipml_norm_forward(void *stream, const void *x_dev, int64_t ldx, 
     if (!norm_rows_ok(x_dev, ldx, rows, cols) || !norm_rows_ok(add_dev, ldadd, rows, cols) ||
         !norm_rows_ok(sum_dev, ldsum, rows, cols) || !norm_rows_ok(y_dev, ldy, rows, cols))
         return ZIPML_EINVAL;
+    if (!in_place_ok(sum_dev, ldsum, x_dev, ldx, rows) || !in_place_ok(sum_dev, ldsum, add_dev, ldadd, rows) ||
+        !in_place_ok(y_dev, ldy, x_dev, ldx, rows) || !in_place_ok(y_dev, ldy, add_dev, ldadd, rows) || (y_dev && y_dev == sum_dev))
+        return ZIPML_EINVAL;
     if ((!y_dev && !codes_dev) || !codes_dev != !scales_dev || (codes_dev && !row8_pitch_ok(rows, cols, ldc))) return ZIPML_EINVAL;
-    if (!aligned16(x_dev) || !aligned16(add_dev) || !aligned16(gain_dev) || !aligned16(sum_dev) || !aligned16(y_dev) ||
+    if (!aligned16(x_dev) || !aligned16(add_dev) || !aligned4(gain_dev) || !aligned16(sum_dev) || !aligned16(y_dev) ||
         !aligned16(codes_dev) || !aligned4(scales_dev) || !aligned4(rstd_dev))
         return ZIPML_EALIGN;
     const NormArgs a{x_dev, add_dev, gain_dev, sum_dev, y_dev, (uint8_t *)codes_dev, scales_dev, rstd_dev, ldx, ldadd, ldsum, ldy,
@@ -354,10 +363,13 @@ extern "C" int zipml_norm_backward(void *stream, const void *dy_dev, int64_t ldd
     if (!norm_rows_ok(dy_dev, lddy, rows, cols) || !norm_rows_ok(sum_dev, ldsum, rows, cols) ||
         !norm_rows_ok(dsum_dev, lddsum, rows, cols) || !norm_rows_ok(dx_dev, lddx, rows, cols))
         return ZIPML_EINVAL;
+    if (!in_place_ok(dx_dev, lddx, dy_dev, lddy, rows) || !in_place_ok(dx_dev, lddx, sum_dev, ldsum, rows) ||
+        !in_place_ok(dx_dev, lddx, dsum_dev, lddsum, rows))
+        return ZIPML_EINVAL;
     if ((flags & ~ZIPML_NORM_ADD) || ((flags & ZIPML_NORM_ADD) && !dgain_dev)) return ZIPML_EINVAL;
     if (dgain_dev && (!workspace_dev || workspace_bytes < zipml_norm_backward_workspace_bytes(rows, cols))) return ZIPML_EWORKSPACE;
-    if (!aligned16(dy_dev) || !aligned16(sum_dev) || !aligned16(gain_dev) || !aligned16(dsum_dev) || !aligned16(dx_dev) ||
-        !aligned16(dgain_dev) || !aligned4(rstd_dev) || (dgain_dev && !aligned16(workspace_dev)))
+    if (!aligned16(dy_dev) || !aligned16(sum_dev) || !aligned4(gain_dev) || !aligned16(dsum_dev) || !aligned16(dx_dev) ||
+        !aligned4(dgain_dev) || !aligned4(rstd_dev) || (dgain_dev && !aligned16(workspace_dev)))
         return ZIPML_EALIGN;
     NormGradArgs a{dy_dev, sum_dev, dsum_dev, gain_dev, rstd_dev, dx_dev, dgain_dev ? (float *)workspace_dev : nullptr, lddy, ldsum,
                    lddsum, lddx, rows, cols, round_up(cols, kRow8Unit) / 8, round_up(cols, kRow8Unit)};

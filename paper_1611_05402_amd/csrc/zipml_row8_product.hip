@@ -454,16 +454,16 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
     return best;
 }
 
-template <typename S, typename K>
-static int launch_tiles(hipStream_t s, ProductArgs a, K k, int64_t most = 1ll << 30)
+// (T tells kernels of one shape apart: each is asked for its LDS once)
+template <typename T, typename S, typename K>
+static int launch_tiles(hipStream_t s, ProductArgs a, K k)
 {
     a.tiles_o = (a.d_out + S::MO - 1) / S::MO;
     const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * a.ranges;
-    if (all > 0x3FFFFFFF) return ZIPML_EINVAL;
     a.tiles_t = (int)tiles;
     static std::atomic<uint64_t> done;
     if (allow_lds((const void *)k, S::kLds, done)) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3((uint32_t)(all < most ? all : most)), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL(k, dim3((uint32_t)all), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
 
@@ -481,7 +481,7 @@ static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, vo
         a.part = parts.part = a.rows * parts.ldy;
         int rc = ZIPML_EINVAL;
         switch (p.shape) {
-#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<S>(s, parts, k_row8_product<int, S>); break; }
+#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<int, S>(s, parts, k_row8_product<int, S>); break; }
             ZIPML_PRODUCT_TILE(TILE)
 #undef TILE
         }
@@ -491,8 +491,8 @@ static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, vo
         return hip_check(hipGetLastError());
     }
     switch (p.shape) {
-#define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, waves> S; return launch_tiles<S>(s, a, k_row8_product_split<T, S>); }
-#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<S>(s, a, k_row8_product<T, S>); }
+#define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, waves> S; return launch_tiles<T, S>(s, a, k_row8_product_split<T, S>); }
+#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<T, S>(s, a, k_row8_product<T, S>); }
         ZIPML_PRODUCT_SPLIT(SPLIT)
         ZIPML_PRODUCT_TILE(TILE)
 #undef SPLIT
