@@ -100,25 +100,28 @@ __device__ __forceinline__ void tile_of(const ProductArgs &a, uint32_t n, uint32
 }
 
 // ---- many tokens: tiles whose waves share the rows ----------------------------------------------
-// MO x MT outputs x tokens of a workgroup, WO x WT waves.
+// MO x MT outputs x tokens of a workgroup, WO x WT waves.  16 x 16 x 64 instructions: what bounds large products is the power that the
+// matrix cores draw, and on random codes these do 3,985 TOP/s by themselves where 32 x 32 x 32 ones do 3,310 (on zeros 4,710 and 4,785).
 template <typename T, int MO_, int MT_, int WO_, int WT_>
 struct ProductShape {
     static constexpr int MO = MO_, MT = MT_, WO = WO_, WT = WT_, kThreads = 64 * WO * WT;
-    static constexpr int TO = MO / WO / 32, TT = MT / WT / 32;
+    static constexpr int TO = MO / WO / 16, TT = MT / WT / 16;      // 16 x 16 tiles of a wave
     static constexpr int kLoadsW = MO * kStep / 16 / kThreads, kLoadsX = MT * kStep / 16 / kThreads, kLoads = kLoadsW + kLoadsX;
     static constexpr int kStage = (MO + MT) * kStep;
+    static constexpr int kBeats = kStep / 64 * TO;                  // of a round: 64 codes of 16 outputs, times all tokens
     static constexpr bool kParts = std::is_same<T, int>::value;     // sums of a range of the contraction, not results
-    static constexpr int HO = 4 / (int)sizeof(T);                   // 32 x 32 tiles side by side in a line of 128 bytes of results
+    static constexpr int HO = 8 / (int)sizeof(T);                   // tiles side by side in a line of 128 bytes of results
     static constexpr int kOut = 32 * 128;                           // LDS of a wave's results on their way out: 32 tokens
     static constexpr int kLds = 2 * kStage > kOut * WO * WT ? 2 * kStage : kOut * WO * WT;
-    static_assert(kLoadsW * 16 * kThreads == MO * kStep && kLoadsX * 16 * kThreads == MT * kStep && TO % HO == 0, "whole loads");
+    static_assert(kLoadsW * 16 * kThreads == MO * kStep && kLoadsX * 16 * kThreads == MT * kStep, "whole loads");
+    static_assert(TO % HO == 0 && TT % 2 == 0 && kBeats % 4 == 0 && kLoads <= kBeats - 2, "beats");
     static_assert(kLds <= 160 * 1024, "LDS");
 };
 
 // What a wave has summed, on its way out.  A lane holds four neighbouring outputs of one token at a time.  Through LDS of its own (`out`), a
 // wave turns 32 tokens' lines of 128 bytes around and writes them 16 bytes a lane.
 template <typename T, typename S>
-__device__ __forceinline__ void write_out(const ProductArgs &a, const i32x16 (&acc)[S::TO][S::TT], char *out, int o_wave, int64_t t_wave,
+__device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&acc)[S::TO][S::TT], char *out, int o_wave, int64_t t_wave,
                                           uint32_t split)
 {
     const int lane = threadIdx.x & 63;
@@ -127,55 +130,47 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x16 (&a
     float sx[S::TT];
 #pragma unroll
     for (int n = 0; n < S::TT && !S::kParts; ++n) {
-        const int64_t t = t_wave + n * 32 + (lane & 31);
+        const int64_t t = t_wave + n * 16 + (lane & 15);
         sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
     }
 #pragma unroll
     for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
         constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
-        const int o = o_wave + m0 * 32 + (lane & 7) * V, left = a.d_out - o;
+        const int o = o_wave + m0 * 16 + (lane & 7) * V, left = a.d_out - o, at = (o_wave + m0 * 16 + 4 * (lane >> 4)) * 4;
         // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256; -0 leaves every value as it is)
-        f32x4 sw[S::HO][4], bias[S::HO][4];
+        f32x4 sw[S::HO], bias[S::HO];
 #pragma unroll
-        for (int m = 0; m < S::HO && !S::kParts; ++m)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int at = (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4;
-                sw[m][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at, 0, 0));
-                bias[m][q] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
-            }
+        for (int m = 0; m < S::HO && !S::kParts; ++m) {
+            sw[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at + m * 64, 0, 0));
+            bias[m] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
+        }
         if (a.bias)
 #pragma unroll
             for (int m = 0; m < S::HO && !S::kParts; ++m)
+                bias[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at + m * 64, 0, 0));
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    bias[m][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                               biases, (o_wave + (m0 + m) * 32 + 8 * q + 4 * (lane >> 5)) * 4, 0, 0));
+        for (int n0 = 0; n0 < S::TT; n0 += 2) {
 #pragma unroll
-        for (int n = 0; n < S::TT; ++n) {
-            const int t32 = lane & 31;
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int m = 0; m < S::HO; ++m)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int m = 0; m < S::HO; ++m) {
                     typedef T T4 __attribute__((ext_vector_type(4)));
                     T4 r;
-                    if constexpr (S::kParts) {
-                        r = T4{acc[m0 + m][n][4 * q], acc[m0 + m][n][4 * q + 1], acc[m0 + m][n][4 * q + 2], acc[m0 + m][n][4 * q + 3]};
-                    } else {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            r[k] = (T)((float)acc[m0 + m][n][4 * q + k] * sx[n] * sw[m][q][k] + bias[m][q][k]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int sum = acc[m0 + m][n0 + n][k];
+                        if constexpr (S::kParts) r[k] = sum;
+                        else r[k] = (T)((float)sum * sx[n0 + n] * sw[m][k] + bias[m][k]);
                     }
-                    const int byte = (m * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
-                    *reinterpret_cast<T4 *>(out + t32 * 128 + (((byte >> 4) ^ (t32 >> 1 & 7)) << 4) + (byte & 15)) = r;
+                    const int row = n * 16 + (lane & 15), byte = (m * 16 + 4 * (lane >> 4)) * (int)sizeof(T);
+                    *reinterpret_cast<T4 *>(out + lds_at(row, byte >> 4) + (byte & 15)) = r;
                 }
             wave_fence();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 8 * i + (lane >> 3);
                 const u32x4 line = *reinterpret_cast<const u32x4 *>(out + lds_at(r, lane & 7));
-                const int64_t t = t_wave + n * 32 + r;
+                const int64_t t = t_wave + n0 * 16 + r;
                 if (t >= a.rows) continue;
                 T *const y = (T *)a.y + split * a.part + t * a.ldy + o;
                 if (left >= V) {
@@ -210,78 +205,73 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
     const int64_t t0 = (int64_t)tile_t * S::MT;
     const CodeRows w(a.w + o0 * a.ldw, a.d_out - o0, a.ldw, a.bytes), x(a.x + t0 * a.ldx, a.rows - t0, a.ldx, a.bytes);
 
-    // The loads and the stores of a round are dealt over its steps but the last.
-    constexpr int kSteps = kStep / 32, kDeals = kSteps - 1;
-    u32x4 v[S::kLoads];
     constexpr int kRowsLoad = S::kThreads / 8;                      // rows that one load of all threads takes
     const int at_w = (tid >> 3) * (int)a.ldw + (tid & 7) * 16, at_x = (tid >> 3) * (int)a.ldx + (tid & 7) * 16;
-    auto load = [&](u32x4 (&to)[S::kLoads], int k0, int deal) {
+    auto load = [&](int k0, int q) {
         const bool there = k0 + (tid & 7) * 16 < a.bytes;
-#pragma unroll
-        for (int q = 0; q < S::kLoads; ++q) {
-            if (q * kDeals / S::kLoads != deal) continue;
-            to[q] = q < S::kLoadsW ? w.load16(there, at_w + k0, q * kRowsLoad) : x.load16(there, at_x + k0, (q - S::kLoadsW) * kRowsLoad);
-        }
+        return q < S::kLoadsW ? w.load16(there, at_w + k0, q * kRowsLoad) : x.load16(there, at_x + k0, (q - S::kLoadsW) * kRowsLoad);
     };
-    auto store = [&](const u32x4 (&from)[S::kLoads], char *stage, int deal) {
-#pragma unroll
-        for (int q = 0; q < S::kLoads; ++q) {
-            if (q * kDeals / S::kLoads != deal) continue;
-            const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
-            *reinterpret_cast<u32x4 *>(stage + (q < S::kLoadsW ? 0 : S::MO * kStep) + lds_at(c >> 3, c & 7)) = from[q];
-        }
+    auto store = [&](u32x4 v, char *stage, int q) {
+        const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
+        *reinterpret_cast<u32x4 *>(stage + (q < S::kLoadsW ? 0 : S::MO * kStep) + lds_at(c >> 3, c & 7)) = v;
     };
 
-    i32x4 fw[2][S::TO], fx[2][S::TT];
-    auto read = [&](const char *stage, int s) {
-        const int chunk = 2 * s + (lane >> 5);
+    // While a round is multiplied, the next one goes from registers to LDS, and each register is loaded anew for the one after it.  A
+    // beat's rows of W are read two beats ahead, all of its tokens' codes in the two beats before their first; so the barrier stands
+    // two beats before the round's end.  Beats are kept apart: the compiler otherwise moves all loads to a round's end.
+    i32x4 fw[4], fx[2][S::TT];
+    auto read_w = [&](const char *stage, int beat) {
+        const int m = beat % S::TO, s = beat / S::TO;
+        fw[beat & 3] = *reinterpret_cast<const i32x4 *>(stage + lds_at((wo * S::TO + m) * 16 + (lane & 15), 4 * s + (lane >> 4)));
+    };
+    auto read_x = [&](const char *stage, int s, int half) {
 #pragma unroll
-        for (int m = 0; m < S::TO; ++m)
-            fw[s & 1][m] = *reinterpret_cast<const i32x4 *>(stage + lds_at((wo * S::TO + m) * 32 + (lane & 31), chunk));
-#pragma unroll
-        for (int n = 0; n < S::TT; ++n)
-            fx[s & 1][n] = *reinterpret_cast<const i32x4 *>(stage + S::MO * kStep + lds_at((wt * S::TT + n) * 32 + (lane & 31), chunk));
+        for (int n = half * S::TT / 2; n < (half + 1) * S::TT / 2; ++n)
+            fx[s][n] = *reinterpret_cast<const i32x4 *>(stage + S::MO * kStep + lds_at((wt * S::TT + n) * 16 + (lane & 15), 4 * s + (lane >> 4)));
     };
     char *here = lds, *next = lds + S::kStage;
+    u32x4 v[S::kLoads];
     {                                      // both first rounds asked for at once: the memory's latency once, not twice
         u32x4 first[S::kLoads];
 #pragma unroll
-        for (int d = 0; d < kDeals; ++d) load(first, k_begin, d);
+        for (int q = 0; q < S::kLoads; ++q) first[q] = load(k_begin, q);
 #pragma unroll
-        for (int d = 0; d < kDeals; ++d) load(v, k_begin + kStep, d);
+        for (int q = 0; q < S::kLoads; ++q) v[q] = load(k_begin + kStep, q);
 #pragma unroll
-        for (int d = 0; d < kDeals; ++d) store(first, here, d);
+        for (int q = 0; q < S::kLoads; ++q) store(first[q], here, q);
     }
-    i32x16 acc[S::TO][S::TT] = {};
+    i32x4 acc[S::TO][S::TT] = {};
     lds_barrier();
-    read(here, 0);
+    read_x(here, 0, 0);
+    read_w(here, 0);
+    read_x(here, 0, 1);
+    read_w(here, 1);
     for (int k0 = k_begin; k0 < k_end; k0 += kStep) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s < kDeals) {
-                read(here, s + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                store(v, next, s);
-                load(v, k0 + 2 * kStep, s);
-            } else {
-                lds_barrier();
-                read(next, 0);
-            }
+        for (int beat = 0; beat < S::kBeats; ++beat) {
+            const int ahead = beat + 2;
+            if (ahead == S::kBeats) lds_barrier();
+            // (the tokens' codes of the next 64 go with the first two rows of W that need them)
+            if (ahead % S::TO < 2) read_x(ahead < S::kBeats ? here : next, ahead / S::TO & 1, ahead % S::TO);
+            read_w(ahead < S::kBeats ? here : next, ahead % S::kBeats);
+#pragma unroll
+            for (int q = 0; q < S::kLoads; ++q)
+                if (q * (S::kBeats - 2) / S::kLoads == beat) {
+                    store(v[q], next, q);
+                    v[q] = load(k0 + 2 * kStep, q);
+                }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int m = 0; m < S::TO; ++m)
-#pragma unroll
-                for (int n = 0; n < S::TT; ++n)
-                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[s & 1][m], fx[s & 1][n], acc[m][n], 0, 0, 0);
+            for (int n = 0; n < S::TT; ++n)
+                acc[beat % S::TO][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[beat & 3], fx[beat / S::TO][n], acc[beat % S::TO][n], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
         char *const t = here;
         here = next;
         next = t;
     }
-
     lds_barrier();                         // (the results may lie where another wave still reads)
-    write_out<T, S>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 32, t0 + wt * S::TT * 32, split);
+    write_out<T, S>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 16, t0 + wt * S::TT * 16, split);
 }
 
 // ---- few tokens, few outputs: the waves of a workgroup share the contraction -------------------
