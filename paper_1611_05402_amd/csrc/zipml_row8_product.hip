@@ -25,7 +25,7 @@ struct ProductArgs {
 // Results that the caches would not hold until they are read: written past them (16,384 x 4,096 bf16 and 4,096 inputs: 237 us against 246,
 // 520 inputs: 67 against 78).
 constexpr int64_t kThroughLeast = 96ll << 20;
-constexpr int kStep = 128;      // codes of a row that are in LDS at a time
+constexpr int kStep = 128;      // codes of a row that are in LDS at a time (2^7)
 
 // Rows of codes as a buffer: rows behind the last one, and what lies behind a row's padding, read as zeros.
 struct CodeRows {
@@ -402,39 +402,39 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 //   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
 //   them: k * shared) + (ranges > 1: a launch, sums written and read).
 // The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
-// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 29 % at most.
+// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 28 % at most.
 struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
 };
 static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
 {
+    // outputs, tokens and waves of a tile as powers of two: the choice is made in every call, and divisions are what it would cost
     struct Cost { int outs, tokens, waves; double start, turn, lone, shared; };
     static const Cost costs[] = {
-        {16, 16, 4, 2.19, 0.00, 0.28, 0.25}, {16, 16, 8, 2.15, 0.00, 0.47, 0.50},
-        {16, 16, 16, 1.88, 0.00, 0.90, 1.12}, {32, 32, 4, 2.24, 0.06, 0.56, 0.51},
-        {32, 32, 8, 2.15, 0.13, 0.95, 1.03}, {32, 32, 16, 1.22, 0.00, 2.09, 2.41},
-        {64, 32, 8, 2.18, 2.36, 1.51, 1.38}, {64, 64, 8, 3.06, 2.93, 1.98, 2.06},
-        {128, 64, 1, 3.80, 1.39, 0.51, 0.43}, {128, 128, 1, 4.36, 2.70, 0.59, 0.61},
-        {256, 256, 1, 9.68, 8.00, 1.30, 1.78},
+        {4, 4, 2, 2.18, 0.00, 0.29, 0.25}, {4, 4, 3, 2.15, 0.00, 0.47, 0.50},
+        {4, 4, 4, 1.87, 0.00, 0.91, 1.12}, {5, 5, 2, 2.25, 0.03, 0.56, 0.51},
+        {5, 5, 3, 2.15, 0.04, 0.95, 1.05}, {5, 5, 4, 1.22, 0.00, 2.09, 2.44},
+        {6, 5, 3, 2.19, 2.25, 1.50, 1.37}, {6, 6, 3, 3.03, 3.28, 1.95, 1.89},
+        {7, 6, 0, 3.69, 1.30, 0.47, 0.41}, {7, 7, 0, 4.05, 2.55, 0.55, 0.58},
+        {8, 8, 0, 9.44, 11.96, 1.25, 1.40},
     };
+    const auto parts = [](int64_t n, int log) { return (n + (1ll << log) - 1) >> log; };
     const int64_t bytes = round_up(d_in, kRow8Unit), sums = rows * round_up(d_out, 4) * 4;
     ProductPlan best{-1, 1, 0, 0};
     double least = 0;
     for (int shape = 0; shape < (int)(sizeof(costs) / sizeof(costs[0])); ++shape) {
         const Cost &c = costs[shape];
-        const int64_t tiles = ((d_out + c.outs - 1) / c.outs) * ((rows + c.tokens - 1) / c.tokens);
-        if (tiles > 0x3FFFFFFF) continue;
-        const double k1 = (double)((tiles + 255) / 256);
-        if (best.shape >= 0 && c.start + (k1 - 1) * c.turn >= least) continue;
+        const int64_t tiles = parts(d_out, c.outs) * parts(rows, c.tokens);
+        if (tiles > 0x3FFFFFFF || (best.shape >= 0 && c.start + (double)(parts(tiles, 8) - 1) * c.turn >= least)) continue;
         for (const int wanted : {1, 2, 3, 4, 8, 16}) {
             // (ranges of two rounds at least, whose sums stay in the caches)
-            if (wanted > 1 && (c.waves > 1 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;
-            const int64_t range = round_up((bytes + wanted - 1) / wanted, kStep), ranges = (bytes + range - 1) / range;
-            const double k = (double)((tiles * ranges + 255) / 256), step = (double)kStep * c.waves;
-            const double rounds = (double)(int64_t)(((double)(range < bytes ? range : bytes) + step - 1) / step);
+            if (wanted > 1 && (c.waves > 0 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;
+            const int64_t range = wanted == 1 ? parts(bytes, 7) << 7 : round_up((bytes + wanted - 1) / wanted, kStep);
+            const int64_t ranges = wanted == 1 ? 1 : (bytes + range - 1) / range;
+            const double k = (double)parts(tiles * ranges, 8), rounds = (double)parts(range < bytes ? range : bytes, 7 + c.waves);
             const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && k * c.shared > c.lone ? k * c.shared : c.lone) +
-                              (ranges > 1 ? 2.1 + (double)(ranges * sums) * 2 / 5.8e6 : 0.0);
+                              (ranges > 1 ? 3.0 + (double)(ranges * sums) * 2 / 6.4e6 : 0.0);
             if (best.shape < 0 || us < least) {
                 least = us;
                 best = ProductPlan{shape, (int)ranges, (int)range, ranges > 1 ? (size_t)(ranges * sums) : 0};
