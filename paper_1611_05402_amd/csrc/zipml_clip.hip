@@ -5,7 +5,9 @@
 // Two passes over the gradients, each one launch for kClipTensors of them: the first leaves one sum a workgroup, the second adds
 // these up (every workgroup for itself, in the same order) and scales.  Squares are summed in 64 bits, so that no gradient that
 // fp32 holds overflows and the norm does not depend on the order.  The second pass goes from the last chunk to the first: what the
-// first pass has read last is still in the caches.
+// first pass has read last is still in the caches, and results are written past them.  302 million fp32 values into a bf16 bucket: 193 us
+// for 1.2 GB, then 327 for 1.8 GB (6.2 and 5.5 TB/s, part of it out of the caches); in one pass over the gradients, which no cache holds,
+// it cannot be done.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -13,7 +15,7 @@ namespace zipml {
 constexpr int kClipTensors = 96;          // of a launch: what its arguments hold
 constexpr int kClipGroups = 1024;         // workgroups of a launch
 // Units of eight values that a thread has under way: four, or one where chunks of four would leave compute units idle (1.6 million
-// values: XXX).
+// values: 8.6 us in both launches, 9.6 with four and with the tensors searched for in the arguments).
 constexpr int kClipMany = 4, kClipFew = 1;
 constexpr int64_t clip_chunk(int units) { return 256 * 8 * units; }
 

@@ -5,6 +5,10 @@
 //
 // The mean square is summed in 64 bits: with rstd rounded to fp32 once and every further step a single fp32 operation, the codes of
 // a row do not depend on the order of the sum, so they can be checked bit for bit (64-bit adds cost nothing next to the bytes).
+//
+// Both passes read and write every byte once and are bound by them.  16,384 x 4,096 bf16: forward 91 to 98 us (two tensors in, the sum
+// and codes out 470 MB, the sum and y 537 MB: 5.0 to 5.6 TB/s), backward 107 to 109 (537 MB, and 17 of dgain's sums), joining these 7.
+// 1,000 x 1,001 fp32: 5.9, 5.8 and 3.6 us, of which an empty launch is 1.4.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -156,7 +160,9 @@ struct NormGradArgs {
     int64_t lddy, ldsum, lddsum, lddx, rows, cols, units, pitch;
 };
 
-// A workgroup takes every gridDim.x-th row (or set of rows, one for each wave) and keeps dgain's sums of its rows in registers.
+// A workgroup takes every gridDim.x-th row (or set of rows, one for each wave) and keeps dgain's sums of its rows in registers.  1,024
+// workgroups: 512 have too few loads under way (157 us in place of 108 at 16,384 x 4,096).  Rows of more than 16,384 values are read
+// twice: the registers of 1,024 threads do not hold four such arrays.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
 {

@@ -171,7 +171,9 @@ struct RowShape {
     static __device__ __forceinline__ int team() { return TPR == kThreads ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); }
     static __device__ __forceinline__ int lane() { return threadIdx.x % TPR; }
 };
-// Calls f with the shape for `rows` rows of so many units, of which registers are to hold `most` at most.
+// Calls f with the shape for `rows` rows of so many units, of which registers are to hold `most` at most.  A wave to a row needs no
+// barrier; where there are few rows, more waves to each bring its loads under way at once (one row of 2,048 through the norm: 2.6 us
+// with four waves, 4.8 with one; at 1,000 rows of 1,001 four waves are as fast as one, and 15 % slower in encoding).
 template <typename F>
 inline int with_row_shape(int64_t rows, int64_t units, int64_t most, F f)
 {

@@ -12,7 +12,9 @@ struct Row8Args {
     uint32_t epoch, stream;
 };
 
-// A row waits in registers between the search for its largest magnitude and the rounding; rows too long for that are read twice.
+// A row waits in registers between the search for its largest magnitude and the rounding; rows too long for that are read twice.  Bound by
+// the bytes: 16,384 x 4,096 bf16, 201 MB in 40 to 45 us (4.5 to 5.0 TB/s).  1,000 x 1,001 fp32 by draws: 3.4 us, of which 1.4 are an
+// empty launch.
 template <typename T, typename S, bool DRAWS>
 __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
 {
@@ -57,6 +59,7 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
     }
 }
 
+// Four rows of eight columns a thread, as in zipml_act.hip.  16,384 x 4,096 to bf16: 30 to 32 us, the codes out of the cache.
 template <typename T>
 __global__ __launch_bounds__(256) void k_row8_decode(const uint8_t *codes, int64_t ldc, const float *scales, int64_t rows,
                                                      int64_t cols, ActGrid g, T *out, int64_t ldo)

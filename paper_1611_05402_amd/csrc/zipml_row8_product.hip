@@ -2,7 +2,13 @@
 //
 // The sums are integers: exact in any order (|code| <= 128 and d_in < 2^17 keep them in 32 bits), so how the contraction is split
 // changes no bit of the result.  Both operands are contracted along their rows, 16 codes of a row are 16 bytes, and a lane of
-// v_mfma_i32_32x32x32_i8 wants just those of one row: tiles lie in LDS as they lie in memory, and are read 16 bytes at a time.
+// the matrix instructions wants just those of one row: tiles lie in LDS as they lie in memory, and are read 16 bytes at a time.
+//
+// Two kinds of kernels, chosen by a model of their times (product_plan): few tokens or outputs are bound by the bytes of W and by latency
+// (one token, 4,096 x 4,096: 5.4 us, 3.4 at the rate of a copy, 1.4 an empty launch; 64 tokens, 8,192 -> 1,024: 6.0; 1,000 tokens,
+// 520 -> 1,001, fp32: 5.9), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 227 us in a long run,
+// 2,420 TOP/s, 178 on zeros with the larger instructions; a library product of the same codes without scales 288; 4,096 tokens, 16,384 ->
+// 4,096: 211 us, 2,600 TOP/s, the library 217).  Of the 227 us some 35 are the results' way out, 134 MB.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -55,20 +61,22 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
-// Scales (and bias) of four neighbouring outputs, and four results of a token from them.
+// Scales (and bias) of four neighbouring outputs and of a token, and four results from them.
 struct Out4 {
-    float sw[4], bias[4];
-    int n;                      // how many of them there are
-    __device__ __forceinline__ Out4(const ProductArgs &a, int o) : n(a.d_out - o)
+    f32x4 sw, bias;
+    float sx;
+    int n;                      // how many of the outputs there are
+    __device__ __forceinline__ Out4() {}
+    __device__ __forceinline__ Out4(const ProductArgs &a, int64_t t, int o) : n(a.d_out - o)
     {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            sw[k] = k < n ? a.sw[o + k] : 0.0f;
-            bias[k] = a.bias && k < n ? a.bias[o + k] : 0.0f;
-        }
+        const auto scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.sw), 0, a.d_out * 4, 0x00020000);
+        const auto biases = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.bias), 0, a.bias ? a.d_out * 4 : 0, 0x00020000);
+        sw = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, o * 4, 0, 0));
+        bias = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, o * 4, 0, 0));
+        sx = a.sx[t < a.rows ? t : a.rows - 1];
     }
     template <typename T>
-    __device__ __forceinline__ void put(const ProductArgs &a, T *y, float sx, i32x4 sum) const
+    __device__ __forceinline__ void put(const ProductArgs &a, T *y, i32x4 sum) const
     {
         float v[4];
 #pragma unroll
@@ -313,9 +321,17 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product_split(ProductArgs 
 #pragma unroll
         for (int q = 0; q < S::kLoadsX; ++q) vx[q] = x.load16(there, at_x + k0, q * 8);
     };
+    load(wave * kStep);
+    // what the results need, long before they are there (5.7 -> 5.4 us at one token, 4,096 x 4,096)
+    constexpr int kUnits = S::MT * S::MO / 4, kMine = (kUnits + S::kThreads - 1) / S::kThreads;
+    Out4 out[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const int i = threadIdx.x + k * S::kThreads;
+        if (kUnits % S::kThreads == 0 || i < kUnits) out[k] = Out4(a, t0 + i / (S::MO / 4), o0 + i % (S::MO / 4) * 4);
+    }
     i32x16 acc[S::TO][S::TT] = {};
     i32x4 small = {};
-    load(wave * kStep);
     for (int k0 = wave * kStep; k0 < a.bytes; k0 += S::WAVES * kStep) {
 #pragma unroll
         for (int q = 0; q < S::kLoadsW; ++q)
@@ -367,13 +383,14 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product_split(ProductArgs 
                         i32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
     }
     lds_barrier();
-    for (int i = threadIdx.x; i < S::MT * S::MO / 4; i += S::kThreads) {
-        const int t = i / (S::MO / 4), o = i % (S::MO / 4) * 4;
-        if (t0 + t >= a.rows || o0 + o >= a.d_out) continue;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const int i = threadIdx.x + k * S::kThreads, t = i / (S::MO / 4), o = i % (S::MO / 4) * 4;
+        if (i >= kUnits || t0 + t >= a.rows || o0 + o >= a.d_out) continue;
         i32x4 sum = {};
 #pragma unroll
         for (int v = 0; v < S::WAVES; ++v) sum += *reinterpret_cast<const i32x4 *>(lds + v * S::kWave + (t * S::kRow + o) * 4);
-        Out4(a, o0 + o).put(a, (T *)a.y + (t0 + t) * a.ldy + o0 + o, a.sx[t0 + t], sum);
+        out[k].put(a, (T *)a.y + (t0 + t) * a.ldy + o0 + o, sum);
     }
 }
 
@@ -385,11 +402,12 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
     const int64_t i = blockIdx.x * 256ll + threadIdx.x, t = i / units;
     const int o = (int)(i - t * units) * 4;
     if (t >= a.rows) return;
+    const Out4 out(a, t, o);
     const int *p = part + t * ld_part + o;
     i32x4 sum = *reinterpret_cast<const i32x4 *>(p);
 #pragma unroll 4
     for (int r = 1; r < ranges; ++r) sum += *reinterpret_cast<const i32x4 *>(p + r * a.part);
-    Out4(a, o).put(a, (T *)a.y + t * a.ldy + o, a.sx[t], sum);
+    out.put(a, (T *)a.y + t * a.ldy + o, sum);
 }
 
 // The shapes: tiles whose waves share the contraction (outputs, tokens, waves), tiles whose waves share the rows (outputs, tokens, waves
