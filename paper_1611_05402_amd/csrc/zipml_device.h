@@ -198,18 +198,27 @@ __device__ __forceinline__ T wave_sum_dpp(T v)
     return wave_reduce_dpp(v, [](T x, T y) { return x + y; });
 }
 
-// The same sum for doubles (two moves a step; through __shfl_xor a step costs two LDS round trips).
-__device__ __forceinline__ double wave_sum_dpp(double v)
+// The same sums for doubles (two moves a step; through __shfl_xor a step costs two LDS round trips): every lane gets that of its row of
+// 16 lanes, or of the 64.
+template <typename Move>
+__device__ __forceinline__ double moved(double x, Move move)
 {
-    auto moved = [](double x, auto move) {
-        const uint64_t b = __builtin_bit_cast(uint64_t, x);
-        const uint32_t lo = move((uint32_t)b), hi = move((uint32_t)(b >> 32));
-        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-    };
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = move((uint32_t)b), hi = move((uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double row_sum_dpp(double v)
+{
     v += moved(v, [](uint32_t w) { return dpp_move<0xB1>(w); });
     v += moved(v, [](uint32_t w) { return dpp_move<0x4E>(w); });
     v += moved(v, [](uint32_t w) { return dpp_move<0x141>(w); });
     v += moved(v, [](uint32_t w) { return dpp_move<0x140>(w); });
+    return v;
+}
+__device__ __forceinline__ float row_sum_dpp(float v) { return row_reduce_dpp(v, [](float x, float y) { return x + y; }); }
+__device__ __forceinline__ double wave_sum_dpp(double v)
+{
+    v = row_sum_dpp(v);
     auto row = [&](int l) { return moved(v, [l](uint32_t w) { return (uint32_t)__builtin_amdgcn_readlane((int)w, l); }); };
     return (row(0) + row(16)) + (row(32) + row(48));
 }

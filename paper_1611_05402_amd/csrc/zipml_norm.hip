@@ -42,7 +42,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
         if (!a.gain) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) g[k] = 1.0f;
-        } else if constexpr (S::NV > 0) {
+        } else if constexpr (S::kBuffer) {
             Row<float>(a.gain, 0, a.cols).load8((int)u, g);
         } else {
             load8(a.gain + u * 8, a.cols - u * 8, g);
@@ -57,11 +57,11 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_forward(NormArgs a)
         double square = 0;
         // eight values of a tensor's row
         auto get = [&](const void *tensor, int64_t ld, int64_t u, float (&w)[8]) {
-            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
+            if constexpr (S::kBuffer) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
             else load8((const T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
         };
         auto set = [&](void *tensor, int64_t ld, int64_t u, const float (&w)[8]) {
-            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).store8((int)u, w);
+            if constexpr (S::kBuffer) Row<T>(tensor, row * ld, a.cols).store8((int)u, w);
             else store8((T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
         };
         auto added = [&](float (&w)[8], const float (&o)[8]) {
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
         if (!a.gain) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) g[k] = 1.0f;
-        } else if constexpr (S::NV > 0) {
+        } else if constexpr (S::kBuffer) {
             Row<float>(a.gain, 0, a.cols).load8((int)u, g);
         } else {
             load8(a.gain + u * 8, a.cols - u * 8, g);
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
         const float rstd = a.rstd[row];
         float g[NV][8], n[NV][8], o[NV][8] = {}, along = 0.0f;
         auto get = [&](const void *tensor, int64_t ld, int64_t u, float (&w)[8]) {
-            if constexpr (S::NV > 0) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
+            if constexpr (S::kBuffer) Row<T>(tensor, row * ld, a.cols).load8((int)u, w);
             else load8((const T *)tensor + row * ld + u * 8, a.cols - u * 8, w);
         };
         // g = dy, n = r rstd of unit u
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
         auto put = [&](int64_t u, const float (&p)[8], const float (&q)[8], float (&d)[8]) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) d[k] = __builtin_fmaf(rstd, __builtin_fmaf(-along, q[k], p[k]), d[k]);
-            if constexpr (S::NV > 0) Row<T>(a.dx, row * a.lddx, a.cols).store8((int)u, d);
+            if constexpr (S::kBuffer) Row<T>(a.dx, row * a.lddx, a.cols).store8((int)u, d);
             else store8((T *)a.dx + row * a.lddx + u * 8, a.cols - u * 8, d);
         };
         if constexpr (S::NV > 0) {
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
     if constexpr (S::NV > 0) {
         if (!part) return;
         if constexpr (S::kRows > 1) {      // the four waves' sums
-            __shared__ float sums[S::kRows - 1][NV][8][kWave];
+            __shared__ float sums[S::kRows - 1][NV][8][S::TPR];
             if (team > 0)
 #pragma unroll
                 for (int k = 0; k < NV; ++k)

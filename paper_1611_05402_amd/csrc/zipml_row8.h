@@ -75,7 +75,7 @@ __device__ __forceinline__ u32x2 row8_stochastic8(const float (&v)[8], const Row
 }
 
 // ---- teams of threads that share a row --------------------------------------------------------
-// A wave, or a workgroup of TPR threads; scratch: one value for each wave of the workgroup, another one for each reduction
+// Sixteen lanes, a wave, or a workgroup of TPR threads; scratch: one value for each wave of the workgroup, another one for each reduction
 // between two uses of the same scratch a barrier has to pass.
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
@@ -84,6 +84,10 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 template <int TPR>
 __device__ __forceinline__ uint32_t team_max(uint32_t v, uint32_t *scratch)
 {
+    if constexpr (TPR < kWave) {
+        static_assert(TPR == 16, "rows of DPP");
+        return row_reduce_dpp(v, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    }
     v = wave_max(v);
     if constexpr (TPR > kWave) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
@@ -96,6 +100,7 @@ __device__ __forceinline__ uint32_t team_max(uint32_t v, uint32_t *scratch)
 template <int TPR, typename F>
 __device__ __forceinline__ F team_sum(F v, F *scratch)
 {
+    if constexpr (TPR < kWave) return row_sum_dpp(v);
     v = wave_sum_dpp(v);
     if constexpr (TPR > kWave) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
@@ -167,8 +172,13 @@ struct Row {
 template <int TPR_, int NV_>
 struct RowShape {
     static constexpr int TPR = TPR_, NV = NV_, kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
-    // the team's number in the workgroup, the same for a whole wave
-    static __device__ __forceinline__ int team() { return TPR == kThreads ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); }
+    static constexpr bool kBuffer = NV > 0 && TPR >= kWave;       // rows are read and written as buffers, whose base a wave shares
+    // the team's number in the workgroup, the same for a whole wave where that is no more than a team
+    static __device__ __forceinline__ int team()
+    {
+        const int t = (int)threadIdx.x / TPR;
+        return TPR == kThreads ? 0 : TPR < kWave ? t : __builtin_amdgcn_readfirstlane(t);
+    }
     static __device__ __forceinline__ int lane() { return threadIdx.x % TPR; }
 };
 // Calls f with the shape for `rows` rows of so many units, of which registers are to hold `most` at most.  A wave to a row needs no
@@ -178,6 +188,8 @@ template <typename F>
 inline int with_row_shape(int64_t rows, int64_t units, int64_t most, F f)
 {
     if (units > most) return f(RowShape<1024, 0>());
+    if (units <= 16) return f(RowShape<16, 1>());
+    if (rows >= kFewRows && units <= 32) return f(RowShape<16, 2>());
     if (units <= 64) return f(RowShape<64, 1>());
     if (rows < kFewRows && units <= 256) return f(RowShape<256, 1>());
     if (rows < kFewRows && units <= 1024) return f(RowShape<1024, 1>());

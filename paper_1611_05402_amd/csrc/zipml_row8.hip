@@ -23,7 +23,6 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * S::kRows + team; row < a.rows; row += (int64_t)gridDim.x * S::kRows, turn ^= 1) {
         const T *x = (const T *)a.x + row * a.ldx;
-        const Row<T> in(a.x, row * a.ldx, a.cols);
         uint8_t *codes = a.codes + row * a.ldc;
         float v[S::NV ? S::NV : 1][8];
         uint32_t top = 0;
@@ -35,7 +34,11 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
         };
         if constexpr (S::NV > 0) {
 #pragma unroll
-            for (int k = 0; k < S::NV; ++k) in.load8(lane + k * S::TPR, v[k]);
+            for (int k = 0; k < S::NV; ++k) {
+                const int u = lane + k * S::TPR;
+                if constexpr (S::kBuffer) Row<T>(a.x, row * a.ldx, a.cols).load8(u, v[k]);
+                else load8(x + u * 8, a.cols - u * 8, v[k]);
+            }
 #pragma unroll
             for (int k = 0; k < S::NV; ++k) top = top_of(v[k], top);
         } else {

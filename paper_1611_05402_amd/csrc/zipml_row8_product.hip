@@ -28,9 +28,11 @@ struct ProductArgs {
     int64_t part;               // sums of a range, [rows][ldy], behind those of the one before
 };
 
-// Results that the caches would not hold until they are read: written past them (16,384 x 4,096 bf16 and 4,096 inputs: 237 us against 246,
-// 520 inputs: 67 against 78).
-constexpr int64_t kThroughLeast = 96ll << 20;
+// Results of which the caches would hold little until they are read, in rows that begin at a line of 128 bytes, are written past them:
+// 16,384 x 4,096 bf16 and 520 inputs 60 us against 70 (with an elementwise kernel that reads them next 106 against 110), 4,096 inputs 223
+// against 233, 8,192 x 4,096 and 520 inputs 32 against 34 (54 against 56); 4,096 x 4,096 is slower to read next (30 against 28.7 for both).
+// Rows that share lines need the caches to put these together: 10,022 x 8,825, 112 inputs, 142 us past them and 74 through them.
+constexpr int64_t kThroughLeast = 48ll << 20;
 constexpr int kStep = 128;      // codes of a row that are in LDS at a time (2^7)
 
 // Rows of codes as a buffer: rows behind the last one, and what lies behind a row's padding, read as zeros.
@@ -128,7 +130,7 @@ struct ProductShape {
 
 // What a wave has summed, on its way out.  A lane holds four neighbouring outputs of one token at a time.  Through LDS of its own (`out`), a
 // wave turns 32 tokens' lines of 128 bytes around and writes them 16 bytes a lane.
-template <typename T, typename S>
+template <typename T, typename S, bool THROUGH>
 __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&acc)[S::TO][S::TT], char *out, int o_wave, int64_t t_wave,
                                           uint32_t split)
 {
@@ -141,23 +143,25 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
         const int64_t t = t_wave + n * 16 + (lane & 15);
         sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
     }
+    // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256; -0 leaves every value as it is)
+    f32x4 sw[S::TO], bias[S::TO];
+    const int at = (o_wave + 4 * (lane >> 4)) * 4;
 #pragma unroll
-    for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
-        constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
-        const int o = o_wave + m0 * 16 + (lane & 7) * V, left = a.d_out - o, at = (o_wave + m0 * 16 + 4 * (lane >> 4)) * 4;
-        // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256; -0 leaves every value as it is)
-        f32x4 sw[S::HO], bias[S::HO];
+    for (int m = 0; m < S::TO && !S::kParts; ++m) {
+        sw[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at + m * 64, 0, 0));
+        bias[m] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
+    }
+    if (a.bias)
 #pragma unroll
-        for (int m = 0; m < S::HO && !S::kParts; ++m) {
-            sw[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at + m * 64, 0, 0));
-            bias[m] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
-        }
-        if (a.bias)
+        for (int m = 0; m < S::TO && !S::kParts; ++m)
+            bias[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at + m * 64, 0, 0));
+    // (a token's lines one after the other: rows that do not begin at a line's start share lines, which the L2 has to put together)
 #pragma unroll
-            for (int m = 0; m < S::HO && !S::kParts; ++m)
-                bias[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at + m * 64, 0, 0));
+    for (int n0 = 0; n0 < S::TT; n0 += 2) {
 #pragma unroll
-        for (int n0 = 0; n0 < S::TT; n0 += 2) {
+        for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
+            constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
+            const int o = o_wave + m0 * 16 + (lane & 7) * V, left = a.d_out - o;
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -168,7 +172,7 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
                     for (int k = 0; k < 4; ++k) {
                         const int sum = acc[m0 + m][n0 + n][k];
                         if constexpr (S::kParts) r[k] = sum;
-                        else r[k] = (T)((float)sum * sx[n0 + n] * sw[m][k] + bias[m][k]);
+                        else r[k] = (T)((float)sum * sx[n0 + n] * sw[m0 + m][k] + bias[m0 + m][k]);
                     }
                     const int row = n * 16 + (lane & 15), byte = (m * 16 + 4 * (lane >> 4)) * (int)sizeof(T);
                     *reinterpret_cast<T4 *>(out + lds_at(row, byte >> 4) + (byte & 15)) = r;
@@ -182,7 +186,7 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
                 if (t >= a.rows) continue;
                 T *const y = (T *)a.y + split * a.part + t * a.ldy + o;
                 if (left >= V) {
-                    if (a.through) __builtin_nontemporal_store((u32x4_any)line, reinterpret_cast<u32x4_any *>(y));
+                    if constexpr (THROUGH) __builtin_nontemporal_store((u32x4_any)line, reinterpret_cast<u32x4_any *>(y));
                     else *reinterpret_cast<u32x4_any *>(y) = line;
                 } else {
 #pragma unroll
@@ -199,7 +203,8 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
     }
 }
 
-template <typename T, typename S>
+// THROUGH: results are written past the caches (a kernel of its own: of a branch the compiler makes one store, which is not).
+template <typename T, typename S, bool THROUGH>
 __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
         next = t;
     }
     lds_barrier();                         // (the results may lie where another wave still reads)
-    write_out<T, S>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 16, t0 + wt * S::TT * 16, split);
+    write_out<T, S, THROUGH>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 16, t0 + wt * S::TT * 16, split);
 }
 
 // ---- few tokens, few outputs: the waves of a workgroup share the contraction -------------------
@@ -469,8 +474,8 @@ static int launch_tiles(hipStream_t s, ProductArgs a, K k)
     a.tiles_o = (a.d_out + S::MO - 1) / S::MO;
     const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * a.ranges;
     a.tiles_t = (int)tiles;
-    static std::atomic<uint64_t> done;
-    if (allow_lds((const void *)k, S::kLds, done)) return ZIPML_ELAUNCH;
+    static std::atomic<uint64_t> done[2];
+    if (allow_lds((const void *)k, S::kLds, done[a.through])) return ZIPML_ELAUNCH;
     hipLaunchKernelGGL(k, dim3((uint32_t)all), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
@@ -489,7 +494,7 @@ static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, vo
         a.part = parts.part = a.rows * parts.ldy;
         int rc = ZIPML_EINVAL;
         switch (p.shape) {
-#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<int, S>(s, parts, k_row8_product<int, S>); break; }
+#define TILE(n, ...) case n: { typedef ProductShape<int, __VA_ARGS__> S; rc = launch_tiles<int, S>(s, parts, k_row8_product<int, S, false>); break; }
             ZIPML_PRODUCT_TILE(TILE)
 #undef TILE
         }
@@ -500,7 +505,7 @@ static int launch_product(hipStream_t s, ProductArgs a, const ProductPlan &p, vo
     }
     switch (p.shape) {
 #define SPLIT(n, o, t, waves) case n: { typedef SplitShape<o, t, waves> S; return launch_tiles<T, S>(s, a, k_row8_product_split<T, S>); }
-#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<T, S>(s, a, k_row8_product<T, S>); }
+#define TILE(n, ...) case n: { typedef ProductShape<T, __VA_ARGS__> S; return launch_tiles<T, S>(s, a, a.through ? k_row8_product<T, S, true> : k_row8_product<T, S, false>); }
         ZIPML_PRODUCT_SPLIT(SPLIT)
         ZIPML_PRODUCT_TILE(TILE)
 #undef SPLIT
@@ -542,9 +547,11 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
     if (!aligned16(x_dev) || !aligned16(w_dev) || !aligned16(y_dev) || !aligned16(workspace_dev) || !aligned4(x_scales_dev) ||
         !aligned4(w_scales_dev) || !aligned4(bias_dev))
         return ZIPML_EALIGN;
+    const int64_t size = (int64_t)dtype_bytes(dtype);
+    const int through = rows * d_out * size > kThroughLeast && ldy * size % 128 == 0 && reinterpret_cast<uintptr_t>(y_dev) % 128 == 0;
     ProductArgs a{(const uint8_t *)x_dev, (const uint8_t *)w_dev, x_scales_dev, w_scales_dev, bias_dev, y_dev, ldx, ldw, ldy, rows,
                   (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0, 0, 0,
-                  rows * d_out * (int64_t)dtype_bytes(dtype) > kThroughLeast, 0};
+                  through, 0};
     hipStream_t s = entry_stream(stream);
     return dtype == ZIPML_F32 ? launch_product<float>(s, a, p, workspace_dev) : launch_product<__bf16>(s, a, p, workspace_dev);
 }

@@ -16,7 +16,7 @@ OTHER, THIRD = C.c_void_p(0x2000), C.c_void_p(0x3000)
 TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
 HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
 SIZES = [(1, 1, 0), (1, 2048, 0), (3, 15, 1), (5, 16, 0), (7, 17, 2), (2, 64, 8), (130, 70, 5), (64, 1021, 3), (1000, 8, 0), (9, 2056, 8),
-         (33, 4104, 0), (3, 9001, 1), (2, 16392, 0), (3, 33000, 5), (1100, 520, 0), (4500, 24, 0)]
+         (33, 4104, 0), (3, 9001, 1), (2, 16392, 0), (3, 33000, 5), (1100, 520, 0), (4500, 24, 0), (601, 200, 3), (515, 255, 0), (17, 128, 1), (16500, 130, 0), (16399, 9, 0)]
 EPS = 1e-6
 
 

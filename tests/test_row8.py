@@ -13,7 +13,7 @@ from paper_1611_05402_amd import zipml
 DEV = "cuda"
 FAKE, ODD, HALF = C.c_void_p(0x1000), C.c_void_p(0x1004), C.c_void_p(0x1002)     # never dereferenced: the checks come first
 SIZES = [(1, 1, 0), (1, 2048, 0), (3, 15, 1), (5, 16, 0), (7, 17, 2), (2, 64, 8), (130, 70, 5), (64, 1021, 3), (1000, 8, 0), (9, 2056, 8),
-         (33, 4104, 0), (3, 9001, 1), (2, 16392, 0), (2, 33000, 5), (5, 512, 0), (6, 513, 0)]
+         (33, 4104, 0), (3, 9001, 1), (2, 16392, 0), (2, 33000, 5), (5, 512, 0), (6, 513, 0), (601, 200, 3), (515, 255, 0), (2000, 256, 0), (17, 128, 1)]
 
 
 @pytest.fixture(scope="module")
