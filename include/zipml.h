@@ -436,7 +436,7 @@ int zipml_norm_backward(void *stream, const void *dy_dev, int64_t lddy, const vo
 typedef struct {
     const void *grad_dev;
     void *out_dev;
-    int64_t count;               /* values, 0 .. 2^34 */
+    int64_t count;               /* values, 0 .. 2^33 */
     int32_t grad_dtype, out_dtype;
 } zipml_clip_tensor;
 size_t zipml_clip_workspace_bytes(int64_t n_tensors);

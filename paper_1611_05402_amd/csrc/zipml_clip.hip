@@ -12,19 +12,24 @@
 
 namespace zipml {
 
-constexpr int kClipTensors = 96;          // of a launch: what its arguments hold
+constexpr int kClipTensors = 160;         // of a launch: what its arguments hold
 constexpr int kClipGroups = 1024;         // workgroups of a launch
 // Units of eight values that a thread has under way: four, or one where chunks of four would leave compute units idle (1.6 million
 // values: 8.6 us in both launches, 9.6 with four and with the tensors searched for in the arguments).
 constexpr int kClipMany = 4, kClipFew = 1;
 constexpr int64_t clip_chunk(int units) { return 256 * 8 * units; }
 
+constexpr int64_t kClipMost = 1ll << 33;  // values of a tensor: 160 of them are fewer than 2^28 chunks
+
 struct ClipTensor {
     const void *grad;
     void *out;
-    int64_t count;
-    uint32_t first;                       // chunks of the tensors before it
-    uint32_t types;                       // 1: bf16 gradient, 2: bf16 output
+    uint32_t count;                       // its low 32 bits
+    uint32_t more;                        // chunks of the tensors before it, 28 bits; bf16 gradient; bf16 output; two more bits of the count
+    __host__ __device__ uint32_t first() const { return more & 0x0FFFFFFFu; }
+    __host__ __device__ bool grad_bf16() const { return more >> 28 & 1; }
+    __host__ __device__ bool out_bf16() const { return more >> 29 & 1; }
+    __host__ __device__ int64_t values() const { return (int64_t)(more >> 30) << 32 | count; }
 };
 struct ClipArgs {
     ClipTensor t[kClipTensors];
@@ -33,16 +38,17 @@ struct ClipArgs {
 };
 static_assert(sizeof(ClipArgs) + 64 <= 4096, "kernel arguments");
 
-// The launch's tensors, in the registers of each wave: a lane keeps those of its number and of 64 more.  Read all at once: kernel
+// The launch's tensors, in the registers of each wave: a lane keeps every 64th.  Read all at once: kernel
 // arguments lie far away, and a search among them would wait for each step.
 struct ClipTable {
-    ClipTensor own[2];
+    static constexpr int kSets = (kClipTensors + 63) / 64;
+    ClipTensor own[kSets];
     int n;
     __device__ __forceinline__ explicit ClipTable(const ClipArgs &a) : n(a.n)
     {
         const int lane = threadIdx.x & 63;
-        own[0] = a.t[lane < n ? lane : 0];
-        own[1] = a.t[lane + 64 < n ? lane + 64 : 0];
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) own[k] = a.t[lane + 64 * k < n ? lane + 64 * k : 0];
     }
     static __device__ __forceinline__ uint64_t lane_of(uint64_t v, int l)
     {
@@ -53,16 +59,24 @@ struct ClipTable {
     __device__ __forceinline__ ClipTensor at(uint32_t chunk) const
     {
         const int lane = threadIdx.x & 63;
-        const int k = __builtin_popcountll(__ballot(lane < n && own[0].first <= chunk)) +
-                      __builtin_popcountll(__ballot(lane + 64 < n && own[1].first <= chunk)) - 1;
-        const ClipTensor &t = k < 64 ? own[0] : own[1];
-        const int l = k & 63;
-        ClipTensor r;
-        r.grad = (const void *)lane_of((uint64_t)t.grad, l);
-        r.out = (void *)lane_of((uint64_t)t.out, l);
-        r.count = (int64_t)lane_of((uint64_t)t.count, l);
-        r.first = (uint32_t)__builtin_amdgcn_readlane((int)t.first, l);
-        r.types = (uint32_t)__builtin_amdgcn_readlane((int)t.types, l);
+        int at = -1;
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) at += __builtin_popcountll(__ballot(lane + 64 * k < n && own[k].first() <= chunk));
+        // (each set's value is read from its lane before one is chosen: a choice among the registers would put them in memory)
+        const int l = at & 63;
+        ClipTensor r{};
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) {
+            const uint64_t grad = lane_of((uint64_t)own[k].grad, l), out = lane_of((uint64_t)own[k].out, l);
+            const uint32_t count = (uint32_t)__builtin_amdgcn_readlane((int)own[k].count, l);
+            const uint32_t more = (uint32_t)__builtin_amdgcn_readlane((int)own[k].more, l);
+            if (at >> 6 == k) {
+                r.grad = (const void *)grad;
+                r.out = (void *)out;
+                r.count = count;
+                r.more = more;
+            }
+        }
         return r;
     }
 };
@@ -82,8 +96,8 @@ __device__ __forceinline__ void clip_load(const void *p, int64_t at, int64_t cou
 template <int U>
 __device__ __forceinline__ void clip_values(const ClipTensor &t, int64_t at, float (&v)[U][8])
 {
-    if (t.types & 1) clip_load<__bf16>(t.grad, at, t.count, v);
-    else clip_load<float>(t.grad, at, t.count, v);
+    if (t.grad_bf16()) clip_load<__bf16>(t.grad, at, t.values(), v);
+    else clip_load<float>(t.grad, at, t.values(), v);
 }
 
 template <int U>
@@ -95,7 +109,7 @@ __global__ __launch_bounds__(256) void k_clip_norm(ClipArgs a, double *part)
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipTensor t = table.at(c);
         float v[U][8];
-        clip_values(t, (int64_t)(c - t.first) * clip_chunk(U) + threadIdx.x * 8, v);
+        clip_values(t, (int64_t)(c - t.first()) * clip_chunk(U) + threadIdx.x * 8, v);
 #pragma unroll
         for (int q = 0; q < U; ++q)
 #pragma unroll
@@ -118,7 +132,7 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, const double *pa
     ClipTensor t{};
     auto fetch = [&]() {
         t = table.at(a.chunks - 1 - i);
-        if (t.out) clip_values(t, (int64_t)(a.chunks - 1 - i - t.first) * clip_chunk(U) + threadIdx.x * 8, v);
+        if (t.out) clip_values(t, (int64_t)(a.chunks - 1 - i - t.first()) * clip_chunk(U) + threadIdx.x * 8, v);
     };
     if (i < a.chunks) fetch();
     const double norm = __builtin_sqrt(team_sum<256>(sum, scratch));
@@ -128,15 +142,15 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, const double *pa
         norm_out[1] = factor;
     }
     while (i < a.chunks) {
-        const int64_t at = (int64_t)(a.chunks - 1 - i - t.first) * clip_chunk(U) + threadIdx.x * 8;
+        const int64_t at = (int64_t)(a.chunks - 1 - i - t.first()) * clip_chunk(U) + threadIdx.x * 8;
         // (a tensor in place stays as it is where nothing is scaled)
         if (t.out && (t.out != t.grad || factor != 1.0f))
 #pragma unroll
             for (int q = 0; q < U; ++q) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[q][j] *= factor;
-                const int64_t to = at + q * 2048, left = t.count - to;
-                if (t.types & 2) store8<true>((__bf16 *)t.out + to, left, v[q]);
+                const int64_t to = at + q * 2048, left = t.values() - to;
+                if (t.out_bf16()) store8<true>((__bf16 *)t.out + to, left, v[q]);
                 else store8<true>((float *)t.out + to, left, v[q]);
             }
         i += gridDim.x;
@@ -156,7 +170,7 @@ extern "C" size_t zipml_clip_workspace_bytes(int64_t n_tensors)
 
 static bool clip_tensor_ok(const zipml_clip_tensor &t)
 {
-    return valid_dtype(t.grad_dtype) && valid_dtype(t.out_dtype) && t.count >= 0 && t.count <= (1ll << 34) &&
+    return valid_dtype(t.grad_dtype) && valid_dtype(t.out_dtype) && t.count >= 0 && t.count <= kClipMost &&
            (!t.count || (t.grad_dev && (t.out_dev != t.grad_dev || t.out_dtype == t.grad_dtype)));
 }
 static bool aligned_as(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype_bytes(dtype) - 1)) == 0; }
@@ -191,7 +205,9 @@ extern "C" int zipml_clip(void *stream, const zipml_clip_tensor *tensors_host, i
             bool writes = i0 == 0;         // (the first launch of the second pass hands the norm on)
             for (int k = 0; k < a.n; ++k) {
                 const zipml_clip_tensor &t = tensors_host[i0 + k];
-                a.t[k] = ClipTensor{t.grad_dev, t.out_dev, t.count, a.chunks, (t.grad_dtype == ZIPML_BF16 ? 1u : 0u) | (t.out_dtype == ZIPML_BF16 ? 2u : 0u)};
+                a.t[k] = ClipTensor{t.grad_dev, t.out_dev, (uint32_t)t.count,
+                                    a.chunks | (t.grad_dtype == ZIPML_BF16 ? 1u << 28 : 0u) | (t.out_dtype == ZIPML_BF16 ? 1u << 29 : 0u) |
+                                        (uint32_t)(t.count >> 32) << 30};
                 a.chunks += (uint32_t)((t.count + chunk - 1) / chunk);
                 writes |= t.out_dev != nullptr;
             }

@@ -82,9 +82,11 @@ def test_in_place_and_without_output(max_norm):
 
 
 @pytest.mark.gpu
-def test_more_tensors_than_a_launch_takes():
-    sizes = [(37 * k) % 5000 for k in range(300)]
-    grads = gradients(sizes, [F32 if k % 3 else BF16 for k in range(300)], 4)
+@pytest.mark.parametrize("n", [64, 65, 128, 129, 160, 161, 500])
+def test_many_tensors(n):
+    """As many as the lanes of a wave, as a launch takes, and more."""
+    sizes = [(37 * k) % 5000 for k in range(n)]
+    grads = gradients(sizes, [F32 if k % 3 else BF16 for k in range(n)], 4)
     bucket = torch.empty(sum(sizes), dtype=BF16, device=DEV)
     check(grads, list(bucket.split(sizes)), 1.0)
 
@@ -94,6 +96,20 @@ def test_many_values():
     """More chunks than workgroups."""
     grads = gradients([9_000_001, 5, 4_000_000], [F32, BF16, BF16], 5)
     check(grads, [torch.empty_like(t, dtype=F32) for t in grads], 1.0)
+
+
+@pytest.mark.gpu
+def test_a_tensor_of_more_than_2_to_the_32_values():
+    """Offsets and chunks past 32 bits: the bits of values at its end, and the norm (all squares are 1/4: exact)."""
+    n = (1 << 32) + 5000
+    big, out = torch.full((n,), 0.5, dtype=BF16, device=DEV), torch.empty(n, dtype=BF16, device=DEV)
+    big[-3:] = 2.0
+    norm, factor = clipped([torch.ones(7, device=DEV), big], [None, out], 256.0)
+    want = math.sqrt(7 + (n - 3) / 4 + 12)
+    assert abs(norm - want) <= 2.0 ** -24 * want and abs(factor - 256.0 / want) <= 2.0 ** -23 * factor
+    ends = torch.cat([out[:4], out[(1 << 32) - 4:(1 << 32) + 4], out[-4:]]).float().cpu()
+    small, large = (float(torch.tensor(v * factor, dtype=F32).to(BF16)) for v in (0.5, 2.0))
+    assert ends.tolist() == [small] * 13 + [large] * 3
 
 
 @pytest.mark.gpu
@@ -153,7 +169,7 @@ def test_refusals(lib):
     ok = entry()
     for kw in ({"n": 0}, {"n": -1}, {"n": (1 << 20) + 1}, {"tensors": False}, {"max_norm": -1.0}, {"max_norm": float("nan")}, {"norm": None}):
         assert call(ok, **kw) == zipml.EINVAL, kw
-    for bad in (entry(gd=2), entry(od=-1), entry(count=-1), entry(count=(1 << 34) + 1), entry(grad=None), entry(od=zipml.BF16)):
+    for bad in (entry(gd=2), entry(od=-1), entry(count=-1), entry(count=(1 << 33) + 1), entry(grad=None), entry(od=zipml.BF16)):
         assert call(ok, bad) == zipml.EINVAL
     assert call(ok, ws=None) == call(ok, size=zipml.clip_workspace_bytes(1) - 1) == zipml.EWORKSPACE
     assert call(ok, entry(grad=ODD)) == call(ok, entry(out=ODD)) == zipml.EALIGN
