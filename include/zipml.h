@@ -405,11 +405,12 @@ int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, const float
                        int dtype, int64_t ldy, void *workspace_dev, size_t workspace_bytes);
 
 /* Root-mean-square norm of a residual stream:
- *   r = x + add rounded to dtype (x alone without add_dev),  rstd = 1 / sqrt(mean r^2 + eps),  v = (r * rstd) * gain,
+ *   r = x + add, formed in fp32 and rounded to dtype (x alone without add_dev),  rstd = 1 / sqrt(mean r^2 + eps),  v = (r * rstd) * gain,
  * row by row; mean and root in 64 bits, rstd rounded to fp32 once.  Outputs, each of them optional but one of the first two:
  * y_dev, v rounded to dtype; codes_dev with scales_dev, v as 8-bit codes (ZIPML_NEAREST); sum_dev, r (for the next block's residual
  * and the backward pass); rstd_dev, fp32 [rows] (for the backward pass).  x, add, sum, y: dtype, rows ld* >= cols apart, each one's
- * leading dimension ignored where it is NULL; gain_dev: fp32 [cols], NULL for ones; eps finite and not negative.  sum_dev or y_dev
+ * leading dimension ignored where it is NULL; gain_dev: fp32 [cols], NULL for ones; eps finite and not negative
+ * (with 0 a row of zeros gives NaN, as the formula has it).  sum_dev or y_dev
  * may be x_dev or add_dev themselves (with the same leading dimension); otherwise outputs must not overlap inputs. */
 int zipml_norm_forward(void *stream, const void *x_dev, int64_t ldx, const void *add_dev, int64_t ldadd, int dtype, int64_t rows,
                        int64_t cols, const float *gain_dev, float eps, void *sum_dev, int64_t ldsum, void *y_dev, int64_t ldy,

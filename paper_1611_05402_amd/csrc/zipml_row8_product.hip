@@ -6,9 +6,9 @@
 //
 // Two kinds of kernels, chosen by a model of their times (product_plan): few tokens or outputs are bound by the bytes of W and by latency
 // (one token, 4,096 x 4,096: 5.4 us, 3.4 at the rate of a copy, 1.4 an empty launch; 64 tokens, 8,192 -> 1,024: 6.0; 1,000 tokens,
-// 520 -> 1,001, fp32: 5.9), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 227 us in a long run,
-// 2,420 TOP/s, 178 on zeros with the larger instructions; a library product of the same codes without scales 288; 4,096 tokens, 16,384 ->
-// 4,096: 211 us, 2,600 TOP/s, the library 217).  Of the 227 us some 35 are the results' way out, 134 MB.
+// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 224 us in a long run, to 235
+// on another box, 2,460 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 212 us,
+// 2,590 TOP/s, the library 217).  Of the 224 us some 35 are the results' way out, 134 MB.
 #include "zipml_row8.h"
 
 namespace zipml {
