@@ -231,7 +231,8 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 
     // While a round is multiplied, the next one goes from registers to LDS, and each register is loaded anew for the one after it.  A
     // beat's rows of W are read two beats ahead, all of its tokens' codes in the two beats before their first; so the barrier stands
-    // two beats before the round's end.  Beats are kept apart: the compiler otherwise moves all loads to a round's end.
+    // two beats before the round's end.  What a beat reads, stores and loads stands between its products, in this order (216 us in place of
+    // 220 for 16,384 tokens, 4,096 x 4,096, with all of it before them); the compiler otherwise moves all loads to a round's end.
     i32x4 fw[4], fx[2][S::TT];
     auto read_w = [&](const char *stage, int beat) {
         const int m = beat % S::TO, s = beat / S::TO;
@@ -263,21 +264,27 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 #pragma unroll
         for (int beat = 0; beat < S::kBeats; ++beat) {
             const int ahead = beat + 2;
-            if (ahead == S::kBeats) lds_barrier();
-            // (the tokens' codes of the next 64 go with the first two rows of W that need them)
-            if (ahead % S::TO < 2) read_x(ahead < S::kBeats ? here : next, ahead / S::TO & 1, ahead % S::TO);
-            read_w(ahead < S::kBeats ? here : next, ahead % S::kBeats);
 #pragma unroll
-            for (int q = 0; q < S::kLoads; ++q)
-                if (q * (S::kBeats - 2) / S::kLoads == beat) {
-                    store(v[q], next, q);
-                    v[q] = load(k0 + 2 * kStep, q);
-                }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int n = 0; n < S::TT; ++n)
+            for (int n = 0; n < S::TT; ++n) {
                 acc[beat % S::TO][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[beat & 3], fx[beat / S::TO][n], acc[beat % S::TO][n], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (n == 0) {
+                    if (ahead == S::kBeats) lds_barrier();
+                    read_w(ahead < S::kBeats ? here : next, ahead % S::kBeats);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (n == S::TT / 4 && ahead % S::TO < 2) {
+                    read_x(ahead < S::kBeats ? here : next, ahead / S::TO & 1, ahead % S::TO);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int q = 0; q < S::kLoads; ++q)
+                    if (q * (S::kBeats - 2) / S::kLoads == beat) {
+                        if (n == S::TT / 2) store(v[q], next, q);
+                        if (n == S::TT * 3 / 4) v[q] = load(k0 + 2 * kStep, q);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
         }
         char *const t = here;
         here = next;
