@@ -6,9 +6,9 @@
 //
 // Two kinds of kernels, chosen by a model of their times (product_plan): few tokens or outputs are bound by the bytes of W and by latency
 // (one token, 4,096 x 4,096: 5.4 us, 3.4 at the rate of a copy, 1.4 an empty launch; 64 tokens, 8,192 -> 1,024: 6.0; 1,000 tokens,
-// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 224 us in a long run, to 235
-// on another box, 2,460 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 212 us,
-// 2,590 TOP/s, the library 217).  Of the 224 us some 35 are the results' way out, 134 MB.
+// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 210 us in a long run,
+// 2,620 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 202 us, 2,720 TOP/s, the library
+// 217).  With the first, 134 MB of results go out.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -33,12 +33,14 @@ struct ProductArgs {
 // against 233, 8,192 x 4,096 and 520 inputs 32 against 34 (54 against 56); 4,096 x 4,096 is slower to read next (30 against 28.7 for both).
 // Rows that share lines need the caches to put these together: 10,022 x 8,825, 112 inputs, 142 us past them and 74 through them.
 constexpr int64_t kThroughLeast = 48ll << 20;
+constexpr int kComputeUnits = 256;
 constexpr int kStep = 128;      // codes of a row that are in LDS at a time (2^7)
 
 // Rows of codes as a buffer: rows behind the last one, and what lies behind a row's padding, read as zeros.
 struct CodeRows {
     __amdgpu_buffer_rsrc_t r;
     int ld, bytes;
+    CodeRows() = default;
     __device__ __forceinline__ CodeRows(const uint8_t *base, int64_t left, int64_t ld_, int bytes_) : ld((int)ld_), bytes(bytes_)
     {
         const int64_t n = (left - 1) * ld_ + bytes_;
@@ -122,7 +124,8 @@ struct ProductShape {
     static constexpr bool kParts = std::is_same<T, int>::value;     // sums of a range of the contraction, not results
     static constexpr int HO = 8 / (int)sizeof(T);                   // tiles side by side in a line of 128 bytes of results
     static constexpr int kOut = 32 * 128;                           // LDS of a wave's results on their way out: 32 tokens
-    static constexpr int kLds = 2 * kStage > kOut * WO * WT ? 2 * kStage : kOut * WO * WT;
+    static constexpr bool kStay = MO * MT == 256 * 256;
+    static constexpr int kLds = kStay ? 2 * kStage + kOut * WO * WT : 2 * kStage > kOut * WO * WT ? 2 * kStage : kOut * WO * WT;
     static_assert(kLoadsW * 16 * kThreads == MO * kStep && kLoadsX * 16 * kThreads == MT * kStep, "whole loads");
     static_assert(TO % HO == 0 && TT % 2 == 0 && kBeats % 4 == 0 && kLoads <= kBeats - 2, "beats");
     static_assert(kLds <= 160 * 1024, "LDS");
@@ -143,18 +146,12 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
         const int64_t t = t_wave + n * 16 + (lane & 15);
         sx[n] = a.sx[t < a.rows ? t : a.rows - 1];
     }
-    // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256; -0 leaves every value as it is)
-    f32x4 sw[S::TO], bias[S::TO];
+    // (all at once: a load at each use waited for the one before, 15 us a tile of 256 x 256)
+    f32x4 sw[S::TO];
     const int at = (o_wave + 4 * (lane >> 4)) * 4;
 #pragma unroll
-    for (int m = 0; m < S::TO && !S::kParts; ++m) {
+    for (int m = 0; m < S::TO && !S::kParts; ++m)
         sw[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at + m * 64, 0, 0));
-        bias[m] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
-    }
-    if (a.bias)
-#pragma unroll
-        for (int m = 0; m < S::TO && !S::kParts; ++m)
-            bias[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at + m * 64, 0, 0));
     // (a token's lines one after the other: rows that do not begin at a line's start share lines, which the L2 has to put together)
 #pragma unroll
     for (int n0 = 0; n0 < S::TT; n0 += 2) {
@@ -162,6 +159,13 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
         for (int m0 = 0; m0 < S::TO; m0 += S::HO) {
             constexpr int V = 16 / (int)sizeof(T);                  // results in 16 bytes
             const int o = o_wave + m0 * 16 + (lane & 7) * V, left = a.d_out - o;
+            f32x4 bias[S::HO];                                      // (-0 leaves every value as it is)
+#pragma unroll
+            for (int m = 0; m < S::HO; ++m) bias[m] = f32x4{-0.0f, -0.0f, -0.0f, -0.0f};
+            if (a.bias && !S::kParts)
+#pragma unroll
+                for (int m = 0; m < S::HO; ++m)
+                    bias[m] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, at + (m0 + m) * 64, 0, 0));
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -172,7 +176,7 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
                     for (int k = 0; k < 4; ++k) {
                         const int sum = acc[m0 + m][n0 + n][k];
                         if constexpr (S::kParts) r[k] = sum;
-                        else r[k] = (T)((float)sum * sx[n0 + n] * sw[m0 + m][k] + bias[m0 + m][k]);
+                        else r[k] = (T)((float)sum * sx[n0 + n] * sw[m0 + m][k] + bias[m][k]);
                     }
                     const int row = n * 16 + (lane & 15), byte = (m * 16 + 4 * (lane >> 4)) * (int)sizeof(T);
                     *reinterpret_cast<T4 *>(out + lds_at(row, byte >> 4) + (byte & 15)) = r;
@@ -204,25 +208,57 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
 }
 
 // THROUGH: results are written past the caches (a kernel of its own: of a branch the compiler makes one store, which is not).
+// Where one workgroup fills a compute unit (S::kStay) it stays and takes every gridDim.x-th piece of work: the first two rounds of the next
+// are under way during the last two of the one before and while its results are written (16,384 tokens, 520 -> 4,096: 61 -> 56 us).
 template <typename T, typename S, bool THROUGH>
 __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wo = wave / S::WT, wt = wave % S::WT;
-    int tile_o, tile_t;
-    const uint32_t tiles = (uint32_t)a.tiles_o * a.tiles_t, split = blockIdx.x / tiles;
-    tile_of(a, tiles, blockIdx.x - split * tiles, tile_o, tile_t);
-    const int k_begin = (int)split * a.range, k_end = k_begin + a.range < a.bytes ? k_begin + a.range : a.bytes;
-    const int o0 = tile_o * S::MO;
-    const int64_t t0 = (int64_t)tile_t * S::MT;
-    const CodeRows w(a.w + o0 * a.ldw, a.d_out - o0, a.ldw, a.bytes), x(a.x + t0 * a.ldx, a.rows - t0, a.ldx, a.bytes);
+    const uint32_t tiles = (uint32_t)a.tiles_o * a.tiles_t, work = tiles * a.ranges;
+    // where a piece of work (a tile, a range of its contraction) lies
+    struct Place {
+        int o0, k_begin, k_end;
+        int64_t t0;
+        uint32_t split;
+    };
+    auto place = [&](uint32_t at) {
+        Place p;
+        int tile_o, tile_t;
+        p.split = at / tiles;
+        tile_of(a, tiles, at - p.split * tiles, tile_o, tile_t);
+        p.o0 = tile_o * S::MO;
+        p.t0 = (int64_t)tile_t * S::MT;
+        p.k_begin = (int)p.split * a.range;
+        p.k_end = p.k_begin + a.range < a.bytes ? p.k_begin + a.range : a.bytes;
+        return p;
+    };
 
+    // What is loaded next: 128 codes from k_load on of these rows.
     constexpr int kRowsLoad = S::kThreads / 8;                      // rows that one load of all threads takes
     const int at_w = (tid >> 3) * (int)a.ldw + (tid & 7) * 16, at_x = (tid >> 3) * (int)a.ldx + (tid & 7) * 16;
-    auto load = [&](int k0, int q) {
-        const bool there = k0 + (tid & 7) * 16 < a.bytes;
-        return q < S::kLoadsW ? w.load16(there, at_w + k0, q * kRowsLoad) : x.load16(there, at_x + k0, (q - S::kLoadsW) * kRowsLoad);
+    CodeRows w, x;
+    uint32_t load_at = blockIdx.x;
+    int k_load = 0, k_stop = 0;
+    auto take = [&]() {
+        const bool there = load_at < work;
+        const Place p = place(there ? load_at : 0);
+        w = CodeRows(a.w + p.o0 * a.ldw, there ? a.d_out - p.o0 : 0, a.ldw, a.bytes);
+        x = CodeRows(a.x + p.t0 * a.ldx, there ? a.rows - p.t0 : 0, a.ldx, a.bytes);
+        k_load = p.k_begin;
+        k_stop = p.k_end;
+    };
+    auto loaded = [&]() {
+        k_load += kStep;
+        if (S::kStay && k_load >= k_stop) {
+            load_at += gridDim.x;
+            take();
+        }
+    };
+    auto load = [&](int q) {
+        const bool there = k_load + (tid & 7) * 16 < a.bytes;
+        return q < S::kLoadsW ? w.load16(there, at_w + k_load, q * kRowsLoad) : x.load16(there, at_x + k_load, (q - S::kLoadsW) * kRowsLoad);
     };
     auto store = [&](u32x4 v, char *stage, int q) {
         const int c = tid + (q < S::kLoadsW ? q : q - S::kLoadsW) * S::kThreads;
@@ -245,53 +281,61 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
     };
     char *here = lds, *next = lds + S::kStage;
     u32x4 v[S::kLoads];
+    take();
     {                                      // both first rounds asked for at once: the memory's latency once, not twice
         u32x4 first[S::kLoads];
 #pragma unroll
-        for (int q = 0; q < S::kLoads; ++q) first[q] = load(k_begin, q);
+        for (int q = 0; q < S::kLoads; ++q) first[q] = load(q);
+        loaded();
 #pragma unroll
-        for (int q = 0; q < S::kLoads; ++q) v[q] = load(k_begin + kStep, q);
+        for (int q = 0; q < S::kLoads; ++q) v[q] = load(q);
+        loaded();
 #pragma unroll
         for (int q = 0; q < S::kLoads; ++q) store(first[q], here, q);
     }
-    i32x4 acc[S::TO][S::TT] = {};
     lds_barrier();
-    read_x(here, 0, 0);
-    read_w(here, 0);
-    read_x(here, 0, 1);
-    read_w(here, 1);
-    for (int k0 = k_begin; k0 < k_end; k0 += kStep) {
+    for (uint32_t at = blockIdx.x; at < work; at += gridDim.x) {
+        const Place p = place(at);
+        i32x4 acc[S::TO][S::TT] = {};
+        read_x(here, 0, 0);
+        read_w(here, 0);
+        read_x(here, 0, 1);
+        read_w(here, 1);
+        for (int k0 = p.k_begin; k0 < p.k_end; k0 += kStep) {
 #pragma unroll
-        for (int beat = 0; beat < S::kBeats; ++beat) {
-            const int ahead = beat + 2;
+            for (int beat = 0; beat < S::kBeats; ++beat) {
+                const int ahead = beat + 2;
 #pragma unroll
-            for (int n = 0; n < S::TT; ++n) {
-                acc[beat % S::TO][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[beat & 3], fx[beat / S::TO][n], acc[beat % S::TO][n], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                if (n == 0) {
-                    if (ahead == S::kBeats) lds_barrier();
-                    read_w(ahead < S::kBeats ? here : next, ahead % S::kBeats);
+                for (int n = 0; n < S::TT; ++n) {
+                    acc[beat % S::TO][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[beat & 3], fx[beat / S::TO][n], acc[beat % S::TO][n], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
-                }
-                if (n == S::TT / 4 && ahead % S::TO < 2) {
-                    read_x(ahead < S::kBeats ? here : next, ahead / S::TO & 1, ahead % S::TO);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-#pragma unroll
-                for (int q = 0; q < S::kLoads; ++q)
-                    if (q * (S::kBeats - 2) / S::kLoads == beat) {
-                        if (n == S::TT / 2) store(v[q], next, q);
-                        if (n == S::TT * 3 / 4) v[q] = load(k0 + 2 * kStep, q);
+                    if (n == 0) {
+                        if (ahead == S::kBeats) lds_barrier();
+                        read_w(ahead < S::kBeats ? here : next, ahead % S::kBeats);
                         __builtin_amdgcn_sched_barrier(0);
                     }
+                    if (n == S::TT / 4 && ahead % S::TO < 2) {
+                        read_x(ahead < S::kBeats ? here : next, ahead / S::TO & 1, ahead % S::TO);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int q = 0; q < S::kLoads; ++q)
+                        if (q * (S::kBeats - 2) / S::kLoads == beat) {
+                            if (n == S::TT / 2) store(v[q], next, q);
+                            if (n == S::TT * 3 / 4) v[q] = load(q);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                }
             }
+            loaded();
+            char *const t = here;
+            here = next;
+            next = t;
         }
-        char *const t = here;
-        here = next;
-        next = t;
+        if (!S::kStay) lds_barrier();          // (the results lie where another wave may still read)
+        write_out<T, S, THROUGH>(a, acc, lds + (S::kStay ? 2 * S::kStage : 0) + wave * S::kOut, p.o0 + wo * S::TO * 16, p.t0 + wt * S::TT * 16, p.split);
+        if (!S::kStay) return;
     }
-    lds_barrier();                         // (the results may lie where another wave still reads)
-    write_out<T, S, THROUGH>(a, acc, lds + wave * S::kOut, o0 + wo * S::TO * 16, t0 + wt * S::TT * 16, split);
 }
 
 // ---- few tokens, few outputs: the waves of a workgroup share the contraction -------------------
@@ -309,6 +353,7 @@ struct SplitShape {
     static constexpr int kSums = MT * kRow * 4;
     static constexpr int kWave = kStage > kSums ? kStage : kSums; // LDS of a wave
     static constexpr int kLds = kWave * WAVES;
+    static constexpr bool kStay = false;
     static_assert(kSmall ? MT == 16 : MO % 32 == 0 && MT % 32 == 0, "tile");
     static_assert(kLds <= 160 * 1024, "LDS");
 };
@@ -426,7 +471,7 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 // along each).
 #define ZIPML_PRODUCT_SPLIT(F)                                                                                                  \
     F(0, 16, 16, 4) F(1, 16, 16, 8) F(2, 16, 16, 16) F(3, 32, 32, 4) F(4, 32, 32, 8) F(5, 32, 32, 16) F(6, 64, 32, 8) F(7, 64, 64, 8)
-#define ZIPML_PRODUCT_TILE(F) F(8, 128, 64, 2, 2) F(9, 128, 128, 2, 4) F(10, 256, 256, 2, 4) 
+#define ZIPML_PRODUCT_TILE(F) F(8, 128, 64, 2, 2) F(9, 128, 128, 2, 4) F(10, 256, 256, 2, 4)
 
 // Which shape, and (of the second kind) in how many ranges the contraction is taken, whose sums a second launch joins: the least of
 //   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
@@ -483,7 +528,7 @@ static int launch_tiles(hipStream_t s, ProductArgs a, K k)
     a.tiles_t = (int)tiles;
     static std::atomic<uint64_t> done[2];
     if (allow_lds((const void *)k, S::kLds, done[a.through])) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3((uint32_t)all), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL(k, dim3((uint32_t)(S::kStay && all > kComputeUnits ? kComputeUnits : all)), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
 

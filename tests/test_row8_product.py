@@ -138,6 +138,14 @@ def test_results_larger_than_the_caches(rows, d_out, d_in, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d_out,d_in", [(4400, 4100, 520), (4864, 3841, 1111), (4097, 8192, 128)])
+def test_more_tiles_than_compute_units(rows, d_out, d_in, kind):
+    """Tiles of several rounds that follow one another in a workgroup, the last of them partly outside."""
+    same(rows, d_out, d_in, kind)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,d_out,d_in", [(1, 520, 4096), (30, 64, 30000), (500, 700, 300)])
 def test_two_streams_at_once_and_a_graph(rows, d_out, d_in):
     """Each stream with its own workspace; a captured call replayed over other inputs, with eager work between the replays."""
