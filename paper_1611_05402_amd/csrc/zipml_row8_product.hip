@@ -6,9 +6,9 @@
 //
 // Two kinds of kernels, chosen by a model of their times (product_plan): few tokens or outputs are bound by the bytes of W and by latency
 // (one token, 4,096 x 4,096: 5.4 us, 3.4 at the rate of a copy, 1.4 an empty launch; 64 tokens, 8,192 -> 1,024: 6.0; 1,000 tokens,
-// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 210 us in a long run,
-// 2,620 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 202 us, 2,720 TOP/s, the library
-// 217).  With the first, 134 MB of results go out.
+// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 210 us in a long run, to
+// 216 on another box, 2,620 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 202 us,
+// 2,720 TOP/s, the library 217).  With the first, 134 MB of results go out.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -210,8 +210,10 @@ __device__ __forceinline__ void write_out(const ProductArgs &a, const i32x4 (&ac
 // THROUGH: results are written past the caches (a kernel of its own: of a branch the compiler makes one store, which is not).
 // Where one workgroup fills a compute unit (S::kStay) it stays and takes every gridDim.x-th piece of work: the first two rounds of the next
 // are under way during the last two of the one before and while its results are written (16,384 tokens, 520 -> 4,096: 61 -> 56 us).
+// (Two waves a SIMD at least: with all 512 registers to itself a wave of 128 x 64 keeps its sums in the upper half and moves them in each
+// round, 1,024 tokens, 4,096 -> 2,048: 19.7 us in place of 15.6.)
 template <typename T, typename S, bool THROUGH>
-__global__ __launch_bounds__(S::kThreads) void k_row8_product(ProductArgs a)
+__global__ __launch_bounds__(S::kThreads, 2) void k_row8_product(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 //   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
 //   them: k * shared) + (ranges > 1: a launch, sums written and read).
 // The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
-// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 28 % at most.
+// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, a third at most.
 struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
