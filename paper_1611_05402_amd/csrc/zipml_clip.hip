@@ -3,7 +3,7 @@
 //   norm = sqrt(sum g^2) over all tensors, factor = norm <= max_norm ? 1 : max_norm / norm, out = round(factor g)
 //
 // Two passes over the gradients, each one launch for kClipTensors of them: the first leaves one sum a workgroup, the second adds
-// these up (every workgroup for itself, in the same order) and scales.  Squares are summed in 64 bits, so that no gradient that
+// these up (every workgroup for itself, in the same order, unless they are many) and scales.  Squares are summed in 64 bits, so that no gradient that
 // fp32 holds overflows and the norm does not depend on the order.  The second pass goes from the last chunk to the first: what the
 // first pass has read last is still in the caches, and results are written past them.  302 million fp32 values into a bf16 bucket: 193 us
 // for 1.2 GB, then 327 for 1.8 GB (6.2 and 5.5 TB/s, part of it out of the caches); in one pass over the gradients, which no cache holds,
@@ -17,6 +17,9 @@ constexpr int kClipGroups = 1024;         // workgroups of a launch
 // Units of eight values that a thread has under way: four, or one where chunks of four would leave compute units idle (1.6 million
 // values: 8.6 us in both launches, 9.6 with four and with the tensors searched for in the arguments).
 constexpr int kClipMany = 4, kClipFew = 1;
+// More sums than these are joined once, by a launch of its own, not by each workgroup (tensors of 20,000 values: 320 of them, 2,048 sums, 24 us
+// and 26 with such a launch, 480 37 and 33, 4,000 592 and 298).
+constexpr int kClipParts = 2048;
 constexpr int64_t clip_chunk(int units) { return 256 * 8 * units; }
 
 constexpr int64_t kClipMost = 1ll << 33;  // values of a tensor: 160 of them are fewer than 2^28 chunks
@@ -158,6 +161,17 @@ __global__ __launch_bounds__(256) void k_clip_scale(ClipArgs a, const double *pa
     }
 }
 
+// All sums into the first of them, by one workgroup.
+__global__ __launch_bounds__(1024) void k_clip_join(double *part, int parts)
+{
+    __shared__ double scratch[16];
+    double sum = 0;
+#pragma unroll 8
+    for (int p = threadIdx.x; p < parts; p += 1024) sum += part[p];
+    sum = team_sum<1024>(sum, scratch);    // (its barrier stands between the last read and the write)
+    if (threadIdx.x == 0) part[0] = sum;
+}
+
 }  // namespace zipml
 
 using namespace zipml;
@@ -198,6 +212,11 @@ extern "C" int zipml_clip(void *stream, const zipml_clip_tensor *tensors_host, i
     double *part = (double *)workspace_dev;
     int parts = 0;
     for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 1 && parts > kClipParts) {
+            hipLaunchKernelGGL(k_clip_join, dim3(1), dim3(1024), 0, s, part, parts);
+            if (const int rc = hip_check(hipGetLastError())) return rc;
+            parts = 1;
+        }
         for (int64_t i0 = 0; i0 < n_tensors; i0 += kClipTensors) {
             ClipArgs a;
             a.n = (int)(n_tensors - i0 < kClipTensors ? n_tensors - i0 : kClipTensors);

@@ -92,6 +92,14 @@ def test_many_tensors(n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,size", [(320, 20001), (330, 20001), (700, 16389), (3001, 300)])
+def test_many_tensors_with_many_sums(n, size):
+    grads = gradients([size - k % 3 for k in range(n)], [F32] * n, seed=n)
+    check(grads, [torch.empty_like(t, dtype=BF16) if k % 7 else None for k, t in enumerate(grads)], 0.5)
+    check(grads, None, 0.5)
+
+
+@pytest.mark.gpu
 def test_many_values():
     """More chunks than workgroups."""
     grads = gradients([9_000_001, 5, 4_000_000], [F32, BF16, BF16], 5)
