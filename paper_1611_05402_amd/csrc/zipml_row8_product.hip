@@ -477,9 +477,11 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 
 // Which shape, and (of the second kind) in how many ranges the contraction is taken, whose sums a second launch joins: the least of
 //   start + further turns of a compute unit * turn + rounds of 128 codes of a wave * (one workgroup on a compute unit: lone, k of
-//   them: k * shared) + (ranges > 1: a launch, sums written and read).
+//   them: k * shared, k the most for the second kind, for the first, which wait for memory that all share, the mean) + (ranges > 1: a
+//   launch, sums written and read).
 // The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
-// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, a third at most.
+// 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 14 % in one of
+// twenty, a third at most (16 ranges, or k the most for both: 18 % in one of twenty).
 struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
@@ -504,13 +506,14 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
         const Cost &c = costs[shape];
         const int64_t tiles = parts(d_out, c.outs) * parts(rows, c.tokens);
         if (tiles > 0x3FFFFFFF || (best.shape >= 0 && c.start + (double)(parts(tiles, 8) - 1) * c.turn >= least)) continue;
-        for (const int wanted : {1, 2, 3, 4, 8, 16}) {
+        for (const int wanted : {1, 2, 3, 4, 8}) {
             // (ranges of two rounds at least, whose sums stay in the caches)
             if (wanted > 1 && (c.waves > 0 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;
             const int64_t range = wanted == 1 ? parts(bytes, 7) << 7 : round_up((bytes + wanted - 1) / wanted, kStep);
             const int64_t ranges = wanted == 1 ? 1 : (bytes + range - 1) / range;
             const double k = (double)parts(tiles * ranges, 8), rounds = (double)parts(range < bytes ? range : bytes, 7 + c.waves);
-            const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && k * c.shared > c.lone ? k * c.shared : c.lone) +
+            const double busy = c.waves > 0 ? (double)tiles * (1.0 / 256) : k;
+            const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && busy * c.shared > c.lone ? busy * c.shared : c.lone) +
                               (ranges > 1 ? 3.0 + (double)(ranges * sums) * 2 / 6.4e6 : 0.0);
             if (best.shape < 0 || us < least) {
                 least = us;
