@@ -469,6 +469,15 @@ int zipml_debug_step(void *stream, const void *packed1_dev, const void *packed2_
                      int32_t *model_codes_dev, int32_t *acc_dev, float *r_dev, float *g_dev,
                      int32_t *grad_codes_dev, void *workspace_dev, size_t workspace_bytes);
 
+/* What zipml_row8_product does for these sizes: its tiles (outputs x tokens, shared by `waves` waves of 64 threads), in how many ranges
+ * it takes the contraction (joined by a second launch), whether results are written past the caches (for y at the start of a line of
+ * 128 bytes), and the workgroups of its (first) launch.  Runs on the host. */
+typedef struct {
+    int32_t outputs, tokens, waves, ranges, past_caches;
+    int64_t workgroups;
+} zipml_product_plan;
+int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, zipml_product_plan *plan_host);
+
 /* A plain streaming pass of known size, for measurements: reads `bytes` bytes (a multiple of 16)
  * at src_dev once, XORs all their 32-bit words into *sink_dev (which the caller clears beforehand)
  * and, if dst_dev is not NULL, also stores them there (a copy).  Asynchronous.  It gives the

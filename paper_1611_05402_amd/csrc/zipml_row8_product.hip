@@ -524,16 +524,23 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
     return best;
 }
 
+// Workgroups that a shape is launched with.
+template <typename S>
+static int64_t product_groups(int64_t rows, int64_t d_out, int ranges)
+{
+    const int64_t all = (rows + S::MT - 1) / S::MT * ((d_out + S::MO - 1) / S::MO) * ranges;
+    return S::kStay && all > kComputeUnits ? kComputeUnits : all;
+}
+
 // (T tells kernels of one shape apart: each is asked for its LDS once)
 template <typename T, typename S, typename K>
 static int launch_tiles(hipStream_t s, ProductArgs a, K k)
 {
     a.tiles_o = (a.d_out + S::MO - 1) / S::MO;
-    const int64_t tiles = (a.rows + S::MT - 1) / S::MT, all = tiles * a.tiles_o * a.ranges;
-    a.tiles_t = (int)tiles;
+    a.tiles_t = (int)((a.rows + S::MT - 1) / S::MT);
     static std::atomic<uint64_t> done[2];
     if (allow_lds((const void *)k, S::kLds, done[a.through])) return ZIPML_ELAUNCH;
-    hipLaunchKernelGGL(k, dim3((uint32_t)(S::kStay && all > kComputeUnits ? kComputeUnits : all)), dim3(S::kThreads), S::kLds, s, a);
+    hipLaunchKernelGGL(k, dim3((uint32_t)product_groups<S>(a.rows, a.d_out, a.ranges)), dim3(S::kThreads), S::kLds, s, a);
     return hip_check(hipGetLastError());
 }
 
@@ -581,6 +588,13 @@ static bool product_sizes_ok(int64_t rows, int64_t d_out, int64_t d_in)
 }
 constexpr int64_t kProductMaxIn = 131071;      // 128 * 128 * d_in < 2^31
 
+// (y's rows begin at lines of 128 bytes where its first one does)
+static bool past_caches(int64_t rows, int64_t d_out, int dtype, int64_t ldy)
+{
+    const int64_t size = (int64_t)dtype_bytes(dtype);
+    return rows * d_out * size > kThroughLeast && ldy * size % 128 == 0;
+}
+
 static size_t product_workspace(const ProductPlan &p) { return p.workspace < 256 ? 256 : p.workspace; }
 
 extern "C" size_t zipml_row8_product_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in)
@@ -604,11 +618,32 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
     if (!aligned16(x_dev) || !aligned16(w_dev) || !aligned16(y_dev) || !aligned16(workspace_dev) || !aligned4(x_scales_dev) ||
         !aligned4(w_scales_dev) || !aligned4(bias_dev))
         return ZIPML_EALIGN;
-    const int64_t size = (int64_t)dtype_bytes(dtype);
-    const int through = rows * d_out * size > kThroughLeast && ldy * size % 128 == 0 && reinterpret_cast<uintptr_t>(y_dev) % 128 == 0;
+    const int through = past_caches(rows, d_out, dtype, ldy) && reinterpret_cast<uintptr_t>(y_dev) % 128 == 0;
     ProductArgs a{(const uint8_t *)x_dev, (const uint8_t *)w_dev, x_scales_dev, w_scales_dev, bias_dev, y_dev, ldx, ldw, ldy, rows,
                   (int)d_out, (int)round_up(d_in, kRow8Unit), 0, 0, 0, 0,
                   through, 0};
     hipStream_t s = entry_stream(stream);
     return dtype == ZIPML_F32 ? launch_product<float>(s, a, p, workspace_dev) : launch_product<__bf16>(s, a, p, workspace_dev);
+}
+
+extern "C" int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, zipml_product_plan *plan_host)
+{
+    if (!plan_host || !valid_dtype(dtype) || !product_sizes_ok(rows, d_out, d_in) || ldy < d_out || ldy > (1ll << 60) / rows) return ZIPML_EINVAL;
+    if (d_in > kProductMaxIn) return ZIPML_ERANGE;
+    const ProductPlan p = product_plan(rows, d_out, d_in);
+    switch (p.shape) {
+#define SPLIT(n, o, t, w) case n: { typedef SplitShape<o, t, w> S; *plan_host = zipml_product_plan{o, t, w, 1, 0, product_groups<S>(rows, d_out, 1)}; break; }
+#define TILE(n, o, t, wo, wt)                                                                                                   \
+    case n: {                                                                                                                   \
+        typedef ProductShape<float, o, t, wo, wt> S;                                                                            \
+        *plan_host = zipml_product_plan{o, t, wo * wt, p.ranges, p.ranges == 1 && past_caches(rows, d_out, dtype, ldy),         \
+                                        product_groups<S>(rows, d_out, p.ranges)};                                              \
+        break;                                                                                                                  \
+    }
+        ZIPML_PRODUCT_SPLIT(SPLIT)
+        ZIPML_PRODUCT_TILE(TILE)
+#undef SPLIT
+#undef TILE
+    }
+    return ZIPML_OK;
 }

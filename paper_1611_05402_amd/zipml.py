@@ -37,7 +37,7 @@ EXPORTS = ["zipml_strerror", "zipml_packed_bytes", "zipml_workspace_bytes", "zip
            "zipml_scan_workspace_bytes", "zipml_scan_forward", "zipml_scan_backward", "zipml_scan_status",
            "zipml_scan_step", "zipml_row8_encode", "zipml_row8_decode", "zipml_row8_product_workspace_bytes",
            "zipml_row8_product", "zipml_norm_forward", "zipml_norm_backward_workspace_bytes", "zipml_norm_backward",
-           "zipml_clip_workspace_bytes", "zipml_clip"]
+           "zipml_clip_workspace_bytes", "zipml_clip", "zipml_debug_product_plan"]
 
 
 class ZipmlError(RuntimeError):
@@ -151,6 +151,8 @@ def lib() -> C.CDLL:
         L.zipml_clip_workspace_bytes.argtypes = [i64]
         L.zipml_clip.restype = i32
         L.zipml_clip.argtypes = [vp, vp, i64, f32, vp, vp, sz]
+        L.zipml_debug_product_plan.restype = i32
+        L.zipml_debug_product_plan.argtypes = [i64, i64, i64, i32, i64, vp]
         _lib = L
     return _lib
 
@@ -538,6 +540,19 @@ def row8_product(x, ldx, x_scales, w, ldw, w_scales, rows, d_out, d_in, y, ldy, 
     _check(lib().zipml_row8_product(_stream(stream), _row(f, "x", x, codes, d), ldx, _floats(f, "x_scales", x_scales, d),
                                     _row(f, "w", w, codes, d), ldw, _floats(f, "w_scales", w_scales, d), _floats(f, "bias", bias, d),
                                     rows, d_out, d_in, _row(f, "y", y, k, d), _CODES[k], ldy, room, size), f)
+
+
+class ProductPlan(C.Structure):
+    """Tiles of outputs x tokens of `waves` waves, ranges of the contraction, results past the caches or not, workgroups."""
+    _fields_ = [("outputs", C.c_int32), ("tokens", C.c_int32), ("waves", C.c_int32), ("ranges", C.c_int32), ("past_caches", C.c_int32),
+                ("workgroups", C.c_int64)]
+
+
+def debug_product_plan(rows, d_out, d_in, dtype=BF16, ldy=None) -> ProductPlan:
+    """What row8_product does for these sizes (rows of y ldy values apart, d_out if none is given)."""
+    plan = ProductPlan()
+    _check(lib().zipml_debug_product_plan(rows, d_out, d_in, dtype, d_out if ldy is None else ldy, C.byref(plan)), "zipml_debug_product_plan")
+    return plan
 
 
 def norm_forward(x, ldx, rows, cols, eps, *, gain=None, add=None, ldadd=0, sum=None, ldsum=0, y=None, ldy=0, codes=None, ldc=0,
