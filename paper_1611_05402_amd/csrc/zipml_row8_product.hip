@@ -505,7 +505,9 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
     for (int shape = 0; shape < (int)(sizeof(costs) / sizeof(costs[0])); ++shape) {
         const Cost &c = costs[shape];
         const int64_t tiles = parts(d_out, c.outs) * parts(rows, c.tokens);
-        if (tiles > 0x3FFFFFFF || (best.shape >= 0 && c.start + (double)(parts(tiles, 8) - 1) * c.turn >= least)) continue;
+        // (a launch has fewer than 2^32 threads; the second kind's tiles are shared by eight waves at most, of the last shape 256 workgroups stay)
+        const bool stays = c.outs == 8;
+        if ((!stays && tiles >= (1ll << 32) >> (6 + (c.waves > 0 ? c.waves : 3))) || (best.shape >= 0 && c.start + (double)(parts(tiles, 8) - 1) * c.turn >= least)) continue;
         for (const int wanted : {1, 2, 3, 4, 8}) {
             // (ranges of two rounds at least, whose sums stay in the caches)
             if (wanted > 1 && (c.waves > 0 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;

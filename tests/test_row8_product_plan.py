@@ -143,3 +143,30 @@ def test_refusals(lib):
     for kw in ({"rows": 0}, {"d_out": 0}, {"d_in": 0}, {"dtype": 2}, {"ldy": 5}, {"ldy": 1 << 60}, {"out": None}, {"d_out": (1 << 24) + 1, "ldy": 1 << 25}):
         assert call(**kw) == zipml.EINVAL, kw
     assert call(d_in=131072) == zipml.ERANGE
+
+
+@pytest.mark.parametrize("rows,d_out,d_in", [(1 << 28, 8, 16), ((1 << 28) - 16, 8, 16), (1 << 27, 8, 600), (1 << 27, 16, 600), (1 << 26, 3, 2000),
+                                             (1 << 31, 1, 1), (1 << 31, 512, 16), ((1 << 31) - 255, 300, 1), (1 << 30, 1024, 100), (1 << 16, 1 << 24, 16),
+                                             (1 << 20, 1 << 20, 131071), (1 << 29, 40, 131071), (7, 1 << 24, 131071), ((1 << 27) + 1, 17, 200)])
+def test_launches_of_all_sizes_fit(lib, rows, d_out, d_in):
+    """A launch holds fewer than 2^32 threads."""
+    p = zipml.debug_product_plan(rows, d_out, d_in)
+    assert 0 < p.workgroups * p.waves * 64 < 1 << 32
+    assert p.ranges == 1 and room(rows, d_out, d_in) == 256
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_of_the_smallest_tiles_holds():
+    """2^28 tokens, all results compared (an elementwise chain of single fp32 operations on exact sums, below 2^24 and so exact in fp32)."""
+    rows, d_out, d_in, piece = 1 << 28, 8, 16, 1 << 24
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randint(-127, 128, (rows // 64, d_in), generator=g, device=DEV, dtype=torch.int8).repeat(64, 1)
+    w = torch.randint(-127, 128, (d_out, d_in), generator=g, device=DEV, dtype=torch.int8)
+    sx, sw = torch.rand(rows, generator=g, device=DEV), torch.rand(d_out, generator=g, device=DEV)
+    y = torch.full((rows + 1, d_out), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(room(rows, d_out, d_in), dtype=torch.uint8, device=DEV)
+    zipml.row8_product(x, d_in, sx, w, d_in, sw, rows, d_out, d_in, y, d_out, ws)
+    for r in range(0, rows, piece):
+        sums = torch.mm(x[r:r + piece].float(), w.float().t().contiguous())
+        assert torch.equal(y[r:r + piece], (sums * sx[r:r + piece, None] * sw).to(torch.bfloat16)), r
+    assert (y[rows] == 7.0).all()
