@@ -306,6 +306,9 @@ __global__ __launch_bounds__(1024) void k_norm_dgain(const float *part, int part
     if (set == 0 && c < cols) dgain[c] = add ? dgain[c] + s : s;
 }
 
+// Columns of a launch of k_norm_dgain, which takes 64 threads a column and holds fewer than 2^32.
+constexpr int64_t kNormColumns = 1ll << 25;
+
 // Workgroups of the backward pass: each one writes a row of sums, 256 MiB of them at most.
 constexpr int64_t kNormGroups = 1024;
 static int64_t norm_groups(int64_t rows, int64_t cols, int64_t rows_group)
@@ -386,8 +389,12 @@ extern "C" int zipml_norm_backward(void *stream, const void *dy_dev, int64_t ldd
         const auto k = dtype == ZIPML_F32 ? k_norm_backward<float, S> : k_norm_backward<__bf16, S>;
         hipLaunchKernelGGL(k, dim3((uint32_t)groups), dim3(S::kThreads), 0, s, a);
         if (const int rc = hip_check(hipGetLastError()); rc || !dgain_dev) return rc;
-        hipLaunchKernelGGL(k_norm_dgain, dim3((uint32_t)(a.pitch / 16)), dim3(1024), 0, s, a.part, (int)groups, a.pitch,
-                           cols, dgain_dev, flags & ZIPML_NORM_ADD ? 1 : 0);
-        return hip_check(hipGetLastError());
+        for (int64_t c = 0; c < cols; c += kNormColumns) {
+            const int64_t n = cols - c < kNormColumns ? cols - c : kNormColumns;
+            hipLaunchKernelGGL(k_norm_dgain, dim3((uint32_t)((n + 15) / 16)), dim3(1024), 0, s, a.part + c, (int)groups, a.pitch, n,
+                               dgain_dev + c, flags & ZIPML_NORM_ADD ? 1 : 0);
+            if (const int rc = hip_check(hipGetLastError())) return rc;
+        }
+        return ZIPML_OK;
     });
 }
