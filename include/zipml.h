@@ -398,7 +398,10 @@ int zipml_row8_decode(void *stream, const void *codes_dev, int64_t ldc, const fl
  * integers), what follows is in fp32 and rounded to dtype once.  x_dev: codes of `rows` tokens, w_dev: of d_out rows of weights,
  * both d_in wide, rows at most 4 MiB apart; bias_dev NULL: none.  d_in up to 131,071 (ZIPML_ERANGE beyond: the sum could leave 32
  * bits), d_out up to 2^24.  A row with a scale of NaN gives NaN.  The same call with rows of a gradient, encoded by draws, and the
- * codes of W^T gives the layer's input gradient, unbiased as those draws are independent of W's codes. */
+ * codes of W^T gives the layer's input gradient, unbiased as those draws are independent of W's codes.
+ * rows up to 2^31, rows * d_out up to 2^40.  Workspace: the bytes with which the call is fastest; they fall and rise with the number of
+ * rows.  256 are enough for every call (ZIPML_EWORKSPACE below): with less than is asked for the contraction is not cut into as many
+ * ranges, which may take longer and changes no bit.  So one workspace may serve calls of any sizes: the largest of theirs is best. */
 size_t zipml_row8_product_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in);
 int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, const float *x_scales_dev, const void *w_dev, int64_t ldw,
                        const float *w_scales_dev, const float *bias_dev, int64_t rows, int64_t d_out, int64_t d_in, void *y_dev,
@@ -469,14 +472,15 @@ int zipml_debug_step(void *stream, const void *packed1_dev, const void *packed2_
                      int32_t *model_codes_dev, int32_t *acc_dev, float *r_dev, float *g_dev,
                      int32_t *grad_codes_dev, void *workspace_dev, size_t workspace_bytes);
 
-/* What zipml_row8_product does for these sizes: its tiles (outputs x tokens, shared by `waves` waves of 64 threads), in how many ranges
+/* What zipml_row8_product does for these sizes and a workspace of this size: its tiles (outputs x tokens, shared by `waves` waves of 64 threads), in how many ranges
  * it takes the contraction (joined by a second launch), whether results are written past the caches (for y at the start of a line of
  * 128 bytes), and the workgroups of its (first) launch.  Runs on the host. */
 typedef struct {
     int32_t outputs, tokens, waves, ranges, past_caches;
     int64_t workgroups;
 } zipml_product_plan;
-int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, zipml_product_plan *plan_host);
+int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, size_t workspace_bytes,
+                             zipml_product_plan *plan_host);
 
 /* A plain streaming pass of known size, for measurements: reads `bytes` bytes (a multiple of 16)
  * at src_dev once, XORs all their 32-bit words into *sink_dev (which the caller clears beforehand)

@@ -486,7 +486,10 @@ struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
 };
-static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
+// room: bytes that the sums of ranges may take.  What is wanted falls and rises with the rows (10,240 -> 2,560: 12 MB at 300 tokens, none at
+// 1,024, 63 MB at 2,048); with less the contraction is taken in fewer ranges, which changes no bit (512 tokens 26 us, with no room at all 38;
+// 195 tokens, 18,880 -> 7,035, 47 and 101).
+static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in, size_t room)
 {
     // outputs, tokens and waves of a tile as powers of two: the choice is made in every call, and divisions are what it would cost
     struct Cost { int outs, tokens, waves; double start, turn, lone, shared; };
@@ -513,6 +516,7 @@ static ProductPlan product_plan(int64_t rows, int64_t d_out, int64_t d_in)
             if (wanted > 1 && (c.waves > 0 || bytes < 2 * wanted * kStep || wanted * sums > (1ll << 28) || wanted * tiles > (1 << 16))) break;
             const int64_t range = wanted == 1 ? parts(bytes, 7) << 7 : round_up((bytes + wanted - 1) / wanted, kStep);
             const int64_t ranges = wanted == 1 ? 1 : (bytes + range - 1) / range;
+            if (ranges > 1 && (size_t)(ranges * sums) > room) break;
             const double k = (double)parts(tiles * ranges, 8), rounds = (double)parts(range < bytes ? range : bytes, 7 + c.waves);
             const double busy = c.waves > 0 ? (double)tiles * (1.0 / 256) : k;
             const double us = c.start + (k - 1) * c.turn + rounds * (k > 1 && busy * c.shared > c.lone ? busy * c.shared : c.lone) +
@@ -597,12 +601,13 @@ static bool past_caches(int64_t rows, int64_t d_out, int dtype, int64_t ldy)
     return rows * d_out * size > kThroughLeast && ldy * size % 128 == 0;
 }
 
-static size_t product_workspace(const ProductPlan &p) { return p.workspace < 256 ? 256 : p.workspace; }
+constexpr size_t kProductRoom = 256;           // the least workspace
+static size_t product_workspace(const ProductPlan &p) { return p.workspace < kProductRoom ? kProductRoom : p.workspace; }
 
 extern "C" size_t zipml_row8_product_workspace_bytes(int64_t rows, int64_t d_out, int64_t d_in)
 {
     if (!product_sizes_ok(rows, d_out, d_in) || d_in > kProductMaxIn) return 0;
-    return product_workspace(product_plan(rows, d_out, d_in));
+    return product_workspace(product_plan(rows, d_out, d_in, SIZE_MAX));
 }
 
 extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, const float *x_scales_dev, const void *w_dev,
@@ -615,8 +620,8 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
         ldy < d_out || ldy > (1ll << 60) / rows)
         return ZIPML_EINVAL;
     if (d_in > kProductMaxIn) return ZIPML_ERANGE;
-    const ProductPlan p = product_plan(rows, d_out, d_in);
-    if (!workspace_dev || workspace_bytes < product_workspace(p)) return ZIPML_EWORKSPACE;
+    if (!workspace_dev || workspace_bytes < kProductRoom) return ZIPML_EWORKSPACE;
+    const ProductPlan p = product_plan(rows, d_out, d_in, workspace_bytes);
     if (!aligned16(x_dev) || !aligned16(w_dev) || !aligned16(y_dev) || !aligned16(workspace_dev) || !aligned4(x_scales_dev) ||
         !aligned4(w_scales_dev) || !aligned4(bias_dev))
         return ZIPML_EALIGN;
@@ -628,11 +633,13 @@ extern "C" int zipml_row8_product(void *stream, const void *x_dev, int64_t ldx, 
     return dtype == ZIPML_F32 ? launch_product<float>(s, a, p, workspace_dev) : launch_product<__bf16>(s, a, p, workspace_dev);
 }
 
-extern "C" int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, zipml_product_plan *plan_host)
+extern "C" int zipml_debug_product_plan(int64_t rows, int64_t d_out, int64_t d_in, int dtype, int64_t ldy, size_t workspace_bytes,
+                                        zipml_product_plan *plan_host)
 {
     if (!plan_host || !valid_dtype(dtype) || !product_sizes_ok(rows, d_out, d_in) || ldy < d_out || ldy > (1ll << 60) / rows) return ZIPML_EINVAL;
     if (d_in > kProductMaxIn) return ZIPML_ERANGE;
-    const ProductPlan p = product_plan(rows, d_out, d_in);
+    if (workspace_bytes < kProductRoom) return ZIPML_EWORKSPACE;
+    const ProductPlan p = product_plan(rows, d_out, d_in, workspace_bytes);
     switch (p.shape) {
 #define SPLIT(n, o, t, w) case n: { typedef SplitShape<o, t, w> S; *plan_host = zipml_product_plan{o, t, w, 1, 0, product_groups<S>(rows, d_out, 1)}; break; }
 #define TILE(n, o, t, wo, wt)                                                                                                   \

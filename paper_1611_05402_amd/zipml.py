@@ -152,7 +152,7 @@ def lib() -> C.CDLL:
         L.zipml_clip.restype = i32
         L.zipml_clip.argtypes = [vp, vp, i64, f32, vp, vp, sz]
         L.zipml_debug_product_plan.restype = i32
-        L.zipml_debug_product_plan.argtypes = [i64, i64, i64, i32, i64, vp]
+        L.zipml_debug_product_plan.argtypes = [i64, i64, i64, i32, i64, sz, vp]
         _lib = L
     return _lib
 
@@ -534,7 +534,8 @@ def row8_product_workspace_bytes(rows: int, d_out: int, d_in: int) -> int:
 
 
 def row8_product(x, ldx, x_scales, w, ldw, w_scales, rows, d_out, d_in, y, ldy, workspace, *, bias=None, stream=None):
-    """y (fp32 or bf16) = x w^T from codes of tokens and of weights, with their scales (fp32) and a bias (fp32)."""
+    """y (fp32 or bf16) = x w^T from codes of tokens and of weights, with their scales (fp32) and a bias (fp32).  The workspace may be that of
+    other sizes: with less than row8_product_workspace_bytes asks for (256 bytes at least) the call may take longer, with the same bits."""
     f, d, k, codes = "zipml_row8_product", _here(), y.dtype, _KINDS["int8"]
     room, size = _room(f, workspace, d)
     _check(lib().zipml_row8_product(_stream(stream), _row(f, "x", x, codes, d), ldx, _floats(f, "x_scales", x_scales, d),
@@ -548,10 +549,12 @@ class ProductPlan(C.Structure):
                 ("workgroups", C.c_int64)]
 
 
-def debug_product_plan(rows, d_out, d_in, dtype=BF16, ldy=None) -> ProductPlan:
-    """What row8_product does for these sizes (rows of y ldy values apart, d_out if none is given)."""
+def debug_product_plan(rows, d_out, d_in, dtype=BF16, ldy=None, workspace_bytes=None) -> ProductPlan:
+    """What row8_product does for these sizes (rows of y ldy values apart, d_out if none is given) with a workspace of so many bytes (of
+    those that it asks for if none are given)."""
     plan = ProductPlan()
-    _check(lib().zipml_debug_product_plan(rows, d_out, d_in, dtype, d_out if ldy is None else ldy, C.byref(plan)), "zipml_debug_product_plan")
+    _check(lib().zipml_debug_product_plan(rows, d_out, d_in, dtype, d_out if ldy is None else ldy,
+                                          (1 << 63) if workspace_bytes is None else workspace_bytes, C.byref(plan)), "zipml_debug_product_plan")
     return plan
 
 

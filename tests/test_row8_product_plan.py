@@ -137,12 +137,13 @@ def test_ranges_on_two_streams_and_in_two_graphs(sizes):
 def test_refusals(lib):
     plan = zipml.ProductPlan()
 
-    def call(rows=4, d_out=6, d_in=40, dtype=zipml.F32, ldy=6, out=C.byref(plan)):
-        return lib.zipml_debug_product_plan(rows, d_out, d_in, dtype, ldy, out)
+    def call(rows=4, d_out=6, d_in=40, dtype=zipml.F32, ldy=6, size=256, out=C.byref(plan)):
+        return lib.zipml_debug_product_plan(rows, d_out, d_in, dtype, ldy, size, out)
     assert call() == zipml.OK
     for kw in ({"rows": 0}, {"d_out": 0}, {"d_in": 0}, {"dtype": 2}, {"ldy": 5}, {"ldy": 1 << 60}, {"out": None}, {"d_out": (1 << 24) + 1, "ldy": 1 << 25}):
         assert call(**kw) == zipml.EINVAL, kw
     assert call(d_in=131072) == zipml.ERANGE
+    assert call(size=255) == call(size=0) == zipml.EWORKSPACE
 
 
 @pytest.mark.parametrize("rows,d_out,d_in", [(1 << 28, 8, 16), ((1 << 28) - 16, 8, 16), (1 << 27, 8, 600), (1 << 27, 16, 600), (1 << 26, 3, 2000),
@@ -170,3 +171,41 @@ def test_more_rows_than_a_launch_of_the_smallest_tiles_holds():
         sums = torch.mm(x[r:r + piece].float(), w.float().t().contiguous())
         assert torch.equal(y[r:r + piece], (sums * sx[r:r + piece, None] * sw).to(torch.bfloat16)), r
     assert (y[rows] == 7.0).all()
+
+
+RANGED = [s for (_, ranges, _), s in PATHS.items() if ranges > 1]
+
+
+@pytest.mark.parametrize("sizes", RANGED)
+def test_less_room_takes_fewer_ranges(lib, sizes):
+    rows, d_out, d_in = sizes
+    need, sums = room(*sizes), rows * (-(-d_out // 4) * 4) * 4
+    most = zipml.debug_product_plan(*sizes).ranges
+    for size in (256, sums, 2 * sums, need - 1, need, need + 1, 1 << 40):
+        p = zipml.debug_product_plan(*sizes, workspace_bytes=max(256, size))
+        assert p.ranges == 1 or p.ranges * sums <= size
+        assert (p.ranges == most) == (size >= need)
+    # the call itself gets past its check of the room (and refuses x, whose address is no multiple of 16)
+    ok, odd = C.c_void_p(0x1000), C.c_void_p(0x1004)
+    ldx = -(-d_in // 16) * 16
+    for size, code in ((256, zipml.EALIGN), (need - 1, zipml.EALIGN), (255, zipml.EWORKSPACE)):
+        assert lib.zipml_row8_product(None, odd, ldx, ok, ok, ldx, ok, None, rows, d_out, d_in, ok, zipml.BF16, d_out, ok, size) == code
+
+
+@pytest.mark.gpu
+def test_the_room_of_one_batch_serves_others():
+    """Of 10,240 -> 2,560, whose need falls and rises with the rows: each call with the room that another number of rows asks for, which
+    leaves what lies behind it as it is."""
+    d_out, d_in, all_rows = 2560, 10240, (300, 1024, 700, 2048)
+    (x, sx), (w, sw) = product_test.codes(2048, d_in, 1), product_test.codes(d_out, d_in, 2)
+    xd, wd, sxd, swd = product_test.on_gpu(x), product_test.on_gpu(w), torch.from_numpy(sx).to(DEV), torch.from_numpy(sw).to(DEV)
+    want = ref.product(x, w, sx, sw, None, torch.float32)
+    needs = sorted({room(r, d_out, d_in) for r in all_rows} | {room(300, d_out, d_in) - 1})
+    assert needs[0] == 256 < needs[1] < needs[-1]
+    for need in needs:
+        ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+        for rows in all_rows:
+            y = torch.full((rows, d_out), float("nan"), device=DEV)
+            zipml.row8_product(xd, d_in, sxd, wd, d_in, swd, rows, d_out, d_in, y, d_out, ws[:need])
+            np.testing.assert_array_equal(y.cpu().numpy(), want[:rows].numpy())
+            assert (ws[need:] == 0xA5).all()
