@@ -435,8 +435,9 @@ int zipml_norm_backward(void *stream, const void *dy_dev, int64_t lddy, const vo
  * tensors_host: n_tensors (1 .. 2^20) descriptions, read before the call returns (a captured graph keeps the addresses in them).
  * Gradients and outputs are aligned to their types; out_dev may be grad_dev itself (of the same type) or NULL where only the norm
  * is wanted; no output may overlap another output or another tensor's gradient.  norm_dev gets {norm, factor}.  Squares are summed
- * in 64 bits in an order of the sizes alone.  A norm that is not finite leaves nothing hidden: an infinity gives factor 0 (and NaN
- * where it stands), a NaN makes all outputs NaN. */
+ * in 64 bits in an order of the sizes alone.  max_norm may be infinite: gradients are measured and copied, not scaled.  A norm that is
+ * not finite leaves nothing hidden: an infinity gives factor 0 (and NaN where it stands) or, with an infinite max_norm, stays as it is;
+ * a NaN makes all outputs NaN. */
 typedef struct {
     const void *grad_dev;
     void *out_dev;
