@@ -384,7 +384,8 @@ int zipml_scan_step(void *stream, const void *x_dev, int64_t ldx, const void *z_
  *   ZIPML_NEAREST: code = t rounded to an integer, ties to even;
  *   ZIPML_STOCHASTIC: code = floor(t + (k + 1/2) / 2^16), at most 127 in magnitude, k a 16-bit draw: v in expectation, to 2^-17 of
  *   the scale.  Draws as those of zipml_act_encode, from (seed, epoch, tag, row, column).
- * A row that holds an infinity or a NaN has a scale of NaN and codes of zero: all it is multiplied with becomes NaN. */
+ * A row that holds an infinity or a NaN has a scale of NaN and codes of zero: all it is multiplied with becomes NaN.  (The largest
+ * number of fp32 itself decodes to an infinity: 127 times its scale rounds to 2^128; the one below it does not.) */
 #define ZIPML_NEAREST    0
 #define ZIPML_STOCHASTIC 1
 int zipml_row8_encode(void *stream, const void *x_dev, int dtype, int64_t rows, int64_t cols, int64_t ldx, int rounding,

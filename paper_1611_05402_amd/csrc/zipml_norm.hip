@@ -3,8 +3,10 @@
 //   r = round(x + add),  rstd = 1 / sqrt(mean r^2 + eps),  n = r rstd,  v = n gain
 //   backward, a = dy gain:  dx = dsum + rstd (a - n mean(a n)),  dgain = sum over the rows of dy n
 //
-// The mean square is summed in 64 bits: with rstd rounded to fp32 once and every further step a single fp32 operation, the codes of
-// a row do not depend on the order of the sum, so they can be checked bit for bit (64-bit adds cost nothing next to the bytes).
+// The mean square is summed in 64 bits (such adds cost nothing next to the bytes), rstd is rounded to fp32 once, and every further step is a single
+// fp32 operation.  The order of the sum, which is another one where a row has more threads (few rows) and in a plain evaluation, moves the
+// mean by some 2^-53 of itself, and rstd's rounding to 24 bits with it in some 2^-28 of all rows: a row's results are all but certain to
+// be the same alone, in a batch and in a check bit for bit, not promised to be.
 //
 // Both passes read and write every byte once and are bound by them.  16,384 x 4,096 bf16: forward 91 to 98 us (two tensors in, the sum
 // and codes out 470 MB, the sum and y 537 MB: 5.0 to 5.6 TB/s), backward 107 to 109 (537 MB, and 17 of dgain's sums), joining these 7.
@@ -160,7 +162,7 @@ struct NormGradArgs {
     int64_t lddy, ldsum, lddsum, lddx, rows, cols, units, pitch;
 };
 
-// A workgroup takes every gridDim.x-th row (or set of rows, one for each wave) and keeps dgain's sums of its rows in registers.  1,024
+// A workgroup takes every gridDim.x-th row (or set of rows, one for each team: a wave, or sixteen lanes) and keeps dgain's sums of its rows in registers.  1,024
 // workgroups: 512 have too few loads under way (157 us in place of 108 at 16,384 x 4,096).  Rows of more than 16,384 values are read
 // twice: the registers of 1,024 threads do not hold four such arrays.
 template <typename T, typename S>
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_backward(NormGradArgs a)
     }
     if constexpr (S::NV > 0) {
         if (!part) return;
-        if constexpr (S::kRows > 1) {      // the four waves' sums
+        if constexpr (S::kRows > 1) {      // the teams' sums: of four waves, or of sixteen times sixteen lanes
             __shared__ float sums[S::kRows - 1][NV][8][S::TPR];
             if (team > 0)
 #pragma unroll

@@ -13,8 +13,8 @@ struct Row8Args {
 };
 
 // A row waits in registers between the search for its largest magnitude and the rounding; rows too long for that are read twice.  Bound by
-// the bytes: 16,384 x 4,096 bf16, 201 MB in 40 to 45 us (4.5 to 5.0 TB/s).  1,000 x 1,001 fp32 by draws: 3.4 us, of which 1.4 are an
-// empty launch.
+// the bytes: 16,384 x 4,096 bf16, 201 MB in 37 to 46 us (4.4 to 5.4 TB/s), by draws 40 to 42 (floor of both 41, at the rate of a copy).
+// 1,000 x 1,001 fp32 by draws: 3.0 to 3.4 us, of which 1.4 are an empty launch.
 template <typename T, typename S, bool DRAWS>
 __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
 {
@@ -62,7 +62,8 @@ __global__ __launch_bounds__(S::kThreads) void k_row8_encode(Row8Args a)
     }
 }
 
-// Four rows of eight columns a thread, as in zipml_act.hip.  16,384 x 4,096 to bf16: 30 to 32 us, the codes out of the cache.
+// Four rows of eight columns a thread, as in zipml_act.hip.  16,384 x 4,096 to bf16: 30 to 32 us, the codes out of the cache that the
+// encoder left them in, 37 out of memory (201 MB, floor 41); to fp32 73 (336 MB, floor 68).  All results go through the caches.
 template <typename T>
 __global__ __launch_bounds__(256) void k_row8_decode(const uint8_t *codes, int64_t ldc, const float *scales, int64_t rows,
                                                      int64_t cols, ActGrid g, T *out, int64_t ldo)

@@ -6,9 +6,10 @@
 //
 // Two kinds of kernels, chosen by a model of their times (product_plan): few tokens or outputs are bound by the bytes of W and by latency
 // (one token, 4,096 x 4,096: 5.4 us, 3.4 at the rate of a copy, 1.4 an empty launch; 64 tokens, 8,192 -> 1,024: 6.0; 1,000 tokens,
-// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw (16,384 tokens, 4,096 x 4,096: 210 us in a long run, to
-// 216 on another box, 2,620 TOP/s; a library product of the same codes without scales 285; 4,096 tokens, 16,384 -> 4,096: 202 us,
-// 2,720 TOP/s, the library 217).  With the first, 134 MB of results go out.
+// 520 -> 1,001, fp32: 6.1), many of both by the power that the matrix cores draw, and a third of their cycles in which they wait (16,384
+// tokens, 4,096 x 4,096: 207 to 220 us from box to box, 2,500 to 2,650 TOP/s, to fp32 221 on the first of them; a library product of the same
+// codes without scales 232 to 285; 4,096 tokens, 16,384 -> 4,096: 195 to 208 us, 2,640 to 2,820 TOP/s, the library 211 to 223).  With the
+// first, 134 MB of results go out.
 #include "zipml_row8.h"
 
 namespace zipml {
@@ -270,7 +271,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_row8_product(ProductArgs a)
     // While a round is multiplied, the next one goes from registers to LDS, and each register is loaded anew for the one after it.  A
     // beat's rows of W are read two beats ahead, all of its tokens' codes in the two beats before their first; so the barrier stands
     // two beats before the round's end.  What a beat reads, stores and loads stands between its products, in this order (216 us in place of
-    // 220 for 16,384 tokens, 4,096 x 4,096, with all of it before them); the compiler otherwise moves all loads to a round's end.
+    // 220 for 16,384 tokens, 4,096 x 4,096, with all of it before them); the compiler otherwise moves all loads to a round's end.  A load
+    // has one round until its register is stored, which is short in 128-wide tiles: by the constants below 0.47 and 0.55 us, their products
+    // alone 0.21 and 0.43.
     i32x4 fw[4], fx[2][S::TT];
     auto read_w = [&](const char *stage, int beat) {
         const int m = beat % S::TO, s = beat / S::TO;
@@ -481,7 +484,8 @@ __global__ __launch_bounds__(256) void k_row8_product_join(ProductArgs a, const 
 //   launch, sums written and read).
 // The constants (us) are those that come nearest to 4,700 times measured over 253 sizes, 1 to 60,000 tokens, 20 to 16,000 outputs, 100 to
 // 32,000 inputs, both types, all shapes and numbers of ranges below; the choice is 3 % slower than the fastest on average, 14 % in one of
-// twenty, a third at most (16 ranges, or k the most for both: 18 % in one of twenty).
+// twenty, a third at most (16 ranges, or k the most for both: 18 % in one of twenty).  They order the shapes; a time by itself may be a fifth
+// off (1,000 tokens, 4,096 x 4,096: 21.7 us by the model, 21.6 to 26 measured).
 struct ProductPlan {
     int shape, ranges, range;              // range: bytes of a row
     size_t workspace;
