@@ -157,9 +157,11 @@ def test_launches_of_all_sizes_fit(lib, rows, d_out, d_in):
 
 
 @pytest.mark.gpu
-def test_more_rows_than_a_launch_of_the_smallest_tiles_holds():
-    """2^28 tokens, all results compared (an elementwise chain of single fp32 operations on exact sums, below 2^24 and so exact in fp32)."""
-    rows, d_out, d_in, piece = 1 << 28, 8, 16, 1 << 24
+@pytest.mark.parametrize("rows,d_out", [(1 << 28, 8), (1 << 31, 3)])
+def test_more_rows_than_a_launch_of_the_smallest_tiles_holds(rows, d_out):
+    """Up to the largest number of tokens, all results compared (an elementwise chain of single fp32 operations on exact sums, below 2^24 and so
+    exact in fp32)."""
+    d_in, piece = 16, 1 << 24
     g = torch.Generator(device=DEV).manual_seed(1)
     x = torch.randint(-127, 128, (rows // 64, d_in), generator=g, device=DEV, dtype=torch.int8).repeat(64, 1)
     w = torch.randint(-127, 128, (d_out, d_in), generator=g, device=DEV, dtype=torch.int8)
